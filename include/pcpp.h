@@ -719,6 +719,147 @@ int pcpp_guided_step(const pcpp_step_params_t* sp, int64_t n, const float* x_t,
                      const float* eps_uncond, const float* eps_cond,
                      const float* z, float* x_prev, void* stream);
 
+/*
+ * Operators of a feed-forward sub-layer with root-mean-square norms, in
+ * inference and training:  s = x + branch;  y = RMSNorm(s);
+ * branch = W2 (value(y) act(gate(y))), with the backward pass of both.
+ *
+ * 8-bit rows.  An activation that the backward pass needs can be kept in 8
+ * bits: groups of 32 consecutive channels share a scale 2^e, and a code is the
+ * e4m3 (OCP: no infinities, largest magnitude 448) nearest to value / 2^e,
+ * ties to even.  e is the smallest integer >= -117 with max |v| / 2^e <= 448
+ * over the group's finite values, so no finite value saturates; infinities and
+ * NaN become NaN.  codes [rows][channels] uint8, scales [rows][channels / 32]
+ * uint8 holding e + 127.  A value read back is exact in bf16 (one within a
+ * step of float32's largest may come back as infinity).
+ */
+
+/*
+ * The two conversions.  x [rows, channels] of dtype (PCPP_DTYPE_F32 or
+ * PCPP_DTYPE_BF16); 1 <= rows <= 2^24, rows * channels <= 2^36; channels a
+ * multiple of 32, <= 65536 (PCPP_ENOTSUP otherwise, and for another dtype); x
+ * and codes 16-byte aligned, no overlap (PCPP_EINVAL).  Asynchronous on
+ * `stream`.
+ */
+int pcpp_checkpoint_save(int64_t rows, int32_t channels, int32_t dtype,
+                         const void* x, void* codes, void* scales,
+                         void* stream);
+int pcpp_checkpoint_load(int64_t rows, int32_t channels, int32_t dtype,
+                         const void* codes, const void* scales, void* x,
+                         void* stream);
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *   s = x + addend;  y = s / sqrt(mean(s^2) + eps) * gamma   over the channels
+ *   x        [rows, channels] of dtype: the residual stream
+ *   addend   [rows, channels] bf16: a branch's output, or NULL (s = x)
+ *   gamma    [channels] bf16
+ *   sum_out  [rows, channels] of dtype: s, or NULL; may be x (in place)
+ *   y        [rows, channels] bf16, or NULL
+ *   codes,   y in 8-bit rows as above, rounded from float32; both or neither,
+ *   scales   channels then a multiple of 32 (PCPP_ENOTSUP otherwise)
+ * y or codes is needed (PCPP_EINVAL).  The norm is that of the sum before it
+ * is rounded to dtype; all of it in float32.  dtype PCPP_DTYPE_F32 or
+ * PCPP_DTYPE_BF16; 1 <= rows <= 2^24; channels a multiple of 8, <= 8192
+ * (PCPP_ENOTSUP otherwise); eps > 0; pointers 16-byte aligned (scales: any),
+ * no overlap but the one named (PCPP_EINVAL).  Asynchronous on `stream`.
+ */
+int pcpp_rms_norm(int64_t rows, int32_t channels, float eps, int32_t dtype,
+                  const void* x, const void* addend, const void* gamma,
+                  void* sum_out, void* y, void* codes, void* scales,
+                  void* stream);
+
+/*
+ * Its backward pass: with n = s / sqrt(mean(s^2) + eps) and w = dy * gamma,
+ *   ds = ds_in + (w - n mean(w n)) / sqrt(mean(s^2) + eps)
+ *   dgamma = sum over the rows of dy * n
+ * ds is the gradient of x and of the addend alike.
+ *   s       [rows, channels] of dtype: the forward pass's sum_out
+ *   dy      [rows, channels] bf16
+ *   ds_in   [rows, channels] of dtype: the gradient that reaches s by the
+ *           residual path, or NULL
+ *   ds      [rows, channels] of dtype; may be ds_in (in place)
+ *   dgamma  [channels] bf16, or NULL (then no workspace is needed); summed in
+ *           float32 in a fixed order
+ * Sizes, types, alignment and errors as pcpp_rms_norm; the workspace needs no
+ * clearing.  Asynchronous on `stream`.
+ */
+size_t pcpp_rms_norm_backward_workspace_size(int64_t rows, int32_t channels);
+int pcpp_rms_norm_backward(int64_t rows, int32_t channels, float eps,
+                           int32_t dtype, const void* s, const void* gamma,
+                           const void* dy, const void* ds_in, void* ds,
+                           void* dgamma, void* workspace, size_t ws_bytes,
+                           void* stream);
+
+/*
+ * Gated feed-forward block, bf16 storage with float32 accumulation:
+ *   [v, g] = x ff1_w^T + ff1_b;  h = v * act(g);  y = h ff2_w^T + ff2_b
+ * act: PCPP_ACT_GELU (exact, g Phi(g)) or PCPP_ACT_SILU (g / (1 + e^-g)).
+ */
+#define PCPP_ACT_GELU 0
+#define PCPP_ACT_SILU 1
+
+typedef struct {
+    int64_t tokens;        /* M, 1 .. 2^24; M * F <= 2^36                    */
+    int32_t channels;      /* C, a multiple of 64, <= 8192                   */
+    int32_t ff_inner;      /* F, a multiple of 64, <= 65536                  */
+    int32_t act;           /* PCPP_ACT_GELU or PCPP_ACT_SILU                 */
+    int32_t reserved;      /* must be 0                                      */
+} pcpp_ff_geom_t;
+
+/* Device pointers, bf16, 16-byte aligned, as in pcpp_block_weights_t. */
+typedef struct {
+    const void* ff1_w;     /* [2F, C] rows [0,F) value, [F,2F) gate          */
+    const void* ff1_b;     /* [2F] or NULL                                   */
+    const void* ff2_w;     /* [C, F]                                         */
+    const void* ff2_b;     /* [C] or NULL                                    */
+} pcpp_ff_weights_t;
+
+/* Their gradients, in the same layouts and type; NULL: not wanted. */
+typedef struct {
+    void* ff1_w;
+    void* ff1_b;
+    void* ff2_w;
+    void* ff2_b;
+} pcpp_ff_grads_t;
+
+/*
+ * Forward.  x [M, C], y [M, C] bf16.  pre_codes [M, 2F], pre_scales
+ * [M, 2F / 32]: NULL (inference), or they receive v and g (in that order along
+ * a row) as 8-bit rows, rounded from float32: what the backward pass reads.
+ * The workspace (h and partial sums) needs no clearing; nothing in it survives
+ * a call.  Errors: PCPP_EINVAL (geometry, NULL or misaligned pointers -
+ * 16 bytes, pre_scales any - or overlaps), PCPP_ENOTSUP (C, F or act),
+ * PCPP_EWORKSPACE.  Asynchronous on `stream`.
+ */
+size_t pcpp_gated_ff_workspace_size(const pcpp_ff_geom_t* g);
+int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w,
+                  const void* x, void* y, void* pre_codes, void* pre_scales,
+                  void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Backward, from the 8-bit checkpoint of v and g (no product is computed
+ * again):
+ *   dh = dy ff2_w;  dv = dh * act(g);  dg = dh * v * act'(g);  h = v * act(g)
+ *   dx = [dv, dg] ff1_w;  d ff1_w = [dv, dg]^T x;  d ff1_b = their sums
+ *   d ff2_w = dy^T h;  d ff2_b = sums of dy
+ *   x         [M, C] bf16 with x_scales NULL, or 8-bit codes [M, C] with
+ *             x_scales [M, C / 32] (pcpp_rms_norm's, or pcpp_checkpoint_save's)
+ *   dy        [M, C] bf16;  dx [M, C] bf16 or NULL
+ *   grads     NULL, or the parameters' gradients; overwritten, in bf16,
+ *             summed in float32 in a fixed order
+ * dx or a gradient is needed (PCPP_EINVAL).  The biases of w are not read.
+ * [dv, dg] and h pass through the workspace in bf16.  Otherwise as
+ * pcpp_gated_ff.
+ */
+size_t pcpp_gated_ff_backward_workspace_size(const pcpp_ff_geom_t* g);
+int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w,
+                           const void* x, const void* x_scales,
+                           const void* pre_codes, const void* pre_scales,
+                           const void* dy, void* dx,
+                           const pcpp_ff_grads_t* grads, void* workspace,
+                           size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,124 @@
+// 8-bit activation checkpoints: rows to codes and scales, and back.
+//   pcpp_checkpoint_save, pcpp_checkpoint_load
+
+#include <stdint.h>
+
+#include "../../include/pcpp.h"
+#include "args.h"
+#include "checkpoint.h"
+#include "common.h"
+#include "eight_bit.h"
+#include "rows8.h"
+
+#define PCPP_EXPORT extern "C" __attribute__((visibility("default")))
+
+namespace pcpp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;
+
+// Both kernels see the rows as one run of n8 chunks of eight channels (a
+// row's channels are a multiple of 32, so no group crosses its end).
+template <typename T>
+__global__ __launch_bounds__(kThreads) void checkpoint_save(const T* x, uint8_t* codes, uint8_t* scales, int64_t n8) {
+    const int64_t i0 = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
+    float v[kUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+        if (i < n8) load8(x + i * 8, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+        if (i >= n8) break;  // n8 is a multiple of four: a group's lanes leave together
+        int scale;
+        *(u32x2*)(codes + i * 8) = to_eight_bits(v[u], scale);
+        if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)scale;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void checkpoint_load(const uint8_t* codes, const uint8_t* scales, T* y,
+                                                            int64_t n8) {
+    const int64_t i0 = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
+    u32x2 c[kUnroll];
+    int s[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+        if (i < n8) {
+            c[u] = *(const u32x2*)(codes + i * 8);
+            s[u] = scales[i >> 2];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+        if (i >= n8) break;
+        const float f = eight_value(s[u]);
+        const f32x4 a = from_e4m3(c[u][0]), b = from_e4m3(c[u][1]);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a[e] * f;
+            v[4 + e] = b[e] * f;
+        }
+        store8(y + i * 8, v);
+    }
+}
+
+unsigned blocks_of(int64_t n8) { return (unsigned)((n8 + kThreads * kUnroll - 1) / (kThreads * kUnroll)); }
+
+}  // namespace
+
+hipError_t launch_checkpoint_load_bf16(const void* codes, const void* scales, void* y, int64_t n, hipStream_t s) {
+    checkpoint_load<bf16><<<blocks_of(n / 8), kThreads, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, (bf16*)y,
+                                                                n / 8);
+    return hipGetLastError();
+}
+
+}  // namespace pcpp
+
+using namespace pcpp;
+
+// Sizes, type and pointers of both calls; `x` the rows in full precision.
+static int check_checkpoint(int64_t rows, int32_t channels, int32_t dtype, const void* x, const void* codes,
+                            const void* scales) {
+    if (rows < 1 || rows > ((int64_t)1 << 24) || channels < 1) return PCPP_EINVAL;
+    if (dtype != PCPP_DTYPE_F32 && dtype != PCPP_DTYPE_BF16) return PCPP_ENOTSUP;
+    if (channels % EIGHT_GROUP != 0 || channels > (1 << 16)) return PCPP_ENOTSUP;
+    if (!x || !codes || !scales || !aligned_to(x, 16) || !aligned_to(codes, 16)) return PCPP_EINVAL;
+    const int64_t n = rows * channels;
+    if (n > ((int64_t)1 << 36)) return PCPP_EINVAL;  // a launch has fewer than 2^32 threads
+    const Range all[] = {{x, n * (dtype == PCPP_DTYPE_F32 ? 4 : 2)}, {codes, n}, {scales, n / EIGHT_GROUP}};
+    return outputs_overlap(all, 3, nullptr, 0) ? PCPP_EINVAL : PCPP_OK;
+}
+
+PCPP_EXPORT int pcpp_checkpoint_save(int64_t rows, int32_t channels, int32_t dtype, const void* x, void* codes,
+                                     void* scales, void* stream) {
+    const int st = check_checkpoint(rows, channels, dtype, x, codes, scales);
+    if (st != PCPP_OK) return st;
+    const int64_t n8 = rows * channels / 8;
+    if (dtype == PCPP_DTYPE_F32)
+        checkpoint_save<<<blocks_of(n8), kThreads, 0, (hipStream_t)stream>>>((const float*)x, (uint8_t*)codes,
+                                                                             (uint8_t*)scales, n8);
+    else
+        checkpoint_save<<<blocks_of(n8), kThreads, 0, (hipStream_t)stream>>>((const bf16*)x, (uint8_t*)codes,
+                                                                             (uint8_t*)scales, n8);
+    return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}
+
+PCPP_EXPORT int pcpp_checkpoint_load(int64_t rows, int32_t channels, int32_t dtype, const void* codes,
+                                     const void* scales, void* y, void* stream) {
+    const int st = check_checkpoint(rows, channels, dtype, y, codes, scales);
+    if (st != PCPP_OK) return st;
+    const int64_t n = rows * channels;
+    if (dtype == PCPP_DTYPE_BF16)
+        return launch_checkpoint_load_bf16(codes, scales, y, n, (hipStream_t)stream) == hipSuccess ? PCPP_OK : PCPP_EHIP;
+    checkpoint_load<<<blocks_of(n / 8), kThreads, 0, (hipStream_t)stream>>>((const uint8_t*)codes,
+                                                                            (const uint8_t*)scales, (float*)y, n / 8);
+    return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}

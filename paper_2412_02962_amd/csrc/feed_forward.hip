@@ -1,0 +1,213 @@
+// The gated feed-forward block and its backward pass (C ABI).
+//   pcpp_gated_ff           [v, g] = x W1^T + b1;  h = v act(g);  y = h W2^T + b2:
+//                           both projections, the activation and the product
+//                           in one kernel (which also writes the 8-bit
+//                           checkpoint of v and g), then the down projection
+//   pcpp_gated_ff_backward  one product dh = dy W2 whose epilogue reads the
+//                           checkpoint and leaves dpre = [dv, dg], h and the
+//                           columns' sums, then dx = dpre W1, dW1 = dpre^T x
+//                           and dW2 = dy^T h
+
+#include "feed_forward.h"
+
+#include "../../include/pcpp.h"
+#include "args.h"
+#include "checkpoint.h"
+#include "column_sums.h"
+#include "eight_bit.h"
+
+#define PCPP_EXPORT extern "C" __attribute__((visibility("default")))
+
+namespace pcpp {
+
+namespace {
+
+constexpr int kMaxC = 8192, kMaxF = 1 << 16;
+
+int check_geom(const pcpp_ff_geom_t* g) {
+    if (!g || g->reserved != 0 || g->tokens < 1 || g->tokens > ((int64_t)1 << 24) || g->channels < 1 || g->ff_inner < 1)
+        return PCPP_EINVAL;
+    if (g->act != PCPP_ACT_GELU && g->act != PCPP_ACT_SILU) return PCPP_ENOTSUP;
+    if (g->channels % 64 != 0 || g->channels > kMaxC || g->ff_inner % 64 != 0 || g->ff_inner > kMaxF) return PCPP_ENOTSUP;
+    // a launch has fewer than 2^32 threads
+    return g->tokens * g->ff_inner > ((int64_t)1 << 36) ? PCPP_EINVAL : PCPP_OK;
+}
+
+// Byte offsets within a workspace, every part 256-byte aligned.
+struct Layout {
+    size_t size = 0;
+    size_t add(int64_t bytes) {
+        const size_t at = size;
+        size += ((size_t)bytes + 255) & ~(size_t)255;
+        return at;
+    }
+};
+
+struct BackwardLayout : Layout {
+    size_t x, dpre, h, sums1, sums2;
+    explicit BackwardLayout(const pcpp_ff_geom_t& g) {
+        const int64_t M = g.tokens, C = g.channels, F = g.ff_inner;
+        x = add(2 * M * C);
+        dpre = add(4 * M * F);
+        h = add(2 * M * F);
+        sums1 = add((int64_t)ff_partial_rows(M) * 2 * F * 4);
+        sums2 = add((int64_t)column_partial_rows(M) * C * 4);
+    }
+};
+
+bool all_aligned(const Range* r, int n) {
+    for (int i = 0; i < n; ++i)
+        if (!aligned_to(r[i].p, 16)) return false;
+    return true;
+}
+
+}  // namespace
+
+}  // namespace pcpp
+
+using namespace pcpp;
+
+PCPP_EXPORT size_t pcpp_gated_ff_workspace_size(const pcpp_ff_geom_t* g) {
+    if (check_geom(g) != PCPP_OK) return 0;
+    Layout l;
+    l.add(2 * g->tokens * g->ff_inner);
+    return l.size;
+}
+
+PCPP_EXPORT int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w, const void* x, void* y,
+                              void* pre_codes, void* pre_scales, void* workspace, size_t ws_bytes, void* stream) {
+    const int st = check_geom(g);
+    if (st != PCPP_OK) return st;
+    if (!w || !w->ff1_w || !w->ff2_w || !x || !y || (pre_codes == nullptr) != (pre_scales == nullptr)) return PCPP_EINVAL;
+    const int64_t M = g->tokens, C = g->channels, F = g->ff_inner;
+    const size_t need = pcpp_gated_ff_workspace_size(g);
+    if (!workspace || ws_bytes < need) return PCPP_EWORKSPACE;
+    const Range in[] = {{x, 2 * M * C}, {w->ff1_w, 4 * F * C}, {w->ff1_b, 4 * F}, {w->ff2_w, 2 * C * F}, {w->ff2_b, 2 * C}};
+    const Range out[] = {{y, 2 * M * C}, {workspace, (int64_t)need}, {pre_codes, 2 * M * F}, {pre_scales, 2 * M * F / EIGHT_GROUP}};
+    if (!all_aligned(in, 5) || !all_aligned(out, 3) || outputs_overlap(out, 4, in, 5)) return PCPP_EINVAL;
+    const hipStream_t s = (hipStream_t)stream;
+    FfProduct up = {};
+    up.x = (const bf16*)x;
+    up.w = (const bf16*)w->ff1_w;
+    up.ldx = up.ldw = C;
+    up.M = (int32_t)M;
+    up.N = (int32_t)F;
+    up.K = (int32_t)C;
+    up.epilogue = FF_GATE;
+    up.act = g->act;
+    up.out = (bf16*)workspace;
+    up.bias = (const bf16*)w->ff1_b;
+    up.codes = (uint8_t*)pre_codes;
+    up.scales = (uint8_t*)pre_scales;
+    if (launch_ff_product(up, s) != hipSuccess) return PCPP_EHIP;
+    FfProduct down = {};
+    down.x = (const bf16*)workspace;
+    down.w = (const bf16*)w->ff2_w;
+    down.ldx = down.ldw = F;
+    down.M = (int32_t)M;
+    down.N = (int32_t)C;
+    down.K = (int32_t)F;
+    down.epilogue = FF_STORE;
+    down.out = (bf16*)y;
+    down.bias = (const bf16*)w->ff2_b;
+    return launch_ff_product(down, s) == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}
+
+PCPP_EXPORT size_t pcpp_gated_ff_backward_workspace_size(const pcpp_ff_geom_t* g) {
+    return check_geom(g) == PCPP_OK ? BackwardLayout(*g).size : 0;
+}
+
+PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w, const void* x,
+                                       const void* x_scales, const void* pre_codes, const void* pre_scales,
+                                       const void* dy, void* dx, const pcpp_ff_grads_t* grads, void* workspace,
+                                       size_t ws_bytes, void* stream) {
+    const int st = check_geom(g);
+    if (st != PCPP_OK) return st;
+    const pcpp_ff_grads_t none = {};
+    const pcpp_ff_grads_t& d = grads ? *grads : none;
+    if (!w || !w->ff1_w || !w->ff2_w || !x || !pre_codes || !pre_scales || !dy) return PCPP_EINVAL;
+    if (!dx && !d.ff1_w && !d.ff1_b && !d.ff2_w && !d.ff2_b) return PCPP_EINVAL;
+    const int64_t M = g->tokens, C = g->channels, F = g->ff_inner;
+    const BackwardLayout l(*g);
+    if (!workspace || ws_bytes < l.size) return PCPP_EWORKSPACE;
+    const Range in[] = {{x, (x_scales ? 1 : 2) * M * C}, {pre_codes, 2 * M * F}, {dy, 2 * M * C}, {w->ff1_w, 4 * F * C},
+                        {w->ff2_w, 2 * C * F}, {x_scales, M * C / EIGHT_GROUP}, {pre_scales, 2 * M * F / EIGHT_GROUP}};
+    const Range out[] = {{dx, 2 * M * C}, {d.ff1_w, 4 * F * C}, {d.ff1_b, 4 * F}, {d.ff2_w, 2 * C * F}, {d.ff2_b, 2 * C},
+                         {workspace, (int64_t)l.size}};
+    if (!all_aligned(in, 5) || !all_aligned(out, 6) || outputs_overlap(out, 6, in, 7)) return PCPP_EINVAL;
+    const hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    bf16 *dpre = (bf16*)(ws + l.dpre), *h = (bf16*)(ws + l.h);
+    float *sums1 = (float*)(ws + l.sums1), *sums2 = (float*)(ws + l.sums2);
+    if (dx || d.ff1_w || d.ff1_b || d.ff2_w) {
+        FfProduct p = {};
+        p.x = (const bf16*)dy;
+        p.w = (const bf16*)w->ff2_w;
+        p.ldx = C;
+        p.ldw = F;
+        p.w_t = 1;
+        p.M = (int32_t)M;
+        p.N = (int32_t)F;
+        p.K = (int32_t)C;
+        p.epilogue = FF_GATE_GRAD;
+        p.act = g->act;
+        p.out = dx || d.ff1_w ? dpre : nullptr;
+        p.codes = (uint8_t*)const_cast<void*>(pre_codes);
+        p.scales = (uint8_t*)const_cast<void*>(pre_scales);
+        p.h = d.ff2_w ? h : nullptr;
+        p.partial = d.ff1_b ? sums1 : nullptr;
+        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
+    }
+    if (d.ff1_b && launch_sum_partials(sums1, ff_partial_rows(M), (int)(2 * F), d.ff1_b, s) != hipSuccess) return PCPP_EHIP;
+    if (d.ff2_b && (launch_column_partials(dy, M, (int)C, sums2, s) != hipSuccess ||
+                    launch_sum_partials(sums2, column_partial_rows(M), (int)C, d.ff2_b, s) != hipSuccess))
+        return PCPP_EHIP;
+    if (dx) {
+        FfProduct p = {};
+        p.x = dpre;
+        p.w = (const bf16*)w->ff1_w;
+        p.ldx = 2 * F;
+        p.ldw = C;
+        p.w_t = 1;
+        p.M = (int32_t)M;
+        p.N = (int32_t)C;
+        p.K = (int32_t)(2 * F);
+        p.epilogue = FF_STORE;
+        p.out = (bf16*)dx;
+        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
+    }
+    if (d.ff1_w) {
+        const void* x16 = x;
+        if (x_scales) {
+            if (launch_checkpoint_load_bf16(x, x_scales, ws + l.x, M * C, s) != hipSuccess) return PCPP_EHIP;
+            x16 = ws + l.x;
+        }
+        FfProduct p = {};
+        p.x = dpre;
+        p.w = (const bf16*)x16;
+        p.ldx = 2 * F;
+        p.ldw = C;
+        p.x_t = p.w_t = 1;
+        p.M = (int32_t)(2 * F);
+        p.N = (int32_t)C;
+        p.K = (int32_t)M;
+        p.epilogue = FF_STORE;
+        p.out = (bf16*)d.ff1_w;
+        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
+    }
+    if (d.ff2_w) {
+        FfProduct p = {};
+        p.x = (const bf16*)dy;
+        p.w = h;
+        p.ldx = C;
+        p.ldw = F;
+        p.x_t = p.w_t = 1;
+        p.M = (int32_t)C;
+        p.N = (int32_t)F;
+        p.K = (int32_t)M;
+        p.epilogue = FF_STORE;
+        p.out = (bf16*)d.ff2_w;
+        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
+    }
+    return PCPP_OK;
+}

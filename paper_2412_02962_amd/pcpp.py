@@ -117,6 +117,28 @@ class pcpp_step_params_t(ctypes.Structure):
     ]
 
 
+PCPP_ACT_GELU = 0
+PCPP_ACT_SILU = 1
+
+
+class pcpp_ff_geom_t(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_int64), ("channels", ctypes.c_int32), ("ff_inner", ctypes.c_int32),
+        ("act", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+FF_PTR_FIELDS = ("ff1_w", "ff1_b", "ff2_w", "ff2_b")
+
+
+class pcpp_ff_weights_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in FF_PTR_FIELDS]
+
+
+class pcpp_ff_grads_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in FF_PTR_FIELDS]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built: run __graft_entry__.build() "
@@ -126,6 +148,7 @@ def _load():
     gp = ctypes.POINTER(pcpp_geom_t)
     wp = ctypes.POINTER(pcpp_block_weights_t)
     i32p = ctypes.POINTER(ctypes.c_int32)
+    fp, fwp = ctypes.POINTER(pcpp_ff_geom_t), ctypes.POINTER(pcpp_ff_weights_t)
     sig = {
         "pcpp_version": (ctypes.c_int, []),
         "pcpp_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -166,6 +189,15 @@ def _load():
         "pcpp_conv3x3": (ctypes.c_int, [ctypes.POINTER(pcpp_conv_geom_t)] + [vp] * 7 + [sz, vp]),
         "pcpp_conv3x3_export": (ctypes.c_int, [ctypes.POINTER(pcpp_conv_geom_t)] + [vp] * 9 + [sz, vp]),
         "pcpp_conv3x3_plan": (ctypes.c_int, [ctypes.POINTER(pcpp_conv_geom_t), i32, i32, vp, i32p, i32p, i32p]),
+        "pcpp_checkpoint_save": (ctypes.c_int, [ctypes.c_int64, i32, i32, vp, vp, vp, vp]),
+        "pcpp_checkpoint_load": (ctypes.c_int, [ctypes.c_int64, i32, i32, vp, vp, vp, vp]),
+        "pcpp_rms_norm": (ctypes.c_int, [ctypes.c_int64, i32, ctypes.c_float, i32] + [vp] * 8),
+        "pcpp_rms_norm_backward_workspace_size": (sz, [ctypes.c_int64, i32]),
+        "pcpp_rms_norm_backward": (ctypes.c_int, [ctypes.c_int64, i32, ctypes.c_float, i32] + [vp] * 7 + [sz, vp]),
+        "pcpp_gated_ff_workspace_size": (sz, [fp]),
+        "pcpp_gated_ff": (ctypes.c_int, [fp, fwp] + [vp] * 5 + [sz, vp]),
+        "pcpp_gated_ff_backward_workspace_size": (sz, [fp]),
+        "pcpp_gated_ff_backward": (ctypes.c_int, [fp, fwp] + [vp] * 6 + [ctypes.POINTER(pcpp_ff_grads_t), vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -187,6 +219,9 @@ EXPORTED = (
     "pcpp_conv3x3_workspace_size", "pcpp_conv3x3", "pcpp_conv3x3_export", "pcpp_conv3x3_plan",
     "pcpp_transformer_module_workspace_size", "pcpp_transformer_module",
     "pcpp_concat_channels", "pcpp_layer_norm", "pcpp_group_norm_workspace_size", "pcpp_group_norm",
+    "pcpp_checkpoint_save", "pcpp_checkpoint_load", "pcpp_rms_norm", "pcpp_rms_norm_backward_workspace_size",
+    "pcpp_rms_norm_backward", "pcpp_gated_ff_workspace_size", "pcpp_gated_ff",
+    "pcpp_gated_ff_backward_workspace_size", "pcpp_gated_ff_backward",
 )
 
 
@@ -486,3 +521,61 @@ def pcpp_group_norm(batch, tokens, channels, groups, eps, silu, x, gamma, beta, 
     _check("pcpp_group_norm", _lib.pcpp_group_norm(batch, tokens, channels, groups, eps, silu, _ptr(x), _ptr(gamma),
                                                     _ptr(beta), _ptr(bands), n_bands, band, _ptr(own_out), _ptr(y),
                                                     _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pcpp_checkpoint_save(rows, channels, dtype, x, codes, scales, stream=None):
+    _check("pcpp_checkpoint_save", _lib.pcpp_checkpoint_save(rows, channels, dtype, _ptr(x), _ptr(codes), _ptr(scales),
+                                                              _stream(stream)))
+
+
+def pcpp_checkpoint_load(rows, channels, dtype, codes, scales, x, stream=None):
+    _check("pcpp_checkpoint_load", _lib.pcpp_checkpoint_load(rows, channels, dtype, _ptr(codes), _ptr(scales), _ptr(x),
+                                                              _stream(stream)))
+
+
+def pcpp_rms_norm(rows, channels, eps, dtype, x, addend, gamma, sum_out, y, codes=None, scales=None, stream=None):
+    _check("pcpp_rms_norm", _lib.pcpp_rms_norm(rows, channels, eps, dtype, _ptr(x), _ptr(addend), _ptr(gamma),
+                                                _ptr(sum_out), _ptr(y), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def pcpp_rms_norm_backward_workspace_size(rows, channels) -> int:
+    return _lib.pcpp_rms_norm_backward_workspace_size(rows, channels)
+
+
+def pcpp_rms_norm_backward(rows, channels, eps, dtype, s, gamma, dy, ds_in, ds, dgamma, workspace=None, ws_bytes=0,
+                           stream=None):
+    _check("pcpp_rms_norm_backward", _lib.pcpp_rms_norm_backward(
+        rows, channels, eps, dtype, _ptr(s), _ptr(gamma), _ptr(dy), _ptr(ds_in), _ptr(ds), _ptr(dgamma),
+        _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def make_ff_geom(tokens, channels, ff_inner, act=PCPP_ACT_GELU, reserved=0) -> pcpp_ff_geom_t:
+    return pcpp_ff_geom_t(tokens, channels, ff_inner, act, reserved)
+
+
+def make_ff_weights(tensors: dict) -> pcpp_ff_weights_t:
+    return pcpp_ff_weights_t(*[_ptr(tensors.get(name)) for name in FF_PTR_FIELDS])
+
+
+def make_ff_grads(tensors: dict) -> pcpp_ff_grads_t:
+    return pcpp_ff_grads_t(*[_ptr(tensors.get(name)) for name in FF_PTR_FIELDS])
+
+
+def pcpp_gated_ff_workspace_size(g) -> int:
+    return _lib.pcpp_gated_ff_workspace_size(ctypes.byref(g))
+
+
+def pcpp_gated_ff(g, w, x, y, pre_codes, pre_scales, workspace, ws_bytes, stream=None):
+    _check("pcpp_gated_ff", _lib.pcpp_gated_ff(ctypes.byref(g), ctypes.byref(w), _ptr(x), _ptr(y), _ptr(pre_codes),
+                                                _ptr(pre_scales), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pcpp_gated_ff_backward_workspace_size(g) -> int:
+    return _lib.pcpp_gated_ff_backward_workspace_size(ctypes.byref(g))
+
+
+def pcpp_gated_ff_backward(g, w, x, x_scales, pre_codes, pre_scales, dy, dx, grads, workspace, ws_bytes, stream=None):
+    """grads: a pcpp_ff_grads_t or None."""
+    _check("pcpp_gated_ff_backward", _lib.pcpp_gated_ff_backward(
+        ctypes.byref(g), ctypes.byref(w), _ptr(x), _ptr(x_scales), _ptr(pre_codes), _ptr(pre_scales), _ptr(dy),
+        _ptr(dx), None if grads is None else ctypes.byref(grads), _ptr(workspace), ws_bytes, _stream(stream)))
