@@ -22,6 +22,13 @@ HIPCC_FLAGS = [
     "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-I", os.path.join(ROOT, "include"),
 ]
+# sources whose wavefronts' sums fill the accumulation registers
+ACC_FORM_SOURCES = ("ff_product.hip",)
+
+
+def flags_of(src):
+    at = HIPCC_FLAGS.index("-mllvm") if os.path.basename(src) in ACC_FORM_SOURCES else len(HIPCC_FLAGS)
+    return HIPCC_FLAGS[:at] + HIPCC_FLAGS[at + 2:]
 
 
 def hipcc():
@@ -58,7 +65,7 @@ def scratch_users(remarks):
 
 def _compile(src):
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
-    cmd = [hipcc()] + HIPCC_FLAGS + RESOURCE_REMARKS + ["-c", src, "-o", obj]
+    cmd = [hipcc()] + flags_of(src) + RESOURCE_REMARKS + ["-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     lines = (r.stderr or "").splitlines()
     errs = "\n".join(l for l in lines if "packed-fp32-ops" not in l and "kernel-resource-usage" not in l)
