@@ -60,8 +60,9 @@ __device__ __forceinline__ u32x2 to_eight_bits(const float (&v)[8], int& scale) 
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(v[i]));
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
+    // the other three lanes' by quad permutations (lanes 1 0 3 2, then 2 3 0 1)
+    top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0xB1, 0xF, 0xF, true)));
+    top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xF, 0xF, true)));
     scale = eight_scale(top);
     const float inv = eight_inverse(scale);
     float t[8];

@@ -31,8 +31,13 @@ struct FfProduct {
     uint8_t* scales;      // [M, 2N / 32]
     bf16* h;              // FF_GATE_GRAD: [M, N] or null
     float* partial;       // FF_GATE_GRAD: [ff_partial_rows(M)][2N] sums of out over rows, or null
+    int32_t tiles, n_xcd, per_xcd;  // set by the launch
 };
 int ff_partial_rows(int64_t M);
+// A product with X along the contraction (w_t as the epilogue has it: only
+// FF_GATE_GRAD's W lies across it).
 hipError_t launch_ff_product(const FfProduct& p, hipStream_t s);
+// Up to three products of FF_STORE with w_t = 1, those with x_t = 1 first, in one launch.
+hipError_t launch_ff_products(const FfProduct* p, int n, hipStream_t s);
 
 }  // namespace pcpp

@@ -162,27 +162,15 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
     if (d.ff2_b && (launch_column_partials(dy, M, (int)C, sums2, s) != hipSuccess ||
                     launch_sum_partials(sums2, column_partial_rows(M), (int)C, d.ff2_b, s) != hipSuccess))
         return PCPP_EHIP;
-    if (dx) {
-        FfProduct p = {};
-        p.x = dpre;
-        p.w = (const bf16*)w->ff1_w;
-        p.ldx = 2 * F;
-        p.ldw = C;
-        p.w_t = 1;
-        p.M = (int32_t)M;
-        p.N = (int32_t)C;
-        p.K = (int32_t)(2 * F);
-        p.epilogue = FF_STORE;
-        p.out = (bf16*)dx;
-        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
-    }
+    FfProduct group[3] = {};
+    int n = 0;
     if (d.ff1_w) {
         const void* x16 = x;
         if (x_scales) {
             if (launch_checkpoint_load_bf16(x, x_scales, ws + l.x, M * C, s) != hipSuccess) return PCPP_EHIP;
             x16 = ws + l.x;
         }
-        FfProduct p = {};
+        FfProduct& p = group[n++];
         p.x = dpre;
         p.w = (const bf16*)x16;
         p.ldx = 2 * F;
@@ -191,12 +179,10 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         p.M = (int32_t)(2 * F);
         p.N = (int32_t)C;
         p.K = (int32_t)M;
-        p.epilogue = FF_STORE;
         p.out = (bf16*)d.ff1_w;
-        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
     }
     if (d.ff2_w) {
-        FfProduct p = {};
+        FfProduct& p = group[n++];
         p.x = (const bf16*)dy;
         p.w = h;
         p.ldx = C;
@@ -205,9 +191,20 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         p.M = (int32_t)C;
         p.N = (int32_t)F;
         p.K = (int32_t)M;
-        p.epilogue = FF_STORE;
         p.out = (bf16*)d.ff2_w;
-        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
     }
+    if (dx) {
+        FfProduct& p = group[n++];
+        p.x = dpre;
+        p.w = (const bf16*)w->ff1_w;
+        p.ldx = 2 * F;
+        p.ldw = C;
+        p.w_t = 1;
+        p.M = (int32_t)M;
+        p.N = (int32_t)C;
+        p.K = (int32_t)(2 * F);
+        p.out = (bf16*)dx;
+    }
+    if (n && launch_ff_products(group, n, s) != hipSuccess) return PCPP_EHIP;
     return PCPP_OK;
 }

@@ -6,6 +6,7 @@
 #include "eight_bit.h"
 #include "feed_forward.h"
 #include "ff_act.h"
+#include "kernels.h"
 #include "rows8.h"
 
 namespace pcpp {
@@ -52,7 +53,7 @@ struct Operand {
     uint32_t voff[PIECES];
     uint32_t most;       // bytes that a k-tile may reach from base
 
-    static __device__ __forceinline__ int swizzle(int k) { return R == 64 ? (k >> 1) & 1 : k & 3; }
+    static constexpr __device__ __forceinline__ int swizzle(int k) { return R == 64 ? (k >> 1) & 1 : k & 3; }
 
     // Rows row0 .. of `rows`; row_of(r) is tile row r's row (T = false: any, T
     // = true: row0 + r, R of them in a run).
@@ -126,111 +127,44 @@ struct View {
     }
 };
 
-// The tile `tile` of product p.
-template <int BM, int BN, int WM, bool XT, bool WT, int EPI>
-__device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char* lds) {
+// Tile `tile` of the product's rows and outputs: groups of kGroup tiles along
+// the rows, walked along the outputs.  An XCD takes a run of tiles; the 32 that
+// it works on at a time are then about 8 x 4 and share their operands in its L2.
+constexpr int kGroup = 8;
+template <int BM, int BNO>
+__device__ __forceinline__ void place(const FfProduct& p, int tile, int& m0, int& n0) {
+    const int mt = (p.M + BM - 1) / BM, nt = (p.N + BNO - 1) / BNO;
+    const int group = tile / (kGroup * nt), in = tile - group * kGroup * nt;
+    const int rows = min(kGroup, mt - group * kGroup);
+    n0 = in / rows * BNO;
+    m0 = (group * kGroup + in % rows) * BM;
+}
+
+// The tile of workgroup b: workgroups are dealt round-robin over the XCDs, an
+// XCD's tiles are a run of p.per_xcd (the last may have fewer).
+__device__ __forceinline__ int tile_of(const FfProduct& p, int b) {
+    const int xcd = b % p.n_xcd, j = b / p.n_xcd;
+    const int tile = xcd * p.per_xcd + j;
+    return tile < p.tiles ? tile : -1;
+}
+
+// The outputs of a tile from its wavefronts' sums (BM / WM x BN / WN each).
+template <int BM, int BN, int WM, int EPI, int ACT>
+__device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN * WM / (32 * WAVES)][BM / (32 * WM)], int m0,
+                                           int n0, char* lds) {
     constexpr int WN = WAVES / WM;
-    constexpr int TM = BM / WM, TN = BN / WN;  // X and W rows of a wavefront
-    constexpr int MB = TM / 32, NB = TN / 32;  // its 32 x 32 blocks
-    constexpr int STAGE = (BM + BN) * KT * 2;
-    constexpr int BNO = EPI == FF_GATE ? BN / 2 : BN;  // outputs of a tile
-    static_assert(EPI != FF_GATE || TN % 64 == 0, "value and gate in one wavefront");
+    constexpr int TM = BM / WM, TN = BN / WN;
+    constexpr int MB = TM / 32, NB = TN / 32;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    const int n_tiles = (p.N + BNO - 1) / BNO;
-    const int m0 = tile / n_tiles * BM, n0 = tile % n_tiles * BNO;
-
-    Operand<BM, XT> x;
-    Operand<BN, WT> w;
-    x.init(p.x, p.ldx, p.M, m0, p.K, [](int r) { return (int64_t)r; });
-    if constexpr (EPI == FF_GATE)  // of every 64 rows 32 are values, 32 their gates
-        w.init(p.w, p.ldw, 2 * (int64_t)p.N, n0, p.K,
-               [&](int r) { return (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0); });
-    else
-        w.init(p.w, p.ldw, p.N, n0, p.K, [](int r) { return (int64_t)r; });
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
-    const View<BM, XT> xv(lds0, wm * TM);
-    const View<BN, WT> wv(lds0 + BM * KT * 2, wn * TN);
-
-    f32x16 acc[NB][MB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < MB; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    struct Ops {
-        bf16x8 x[MB], w[NB];
-    };
-    Ops o[2];
-#pragma unroll
-    for (int j = 0; j < MB; ++j) o[1].x[j] = bf16x8{};
-#pragma unroll
-    for (int i = 0; i < NB; ++i) o[1].w[i] = bf16x8{};
-
-    constexpr int PX = decltype(x)::PIECES, PW = decltype(w)::PIECES;
-    const int nkt = (p.K + KT - 1) / KT;
-    {
-        const u32x4 xb = x.buffer(), wb = w.buffer();
-#pragma unroll
-        for (int q = 0; q < PX; ++q) x.load(xb, q, lds0);
-#pragma unroll
-        for (int q = 0; q < PW; ++q) w.load(wb, q, lds0 + BM * KT * 2);
-    }
-    // The k-tiles alternate between two stages.  A step's operands are read
-    // behind the products of the step before, a tile's first ones behind the
-    // last of the tile before it (the first tile's are products with zeros);
-    // the next tile's loads are spread over the steps.
-    uint32_t slot = 0;
-    for (int t = 0; t < nkt; ++t) {
-        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): the tile has landed, the one before has been read
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        x.advance();
-        w.advance();
-        const bool more = t + 1 < nkt;
-        const u32x4 xb = x.buffer(), wb = w.buffer();
-        const uint32_t next = lds0 + (slot ^ STAGE);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            Ops& in = o[s & 1];
-            const Ops& use = o[(s & 1) ^ 1];
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {  // a row of blocks between the reads and loads
-#pragma unroll
-                for (int j = 0; j < MB; ++j)
-                    if (j * NB / MB == i) in.x[j] = xv.read(slot, s, j);
-                in.w[i] = wv.read(slot, s, i);
-                if (more) {
-#pragma unroll
-                    for (int q = 0; q < PX + PW; ++q)
-                        if (q * 4 * NB / (PX + PW) == s * NB + i) {
-                            if (q < PX)
-                                x.load(xb, q, next);
-                            else
-                                w.load(wb, q - PX, next + BM * KT * 2);
-                        }
-                }
-#pragma unroll
-                for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(use.w[i], use.x[j], acc[i][j]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-        slot ^= STAGE;
-    }
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(o[1].w[i], o[1].x[j], acc[i][j]);
-
     // acc[i][j][e]: W row 32 i + 8 (e / 4) + 4 (lane / 32) + e % 4 of the
     // wavefront, X row 32 j + lane % 32.  The sums go through LDS, 32 X rows
     // of the wavefront at a time, so that a lane then has eight consecutive
     // outputs of a row: loads and stores run along the rows, and a lane's
     // columns are the same in every pass.
     constexpr int LDF = TN + 4;  // floats per row: 16 rows written at one column on distinct banks
-    static_assert(WAVES * 32 * LDF * 4 <= 2 * STAGE, "a slab of every wavefront fits the stages");
+    static_assert(WAVES * 32 * LDF * 4 <= 2 * (BM + BN) * KT * 2, "a slab of every wavefront fits the stages");
     constexpr int TNO = EPI == FF_GATE ? TN / 2 : TN;  // outputs of a wavefront's row
     constexpr int C8 = TNO / 8, RPP = 64 / C8, PASSES = 32 / RPP;
     float* tab = (float*)lds + wave * 32 * LDF;
@@ -299,7 +233,7 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char*
                     if ((lane & 3) == 0) p.scales[(at + p.N) / EIGHT_GROUP] = (uint8_t)scale;
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= ff_act(p.act, g[e]);
+                for (int e = 0; e < 8; ++e) v[e] *= ff_act<ACT>(g[e]);
                 store8(p.out + (int64_t)m * p.N + n, v);
             } else {
                 float a[8], b[8], h[8];
@@ -310,7 +244,7 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char*
                 for (int e = 0; e < 8; ++e) {
                     const float val = kv[e >> 2][e & 3] * fv;
                     float d;
-                    const float y = ff_act(p.act, kg[e >> 2][e & 3] * fg, &d);
+                    const float y = ff_act<ACT>(kg[e >> 2][e & 3] * fg, &d);
                     a[e] = v[e] * y;
                     b[e] = v[e] * val * d;
                     h[e] = val * y;
@@ -341,26 +275,378 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char*
     }
 }
 
-template <int BM, int BN, int WM, bool XT, bool WT, int EPI>
+// The tile `tile` of product p.
+template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
+__device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char* lds) {
+    constexpr int WN = WAVES / WM;
+    constexpr int TM = BM / WM, TN = BN / WN;  // X and W rows of a wavefront
+    constexpr int MB = TM / 32, NB = TN / 32;  // its 32 x 32 blocks
+    constexpr int STAGE = (BM + BN) * KT * 2;
+    constexpr int BNO = EPI == FF_GATE ? BN / 2 : BN;  // outputs of a tile
+    static_assert(EPI != FF_GATE || TN % 64 == 0, "value and gate in one wavefront");
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    int m0, n0;
+    place<BM, BNO>(p, tile, m0, n0);
+
+    Operand<BM, XT> x;
+    Operand<BN, WT> w;
+    x.init(p.x, p.ldx, p.M, m0, p.K, [](int r) { return (int64_t)r; });
+    if constexpr (EPI == FF_GATE)  // of every 64 rows 32 are values, 32 their gates
+        w.init(p.w, p.ldw, 2 * (int64_t)p.N, n0, p.K,
+               [&](int r) { return (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0); });
+    else
+        w.init(p.w, p.ldw, p.N, n0, p.K, [](int r) { return (int64_t)r; });
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
+    const View<BM, XT> xv(lds0, wm * TM);
+    const View<BN, WT> wv(lds0 + BM * KT * 2, wn * TN);
+
+    f32x16 acc[NB][MB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    struct Ops {
+        bf16x8 x[MB], w[NB];
+    };
+    Ops o[2];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) o[1].x[j] = bf16x8{};
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[1].w[i] = bf16x8{};
+
+    constexpr int PX = decltype(x)::PIECES, PW = decltype(w)::PIECES;
+    const int nkt = (p.K + KT - 1) / KT;
+    {
+        const u32x4 xb = x.buffer(), wb = w.buffer();
+#pragma unroll
+        for (int q = 0; q < PX; ++q) x.load(xb, q, lds0);
+#pragma unroll
+        for (int q = 0; q < PW; ++q) w.load(wb, q, lds0 + BM * KT * 2);
+    }
+    // The k-tiles alternate between two stages.  A step's operands are read
+    // behind the products of the step before, a tile's first ones behind the
+    // last of the tile before it (the first tile's are products with zeros);
+    // the next tile's loads are spread over the steps.
+    uint32_t slot = 0;
+    for (int t = 0; t < nkt; ++t) {
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): the tile has landed, the one before has been read
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        x.advance();
+        w.advance();
+        const bool more = t + 1 < nkt;
+        const u32x4 xb = x.buffer(), wb = w.buffer();
+        const uint32_t next = lds0 + (slot ^ STAGE);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            Ops& in = o[s & 1];
+            const Ops& use = o[(s & 1) ^ 1];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {  // a row of blocks between the reads and loads
+#pragma unroll
+                for (int j = 0; j < MB; ++j)
+                    if (j * NB / MB == i) in.x[j] = xv.read(slot, s, j);
+                in.w[i] = wv.read(slot, s, i);
+                if (more) {
+#pragma unroll
+                    for (int q = 0; q < PX + PW; ++q)
+                        if (q * 2 * NB / (PX + PW) == s * NB + i) {
+                            if (q < PX)
+                                x.load(xb, q, next);
+                            else
+                                w.load(wb, q - PX, next + BM * KT * 2);
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(use.w[i], use.x[j], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        slot ^= STAGE;
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(o[1].w[i], o[1].x[j], acc[i][j]);
+
+    store_tile<BM, BN, WM, EPI, ACT>(p, acc, m0, n0, lds);
+}
+
+// One operand of the 256 x 256 tiles: the same layouts in units of 128 rows x
+// KT, half of every wavefront's 128 rows (or columns) in each: unit row r is
+// tile row 128 (r / 64) + r % 64, the second half's 64 rows further on.
+template <bool T>
+struct HalfOperand {
+    static constexpr int PIECES = 4;  // 1 KB loads per wavefront and unit
+    const char* base[2];          // the halves of the k-tile to load next
+    int64_t step;                 // bytes to the next k-tile
+    uint32_t bytes[2], last[2];   // from base to where a load may reach; T: in the last k-tile
+    uint32_t less;                // T = false: what bytes shrinks by per k-tile
+    int32_t tiles;                // k-tiles that are left
+    uint32_t voff[PIECES];
+
+    // row_of as in Operand, half_rows: the rows between a unit and the next.
+    template <typename RowOf>
+    __device__ __forceinline__ void init(const bf16* p, int64_t ld, int64_t rows, int64_t row0, int32_t K, int half_rows,
+                                         int wave, RowOf row_of) {
+        const int lane = threadIdx.x & 63;
+        tiles = (K + KT - 1) / KT;
+        if constexpr (T) {
+            const int64_t half = half_rows * 2;
+            base[0] = (const char*)(p + row0);
+            base[1] = base[0] + half;
+            step = KT * ld * 2;
+            const int64_t end = (K - (int64_t)KT * (tiles - 1)) * ld * 2 - row0 * 2;
+            last[0] = (uint32_t)end;
+            last[1] = (uint32_t)(end > half ? end - half : 0);
+            bytes[0] = tiles == 1 ? last[0] : (uint32_t)(step - row0 * 2);
+            bytes[1] = tiles == 1 ? last[1] : (uint32_t)(step - row0 * 2 - half);
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) {
+                const int k = 4 * (wave + WAVES * q) + (lane >> 4), ch = lane & 15;
+                const int c = 32 * ((ch >> 2) ^ Operand<128, true>::swizzle(k)) + 8 * (ch & 3);
+                voff[q] = (uint32_t)(k * ld * 2) + 2 * (128 * (c >> 6) + (c & 63));
+            }
+        } else {
+            const int64_t left = (rows - row0) * ld * 2, half = half_rows * ld * 2;
+            base[0] = (const char*)(p + row0 * ld);
+            base[1] = base[0] + half;
+            step = KT * 2;
+            bytes[0] = (uint32_t)(left < 0xffffffffll ? left : 0xffffffffll);
+            bytes[1] = (uint32_t)(left - half < 0xffffffffll ? (left > half ? left - half : 0) : 0xffffffffll);
+            less = bytes[1] ? KT * 2 : 0;  // bytes[0] > 0; a row is at least K long
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) {
+                const int r = 8 * (wave + WAVES * q) + (lane >> 3);
+                voff[q] = (uint32_t)(row_of(128 * (r >> 6) + (r & 63)) * ld * 2) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+            }
+        }
+    }
+    __device__ __forceinline__ u32x4 buffer(int h) const { return buffer_of(base[h], bytes[h]); }
+    // The next k-tile; past the last every load gives zeros.
+    __device__ __forceinline__ void advance() {
+        base[0] += step;
+        base[1] += step;
+        --tiles;
+        if constexpr (T) {
+            bytes[0] = tiles > 1 ? bytes[0] : last[0];
+            bytes[1] = tiles > 1 ? bytes[1] : last[1];
+        } else {
+            bytes[0] -= KT * 2;
+            bytes[1] -= less;
+        }
+        if (tiles <= 0) bytes[0] = bytes[1] = last[0] = last[1] = less = 0;
+    }
+};
+
+// A 256 x 256 tile.  Four wavefronts of 128 x 128, one per SIMD: their sums
+// fill the 256 accumulation registers, and LDS delivers 128 KB per k-tile for
+// 2048 cycles of products.  What a loop over whole k-tiles in two stages is
+// bound by is the wait for the next one: 64 KB take as long to arrive at 33
+// bytes a clock as their products take, and the latency comes on top.  So the
+// ring holds eight units of 16 KB, a k-tile being four: the first halves of X
+// and W, the second halves of W and X.  A k-tile's products are four phases, a
+// quarter of the tile each (X1 W1, X1 W2, X2 W2, X2 W1); each phase reads one
+// unit into registers, the one whose products begin two phases on (one, for
+// W2 and X2), and loads the unit six after it into the slot that the phase
+// before the last has read.  Five units are always in flight, and a phase
+// waits only for a load that was issued five phases (about 2500 cycles) before.
+template <bool XT, bool WT, int EPI, int ACT>
+__device__ __forceinline__ void product_tile_256(const FfProduct& p, int tile, char* lds) {
+    constexpr int BNO = EPI == FF_GATE ? 128 : 256;  // outputs of a tile
+    constexpr uint32_t UNIT = 128 * KT * 2;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    int m0, n0;
+    place<256, BNO>(p, tile, m0, n0);
+
+    HalfOperand<XT> x;
+    HalfOperand<WT> w;
+    x.init(p.x, p.ldx, p.M, m0, p.K, 64, wave, [](int r) { return (int64_t)r; });
+    if constexpr (EPI == FF_GATE)  // of every 64 rows 32 are values, 32 their gates
+        w.init(p.w, p.ldw, 2 * (int64_t)p.N, n0, p.K, 32, wave,
+               [&](int r) { return (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0); });
+    else
+        w.init(p.w, p.ldw, p.N, n0, p.K, 64, wave, [](int r) { return (int64_t)r; });
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
+    const View<128, XT> xv(lds0, 64 * wm);
+    const View<128, WT> wv(lds0, 64 * wn);
+    const int nkt = (p.K + KT - 1) / KT;
+
+    f32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    const uint32_t dst = lds0 + wave * 1024;
+    auto load = [&](const u32x4& buf, const uint32_t (&voff)[4], int q, uint32_t slot) {
+        dma16(buf, voff[q], dst + slot * UNIT + q * (WAVES * 1024));
+    };
+    // Unit u (0: X1, 1: W1, 2: W2, 3: X2) of the k-tile that x and w stand at.
+    auto buffer_of_unit = [&](int u) { return u == 0 || u == 3 ? x.buffer(u == 3) : w.buffer(u == 2); };
+    auto step_after = [&](int u) {  // X2 and W2 are the last of their operand's k-tile
+        if (u == 3) x.advance();
+        if (u == 2) w.advance();
+    };
+    auto load_unit = [&](int u, uint32_t slot) {
+        const u32x4 b = buffer_of_unit(u);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (u == 0 || u == 3)
+                load(b, x.voff, q, slot);
+            else
+                load(b, w.voff, q, slot);
+        step_after(u);
+    };
+
+    struct Frag {
+        bf16x8 v[2][4];  // row block, k-step
+    };
+    Frag xa, xb, wa, wb;
+    // The phase that computes acc[ni ..][mj ..] from xr and wr, reads the unit
+    // in slot `from` into `next` and loads unit `u` into slot `to`.
+    auto phase = [&](const Frag& wr, const Frag& xr, int ni, int mj, Frag& next, bool next_x, uint32_t from, int u,
+                     uint32_t to) {
+        // This wavefront's part of the unit to read has landed (20 younger
+        // loads may be in flight), and it has read the unit of two phases ago
+        // (eight younger reads may be in flight); then everyone's.
+        asm volatile("s_waitcnt vmcnt(20) lgkmcnt(8)\n\ts_barrier" ::: "memory");
+        const u32x4 b = buffer_of_unit(u);
+        // A product occupies the matrix unit for 32 cycles: reads after every
+        // second one, loads after every fourth.
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int s = k >> 2, i = (k >> 1) & 1, j = k & 1;
+            acc[ni + i][mj + j] = mfma32x32x16(wr.v[i][s], xr.v[j][s], acc[ni + i][mj + j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (k % 2 == 0) {
+                const int f = k / 2;
+                next.v[f & 1][f >> 1] = next_x ? xv.read(from * UNIT, f >> 1, f & 1) : wv.read(from * UNIT, f >> 1, f & 1);
+            } else if (k % 4 == 1) {
+                if (u == 0 || u == 3)
+                    load(b, x.voff, k / 4, to);
+                else
+                    load(b, w.voff, k / 4, to);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        step_after(u);
+    };
+
+#pragma unroll
+    for (int u = 0; u < 8; ++u) load_unit(u & 3, u);
+    asm volatile("s_waitcnt vmcnt(24)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            xa.v[r][s] = xv.read(0, s, r);
+            wa.v[r][s] = wv.read(UNIT, s, r);
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // Two k-tiles a round, so that every slot is a constant; W1 of the second
+    // is read into W2's registers of the first and the other way round.  (An
+    // odd last k-tile runs with one of zeros: leaving the round in its middle
+    // made the compiler spill.)
+    for (int t = 0; t < nkt; t += 2) {
+        phase(wa, xa, 0, 0, wb, false, 2, 0, 0);
+        phase(wb, xa, 2, 0, xb, true, 3, 1, 1);
+        phase(wb, xb, 2, 2, xa, true, 4, 2, 2);
+        phase(wa, xb, 0, 2, wb, false, 5, 3, 3);
+        phase(wb, xa, 0, 0, wa, false, 6, 0, 4);
+        phase(wa, xa, 2, 0, xb, true, 7, 1, 5);
+        phase(wa, xb, 2, 2, xa, true, 0, 2, 6);
+        phase(wb, xb, 0, 2, wa, false, 1, 3, 7);
+    }
+    // Loads past the end are still on their way (zeros) to the slots.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    store_tile<256, 256, 2, EPI, ACT>(p, acc, m0, n0, lds);
+}
+
+template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
 __global__ __launch_bounds__(THREADS, BM * BN > 128 * 128 ? 1 : 2) void ff_product(FfProduct p) {
     __shared__ __attribute__((aligned(256))) char lds[2 * (BM + BN) * KT * 2];
-    product_tile<BM, BN, WM, XT, WT, EPI>(p, blockIdx.x, lds);
+    const int tile = tile_of(p, blockIdx.x);
+    if (tile < 0) return;
+    if constexpr (BM == 256)
+        product_tile_256<XT, WT, EPI, ACT>(p, tile, lds);
+    else
+        product_tile<BM, BN, WM, XT, WT, EPI, ACT>(p, tile, lds);
+}
+
+// Up to three products of FF_STORE in one launch: first those with both
+// operands across the contraction (the weights' gradients, the longest), then
+// one with W alone across it.  Their tiles together leave fewer compute units
+// idle at the end than three launches do.
+struct FfGroup {
+    FfProduct p[3];
+    int32_t n;
+};
+template <int BM, int BN, int WM>
+__global__ __launch_bounds__(THREADS, BM * BN > 128 * 128 ? 1 : 2) void ff_products(FfGroup g) {
+    __shared__ __attribute__((aligned(256))) char lds[2 * (BM + BN) * KT * 2];
+    const int xcd = blockIdx.x % g.p[0].n_xcd;
+    int j = blockIdx.x / g.p[0].n_xcd, which = 0;
+    while (which < g.n - 1 && j >= g.p[which].per_xcd) j -= g.p[which++].per_xcd;
+    const FfProduct& p = g.p[which];
+    const int tile = xcd * p.per_xcd + j;
+    if (tile >= p.tiles) return;
+    if (p.x_t) {
+        if constexpr (BM == 256)
+            product_tile_256<true, true, FF_STORE, 0>(p, tile, lds);
+        else
+            product_tile<BM, BN, WM, true, true, FF_STORE, 0>(p, tile, lds);
+    } else {
+        if constexpr (BM == 256)
+            product_tile_256<false, true, FF_STORE, 0>(p, tile, lds);
+        else
+            product_tile<BM, BN, WM, false, true, FF_STORE, 0>(p, tile, lds);
+    }
+}
+
+// The tiles of p, dealt over the XCDs.
+void set_tiles(FfProduct& p, int bm, int bno) {
+    const int cus = device_cus();
+    p.tiles = (p.M + bm - 1) / bm * ((p.N + bno - 1) / bno);
+    p.n_xcd = layout_for(cus, cus).n_xcd;
+    p.per_xcd = (p.tiles + p.n_xcd - 1) / p.n_xcd;
 }
 
 template <int BM, int BN, int WM>
-hipError_t launch(const FfProduct& p, hipStream_t s) {
-    const int bno = p.epilogue == FF_GATE ? BN / 2 : BN;
-    const unsigned grid = (unsigned)((int64_t)((p.M + BM - 1) / BM) * ((p.N + bno - 1) / bno));
+hipError_t launch(FfProduct p, hipStream_t s) {
+    set_tiles(p, BM, p.epilogue == FF_GATE ? BN / 2 : BN);
+    const unsigned grid = (unsigned)p.n_xcd * p.per_xcd;
+    const bool silu = p.act == PCPP_ACT_SILU;
+    auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p); };
     if (p.epilogue == FF_GATE)
-        ff_product<BM, BN, WM, false, false, FF_GATE><<<grid, THREADS, 0, s>>>(p);
+        run(silu ? ff_product<BM, BN, WM, false, false, FF_GATE, PCPP_ACT_SILU>
+                 : ff_product<BM, BN, WM, false, false, FF_GATE, PCPP_ACT_GELU>);
     else if (p.epilogue == FF_GATE_GRAD)
-        ff_product<BM, BN, WM, false, true, FF_GATE_GRAD><<<grid, THREADS, 0, s>>>(p);
-    else if (p.x_t)
-        ff_product<BM, BN, WM, true, true, FF_STORE><<<grid, THREADS, 0, s>>>(p);
-    else if (p.w_t)
-        ff_product<BM, BN, WM, false, true, FF_STORE><<<grid, THREADS, 0, s>>>(p);
+        run(silu ? ff_product<BM, BN, WM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
+                 : ff_product<BM, BN, WM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
     else
-        ff_product<BM, BN, WM, false, false, FF_STORE><<<grid, THREADS, 0, s>>>(p);
+        run(ff_product<BM, BN, WM, false, false, FF_STORE, 0>);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int WM>
+hipError_t launch_group(const FfProduct* p, int n, hipStream_t s) {
+    FfGroup g = {};
+    g.n = n;
+    unsigned grid = 0;
+    for (int i = 0; i < n; ++i) {
+        g.p[i] = p[i];
+        set_tiles(g.p[i], BM, BN);
+        grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;
+    }
+    ff_products<BM, BN, WM><<<grid, THREADS, 0, s>>>(g);
     return hipGetLastError();
 }
 
@@ -372,6 +658,10 @@ int ff_partial_rows(int64_t M) { return (int)(big(M) ? (M + 255) / 256 * 2 : (M 
 
 hipError_t launch_ff_product(const FfProduct& p, hipStream_t s) {
     return big(p.M) ? launch<256, 256, 2>(p, s) : launch<128, 128, 2>(p, s);
+}
+
+hipError_t launch_ff_products(const FfProduct* p, int n, hipStream_t s) {
+    return big(p[0].M) ? launch_group<256, 256, 2>(p, n, s) : launch_group<128, 128, 2>(p, n, s);
 }
 
 }  // namespace pcpp
