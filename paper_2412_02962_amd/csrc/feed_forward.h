@@ -30,14 +30,23 @@ struct FfProduct {
     uint8_t* codes;       // [M, 2N] e4m3 of value and gate (FF_GATE: written, or null; FF_GATE_GRAD: read)
     uint8_t* scales;      // [M, 2N / 32]
     bf16* h;              // FF_GATE_GRAD: [M, N] or null
-    float* partial;       // FF_GATE_GRAD: [ff_partial_rows(M)][2N] sums of out over rows, or null
-    int32_t tiles, n_xcd, per_xcd;  // set by the launch
+    float* partial;       // FF_GATE_GRAD: [ff_partial_rows(p)][2N] sums of out over rows, or null
+    // Set by the launch: the pieces that the contraction is worked in, their
+    // float32 sums [pieces][M][N], tiles x pieces, and how they go to the XCDs.
+    int32_t pieces;
+    float* part;
+    int32_t items, n_xcd, per_xcd;
 };
-int ff_partial_rows(int64_t M);
-// A product with X along the contraction (w_t as the epilogue has it: only
-// FF_GATE_GRAD's W lies across it).
-hipError_t launch_ff_product(const FfProduct& p, hipStream_t s);
-// Up to three products of FF_STORE with w_t = 1, those with x_t = 1 first, in one launch.
-hipError_t launch_ff_products(const FfProduct* p, int n, hipStream_t s);
+int ff_partial_rows(const FfProduct& p);  // of a product's sizes and epilogue
+// FF_STORE or FF_GATE on at most FF_SKINNY_ROWS rows of X, both operands along
+// the contraction (ff_skinny.hip); launch_ff_product calls it for these.
+constexpr int FF_SKINNY_ROWS = 32;
+hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s);
+// A product with X along the contraction (W across it for FF_GATE_GRAD alone),
+// and up to three of FF_STORE with w_t = 1, those with x_t = 1 first, in one
+// launch.  part: ff_part_floats of the same products, or of these and others.
+hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s);
+hipError_t launch_ff_products(const FfProduct* p, int n, float* part, hipStream_t s);
+int64_t ff_part_floats(const FfProduct* p, int n);
 
 }  // namespace pcpp

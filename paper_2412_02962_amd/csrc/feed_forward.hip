@@ -43,15 +43,53 @@ struct Layout {
     }
 };
 
+// The products of both passes, without their pointers.
+FfProduct product(const pcpp_ff_geom_t& g, FfEpilogue epilogue, int64_t M, int64_t N, int64_t K, int x_t, int w_t) {
+    FfProduct p = {};
+    p.M = (int32_t)M;
+    p.N = (int32_t)N;
+    p.K = (int32_t)K;
+    p.ldx = x_t ? M : K;
+    p.ldw = w_t ? N : K;
+    p.x_t = x_t;
+    p.w_t = w_t;
+    p.epilogue = epilogue;
+    p.act = g.act;
+    return p;
+}
+FfProduct up_of(const pcpp_ff_geom_t& g) { return product(g, FF_GATE, g.tokens, g.ff_inner, g.channels, 0, 0); }
+FfProduct down_of(const pcpp_ff_geom_t& g) { return product(g, FF_STORE, g.tokens, g.channels, g.ff_inner, 0, 0); }
+FfProduct gate_grad_of(const pcpp_ff_geom_t& g) {
+    return product(g, FF_GATE_GRAD, g.tokens, g.ff_inner, g.channels, 0, 1);
+}
+FfProduct w1_grad_of(const pcpp_ff_geom_t& g) {
+    return product(g, FF_STORE, 2 * (int64_t)g.ff_inner, g.channels, g.tokens, 1, 1);
+}
+FfProduct w2_grad_of(const pcpp_ff_geom_t& g) { return product(g, FF_STORE, g.channels, g.ff_inner, g.tokens, 1, 1); }
+FfProduct x_grad_of(const pcpp_ff_geom_t& g) {
+    return product(g, FF_STORE, g.tokens, g.channels, 2 * (int64_t)g.ff_inner, 0, 1);
+}
+
+struct ForwardLayout : Layout {
+    size_t h, part;
+    explicit ForwardLayout(const pcpp_ff_geom_t& g) {
+        h = add(2 * g.tokens * g.ff_inner);
+        const FfProduct down = down_of(g);
+        part = add(4 * ff_part_floats(&down, 1));
+    }
+};
+
 struct BackwardLayout : Layout {
-    size_t x, dpre, h, sums1, sums2;
+    size_t x, dpre, h, sums1, sums2, part;
     explicit BackwardLayout(const pcpp_ff_geom_t& g) {
         const int64_t M = g.tokens, C = g.channels, F = g.ff_inner;
         x = add(2 * M * C);
         dpre = add(4 * M * F);
         h = add(2 * M * F);
-        sums1 = add((int64_t)ff_partial_rows(M) * 2 * F * 4);
+        sums1 = add((int64_t)ff_partial_rows(gate_grad_of(g)) * 2 * F * 4);
         sums2 = add((int64_t)column_partial_rows(M) * C * 4);
+        const FfProduct p[] = {w1_grad_of(g), w2_grad_of(g), x_grad_of(g)};
+        part = add(4 * ff_part_floats(p, 3));
     }
 };
 
@@ -69,9 +107,7 @@ using namespace pcpp;
 
 PCPP_EXPORT size_t pcpp_gated_ff_workspace_size(const pcpp_ff_geom_t* g) {
     if (check_geom(g) != PCPP_OK) return 0;
-    Layout l;
-    l.add(2 * g->tokens * g->ff_inner);
-    return l.size;
+    return ForwardLayout(*g).size;
 }
 
 PCPP_EXPORT int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w, const void* x, void* y,
@@ -80,37 +116,27 @@ PCPP_EXPORT int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* 
     if (st != PCPP_OK) return st;
     if (!w || !w->ff1_w || !w->ff2_w || !x || !y || (pre_codes == nullptr) != (pre_scales == nullptr)) return PCPP_EINVAL;
     const int64_t M = g->tokens, C = g->channels, F = g->ff_inner;
-    const size_t need = pcpp_gated_ff_workspace_size(g);
-    if (!workspace || ws_bytes < need) return PCPP_EWORKSPACE;
+    const ForwardLayout l(*g);
+    if (!workspace || ws_bytes < l.size) return PCPP_EWORKSPACE;
     const Range in[] = {{x, 2 * M * C}, {w->ff1_w, 4 * F * C}, {w->ff1_b, 4 * F}, {w->ff2_w, 2 * C * F}, {w->ff2_b, 2 * C}};
-    const Range out[] = {{y, 2 * M * C}, {workspace, (int64_t)need}, {pre_codes, 2 * M * F}, {pre_scales, 2 * M * F / EIGHT_GROUP}};
+    const Range out[] = {{y, 2 * M * C}, {workspace, (int64_t)l.size}, {pre_codes, 2 * M * F}, {pre_scales, 2 * M * F / EIGHT_GROUP}};
     if (!all_aligned(in, 5) || !all_aligned(out, 3) || outputs_overlap(out, 4, in, 5)) return PCPP_EINVAL;
     const hipStream_t s = (hipStream_t)stream;
-    FfProduct up = {};
+    bf16* h = (bf16*)((char*)workspace + l.h);
+    FfProduct up = up_of(*g);
     up.x = (const bf16*)x;
     up.w = (const bf16*)w->ff1_w;
-    up.ldx = up.ldw = C;
-    up.M = (int32_t)M;
-    up.N = (int32_t)F;
-    up.K = (int32_t)C;
-    up.epilogue = FF_GATE;
-    up.act = g->act;
-    up.out = (bf16*)workspace;
+    up.out = h;
     up.bias = (const bf16*)w->ff1_b;
     up.codes = (uint8_t*)pre_codes;
     up.scales = (uint8_t*)pre_scales;
-    if (launch_ff_product(up, s) != hipSuccess) return PCPP_EHIP;
-    FfProduct down = {};
-    down.x = (const bf16*)workspace;
+    if (launch_ff_product(up, nullptr, s) != hipSuccess) return PCPP_EHIP;
+    FfProduct down = down_of(*g);
+    down.x = h;
     down.w = (const bf16*)w->ff2_w;
-    down.ldx = down.ldw = F;
-    down.M = (int32_t)M;
-    down.N = (int32_t)C;
-    down.K = (int32_t)F;
-    down.epilogue = FF_STORE;
     down.out = (bf16*)y;
     down.bias = (const bf16*)w->ff2_b;
-    return launch_ff_product(down, s) == hipSuccess ? PCPP_OK : PCPP_EHIP;
+    return launch_ff_product(down, (float*)((char*)workspace + l.part), s) == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }
 
 PCPP_EXPORT size_t pcpp_gated_ff_backward_workspace_size(const pcpp_ff_geom_t* g) {
@@ -140,25 +166,18 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
     bf16 *dpre = (bf16*)(ws + l.dpre), *h = (bf16*)(ws + l.h);
     float *sums1 = (float*)(ws + l.sums1), *sums2 = (float*)(ws + l.sums2);
     if (dx || d.ff1_w || d.ff1_b || d.ff2_w) {
-        FfProduct p = {};
+        FfProduct p = gate_grad_of(*g);
         p.x = (const bf16*)dy;
         p.w = (const bf16*)w->ff2_w;
-        p.ldx = C;
-        p.ldw = F;
-        p.w_t = 1;
-        p.M = (int32_t)M;
-        p.N = (int32_t)F;
-        p.K = (int32_t)C;
-        p.epilogue = FF_GATE_GRAD;
-        p.act = g->act;
         p.out = dx || d.ff1_w ? dpre : nullptr;
         p.codes = (uint8_t*)const_cast<void*>(pre_codes);
         p.scales = (uint8_t*)const_cast<void*>(pre_scales);
         p.h = d.ff2_w ? h : nullptr;
         p.partial = d.ff1_b ? sums1 : nullptr;
-        if (launch_ff_product(p, s) != hipSuccess) return PCPP_EHIP;
+        if (launch_ff_product(p, nullptr, s) != hipSuccess) return PCPP_EHIP;
     }
-    if (d.ff1_b && launch_sum_partials(sums1, ff_partial_rows(M), (int)(2 * F), d.ff1_b, s) != hipSuccess) return PCPP_EHIP;
+    if (d.ff1_b && launch_sum_partials(sums1, ff_partial_rows(gate_grad_of(*g)), (int)(2 * F), d.ff1_b, s) != hipSuccess)
+        return PCPP_EHIP;
     if (d.ff2_b && (launch_column_partials(dy, M, (int)C, sums2, s) != hipSuccess ||
                     launch_sum_partials(sums2, column_partial_rows(M), (int)C, d.ff2_b, s) != hipSuccess))
         return PCPP_EHIP;
@@ -170,41 +189,23 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
             if (launch_checkpoint_load_bf16(x, x_scales, ws + l.x, M * C, s) != hipSuccess) return PCPP_EHIP;
             x16 = ws + l.x;
         }
-        FfProduct& p = group[n++];
+        FfProduct& p = group[n++] = w1_grad_of(*g);
         p.x = dpre;
         p.w = (const bf16*)x16;
-        p.ldx = 2 * F;
-        p.ldw = C;
-        p.x_t = p.w_t = 1;
-        p.M = (int32_t)(2 * F);
-        p.N = (int32_t)C;
-        p.K = (int32_t)M;
         p.out = (bf16*)d.ff1_w;
     }
     if (d.ff2_w) {
-        FfProduct& p = group[n++];
+        FfProduct& p = group[n++] = w2_grad_of(*g);
         p.x = (const bf16*)dy;
         p.w = h;
-        p.ldx = C;
-        p.ldw = F;
-        p.x_t = p.w_t = 1;
-        p.M = (int32_t)C;
-        p.N = (int32_t)F;
-        p.K = (int32_t)M;
         p.out = (bf16*)d.ff2_w;
     }
     if (dx) {
-        FfProduct& p = group[n++];
+        FfProduct& p = group[n++] = x_grad_of(*g);
         p.x = dpre;
         p.w = (const bf16*)w->ff1_w;
-        p.ldx = 2 * F;
-        p.ldw = C;
-        p.w_t = 1;
-        p.M = (int32_t)M;
-        p.N = (int32_t)C;
-        p.K = (int32_t)(2 * F);
         p.out = (bf16*)dx;
     }
-    if (n && launch_ff_products(group, n, s) != hipSuccess) return PCPP_EHIP;
+    if (n && launch_ff_products(group, n, (float*)(ws + l.part), s) != hipSuccess) return PCPP_EHIP;
     return PCPP_OK;
 }

@@ -16,6 +16,13 @@ namespace {
 constexpr int KT = 64;  // contraction per tile
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
+#ifndef TK0
+#define TK0 0.2
+#define TK1 0.5
+#endif
+
+// LDS of a tile of bm x 2 bm: the rings of product_tile_64x128 and product_tile_128x256.
+constexpr int lds_bytes(int bm) { return (bm == 128 ? 80 : 144) * 1024; }
 
 typedef __attribute__((address_space(3))) void* lptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -36,63 +43,76 @@ __device__ __forceinline__ u32x4 buffer_of(const char* p, uint32_t bytes) {
                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
-// One operand: R rows of a tile (R = BM or BN), KT of the contraction, in LDS.
+// Where the k-tiles of an operand's rows are read from: what lies past the
+// last row, the contraction's end or the last of the k-tiles comes as zeros.
+// T: stored across the contraction, [K, rows], else [rows, K].
+template <bool T>
+struct Source {
+    const char* base;      // the k-tile to load next
+    int64_t step;          // bytes to the one after it
+    uint32_t bytes, last;  // from base to where a load may reach; T: in the last k-tile
+    int32_t tiles;         // k-tiles that are left
+
+    // `count` k-tiles from k-tile `first` of rows row0 .. of p [rows, K].
+    __device__ __forceinline__ void init(const bf16* p, int64_t ld, int64_t rows, int64_t row0, int32_t K, int32_t first,
+                                         int32_t count) {
+        tiles = count;
+        if constexpr (T) {
+            step = KT * ld * 2;
+            base = (const char*)(p + row0) + first * step;
+            const int64_t full = step - row0 * 2, end = (K - (int64_t)KT * (first + count - 1)) * ld * 2 - row0 * 2;
+            last = (uint32_t)(end < full ? end : full);
+            bytes = count == 1 ? last : (uint32_t)full;
+        } else {
+            step = KT * 2;
+            base = (const char*)(p + row0 * ld) + first * step;
+            const int64_t left = (rows - row0) * ld * 2 - first * step;
+            bytes = (uint32_t)(left < 0xffffffffll ? left : 0xffffffffll);
+        }
+    }
+    // From `off` bytes further on.
+    __device__ __forceinline__ u32x4 buffer(uint32_t off) const {
+        return buffer_of(base + off, bytes > off ? bytes - off : 0);
+    }
+    __device__ __forceinline__ void advance() {
+        base += step;
+        --tiles;
+        if constexpr (T)
+            bytes = tiles > 1 ? bytes : last;
+        else
+            bytes -= KT * 2;
+        if (tiles <= 0) bytes = 0;
+    }
+};
+
+// R rows of a k-tile in LDS, and what a wavefront loads of them: PIECES loads
+// of 1 KB.
 //
 // Along the contraction (T = false) an LDS row is a row's 128 bytes, 16-byte
 // chunk c of row r at slot c ^ (r / 2 % 8): 16 consecutive rows read at one
 // chunk are conflict-free.  Across it (T = true) an LDS row is one k of all R
-// rows, 64-byte unit u of it at u ^ (k % 4) (two units a row: u ^ (k / 2 %
-// 2)), so that the four k of a transposing read lie on different banks.
+// rows, 64-byte unit u of it at u ^ swizzle(k), so that the four k of a
+// transposing read lie on different banks.
 template <int R, bool T>
-struct Operand {
+struct Layout {
     static constexpr int BYTES = R * KT * 2;
-    static constexpr int PIECES = R / (8 * WAVES);  // 1 KB loads per wavefront and k-tile
-    static constexpr int RB = R / 32;               // 32-row blocks
-    const char* base;
-    int64_t step, left;  // bytes to the next k-tile; bytes from base to the operand's end
-    uint32_t voff[PIECES];
-    uint32_t most;       // bytes that a k-tile may reach from base
-
+    static constexpr int PIECES = R / (8 * WAVES);
     static constexpr __device__ __forceinline__ int swizzle(int k) { return R == 64 ? (k >> 1) & 1 : k & 3; }
 
-    // Rows row0 .. of `rows`; row_of(r) is tile row r's row (T = false: any, T
-    // = true: row0 + r, R of them in a run).
+    // The byte of a k-tile that this lane reads in the wavefront's q-th load;
+    // row_of(r): LDS row r's row, 32 in a run (T: 64 bytes of a k).
     template <typename RowOf>
-    __device__ __forceinline__ void init(const bf16* p, int64_t ld, int64_t rows, int64_t row0, int64_t K, RowOf row_of) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    static __device__ __forceinline__ uint32_t offset(int q, int wave, int64_t ld, RowOf row_of) {
+        const int lane = threadIdx.x & 63;
         if constexpr (T) {
-            base = (const char*)(p + row0);
-            step = KT * ld * 2;
-            left = (K * ld - row0) * 2;
-            most = (uint32_t)step;
-            constexpr int CH = R / 8, PER = 64 / CH;  // chunks of an LDS row, rows of a piece
-#pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int k = PER * (wave + WAVES * q) + lane / CH, ch = lane % CH;
-                voff[q] = (uint32_t)(k * ld * 2) + 16 * ((((ch >> 2) ^ swizzle(k)) << 2) | (ch & 3));
-            }
+            constexpr int CH = R / 8, PER = 64 / CH;  // chunks of an LDS row, rows of a load
+            const int k = PER * (wave + WAVES * q) + lane / CH, ch = lane % CH;
+            const int c = 32 * ((ch >> 2) ^ swizzle(k)) + 8 * (ch & 3);
+            return (uint32_t)(k * ld * 2) + 2 * (uint32_t)row_of(c);
         } else {
-            base = (const char*)(p + row0 * ld);
-            step = KT * 2;
-            left = (rows - row0) * ld * 2;
-            most = 0xffffffffu;
-#pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int r = 8 * (wave + WAVES * q) + (lane >> 3);
-                voff[q] = (uint32_t)(row_of(r) * ld * 2) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
-            }
+            const int r = 8 * (wave + WAVES * q) + (lane >> 3);
+            return (uint32_t)(row_of(r) * ld * 2) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
         }
-    }
-
-    __device__ __forceinline__ u32x4 buffer() const {
-        return buffer_of(base, (uint32_t)(left < (int64_t)most ? left : (int64_t)most));
-    }
-    __device__ __forceinline__ void advance() {
-        base += step;
-        left -= step;
-    }
-    __device__ __forceinline__ void load(u32x4 buf, int q, uint32_t lds) const {
-        dma16(buf, voff[q], lds + ((threadIdx.x >> 6) + WAVES * q) * 1024);
     }
 };
 
@@ -107,7 +127,7 @@ struct View {
             // 16 lanes of a transposing read: 4 k x 16 rows, four rows a lane
             const int g = lane >> 4, i = lane & 15;
             const int k = 8 * (g >> 1) + (i >> 2);
-            at = lds + k * (R * 2) + ((((uint32_t)row0 >> 5) ^ Operand<R, T>::swizzle(k)) << 6) + 32 * (g & 1) + 8 * (i & 3);
+            at = lds + k * (R * 2) + ((((uint32_t)row0 >> 5) ^ Layout<R, T>::swizzle(k)) << 6) + 32 * (g & 1) + 8 * (i & 3);
         } else {
             const int r = row0 + (lane & 31);
             at = lds + r * 128 + (((lane >> 5) ^ ((r >> 1) & 7)) << 4);
@@ -127,31 +147,36 @@ struct View {
     }
 };
 
-// Tile `tile` of the product's rows and outputs: groups of kGroup tiles along
-// the rows, walked along the outputs.  An XCD takes a run of tiles; the 32 that
-// it works on at a time are then about 8 x 4 and share their operands in its L2.
-constexpr int kGroup = 8;
+// An item of a product's work: a tile of its rows and outputs, and a run of
+// its k-tiles.  Workgroups are dealt round-robin over the XCDs; an XCD takes a
+// run of items, and those are ordered as pieces of the contraction, then
+// groups of kGroup tiles along the rows, walked along the outputs: what an XCD
+// works on at a time is about square and shares its operands in the L2.
+constexpr int kGroup = 16;
+struct Item {
+    int m0, n0, piece, first, count;  // rows and outputs from; piece; its k-tiles
+};
 template <int BM, int BNO>
-__device__ __forceinline__ void place(const FfProduct& p, int tile, int& m0, int& n0) {
+__device__ __forceinline__ Item item_of(const FfProduct& p, int item) {
     const int mt = (p.M + BM - 1) / BM, nt = (p.N + BNO - 1) / BNO;
+    Item it;
+    it.piece = item / (mt * nt);
+    const int tile = item - it.piece * mt * nt;
     const int group = tile / (kGroup * nt), in = tile - group * kGroup * nt;
     const int rows = min(kGroup, mt - group * kGroup);
-    n0 = in / rows * BNO;
-    m0 = (group * kGroup + in % rows) * BM;
-}
-
-// The tile of workgroup b: workgroups are dealt round-robin over the XCDs, an
-// XCD's tiles are a run of p.per_xcd (the last may have fewer).
-__device__ __forceinline__ int tile_of(const FfProduct& p, int b) {
-    const int xcd = b % p.n_xcd, j = b / p.n_xcd;
-    const int tile = xcd * p.per_xcd + j;
-    return tile < p.tiles ? tile : -1;
+    it.n0 = in / rows * BNO;
+    it.m0 = (group * kGroup + in % rows) * BM;
+    const int nkt = (p.K + KT - 1) / KT;
+    it.first = (int)((int64_t)nkt * it.piece / p.pieces);
+    it.count = (int)((int64_t)nkt * (it.piece + 1) / p.pieces) - it.first;
+    return it;
 }
 
 // The outputs of a tile from its wavefronts' sums (BM / WM x BN / WN each).
 template <int BM, int BN, int WM, int EPI, int ACT>
-__device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN * WM / (32 * WAVES)][BM / (32 * WM)], int m0,
-                                           int n0, char* lds) {
+__device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
+                                           f32x16 (&acc)[BN * WM / (32 * WAVES)][BM / (32 * WM)], char* lds) {
+    const int m0 = it.m0, n0 = it.n0;
     constexpr int WN = WAVES / WM;
     constexpr int TM = BM / WM, TN = BN / WN;
     constexpr int MB = TM / 32, NB = TN / 32;
@@ -164,7 +189,7 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN 
     // outputs of a row: loads and stores run along the rows, and a lane's
     // columns are the same in every pass.
     constexpr int LDF = TN + 4;  // floats per row: 16 rows written at one column on distinct banks
-    static_assert(WAVES * 32 * LDF * 4 <= 2 * (BM + BN) * KT * 2, "a slab of every wavefront fits the stages");
+    static_assert(WAVES * 32 * LDF * 4 <= lds_bytes(BM), "a slab of every wavefront fits the stages");
     constexpr int TNO = EPI == FF_GATE ? TN / 2 : TN;  // outputs of a wavefront's row
     constexpr int C8 = TNO / 8, RPP = 64 / C8, PASSES = 32 / RPP;
     float* tab = (float*)lds + wave * 32 * LDF;
@@ -176,7 +201,8 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN 
     float b0[8], b1[8], s0[8], s1[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) b0[e] = b1[e] = s0[e] = s1[e] = 0.f;
-    if (EPI != FF_GATE_GRAD && p.bias != nullptr && inside) {
+    const bool whole = EPI != FF_STORE || p.pieces == 1;
+    if (EPI != FF_GATE_GRAD && whole && p.bias != nullptr && inside) {
         load8(p.bias + n, b0);
         if constexpr (EPI == FF_GATE) load8(p.bias + p.N + n, b1);
     }
@@ -213,6 +239,10 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN 
             load8(tab + (r0 + RPP * ps) * LDF + col, v);
             if (m >= p.M || !inside) continue;  // four lanes of a group together
             if constexpr (EPI == FF_STORE) {
+                if (!whole) {
+                    store8(p.part + ((int64_t)it.piece * p.M + m) * p.N + n, v);
+                    continue;
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += b0[e];
                 store8(p.out + (int64_t)m * p.N + n, v);
@@ -275,393 +305,451 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, f32x16 (&acc)[BN 
     }
 }
 
-// The tile `tile` of product p.
-template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
-__device__ __forceinline__ void product_tile(const FfProduct& p, int tile, char* lds) {
-    constexpr int WN = WAVES / WM;
-    constexpr int TM = BM / WM, TN = BN / WN;  // X and W rows of a wavefront
-    constexpr int MB = TM / 32, NB = TN / 32;  // its 32 x 32 blocks
-    constexpr int STAGE = (BM + BN) * KT * 2;
-    constexpr int BNO = EPI == FF_GATE ? BN / 2 : BN;  // outputs of a tile
-    static_assert(EPI != FF_GATE || TN % 64 == 0, "value and gate in one wavefront");
-    const int lane = threadIdx.x & 63;
+// A 64 x 128 tile, for few tiles: four wavefronts of 32 x 64 and a ring of six
+// stages of 24 KB, so that five k-tiles are on their way while one is worked
+// on.  A step's operands are read behind the products of the step before, a
+// k-tile's first ones behind the last of the one before it (the first
+// k-tile's are products with zeros).
+template <bool XT, bool WT, int EPI, int ACT>
+__device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item, char* lds) {
+    constexpr int STAGES = 6, STAGE = (64 + 128) * KT * 2;
+    typedef Layout<64, XT> LX;
+    typedef Layout<128, WT> LW;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % WM, wn = wave / WM;
-    int m0, n0;
-    place<BM, BNO>(p, tile, m0, n0);
+    const int wm = wave & 1, wn = wave >> 1;
+    const Item it = item_of<64, EPI == FF_GATE ? 64 : 128>(p, item);
 
-    Operand<BM, XT> x;
-    Operand<BN, WT> w;
-    x.init(p.x, p.ldx, p.M, m0, p.K, [](int r) { return (int64_t)r; });
-    if constexpr (EPI == FF_GATE)  // of every 64 rows 32 are values, 32 their gates
-        w.init(p.w, p.ldw, 2 * (int64_t)p.N, n0, p.K,
-               [&](int r) { return (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0); });
-    else
-        w.init(p.w, p.ldw, p.N, n0, p.K, [](int r) { return (int64_t)r; });
+    Source<XT> x;
+    Source<WT> w;
+    x.init(p.x, p.ldx, p.M, it.m0, p.K, it.first, it.count);
+    w.init(p.w, p.ldw, EPI == FF_GATE ? 2 * (int64_t)p.N : p.N, it.n0, p.K, it.first, it.count);
+    uint32_t xoff[LX::PIECES], woff[LW::PIECES];
+#pragma unroll
+    for (int q = 0; q < LX::PIECES; ++q) xoff[q] = LX::offset(q, wave, p.ldx, [](int r) { return (int64_t)r; });
+    // FF_GATE: of every 64 rows 32 are values, 32 their gates
+#pragma unroll
+    for (int q = 0; q < LW::PIECES; ++q)
+        woff[q] = LW::offset(q, wave, p.ldw, [&](int r) {
+            return EPI == FF_GATE ? (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0) : (int64_t)r;
+        });
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
-    const View<BM, XT> xv(lds0, wm * TM);
-    const View<BN, WT> wv(lds0 + BM * KT * 2, wn * TN);
+    const View<64, XT> xv(lds0, 32 * wm);
+    const View<128, WT> wv(lds0 + LX::BYTES, 64 * wn);
 
-    f32x16 acc[NB][MB];
+    f32x16 acc[2][1];
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < MB; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        for (int e = 0; e < 16; ++e) acc[i][0][e] = 0.f;
     struct Ops {
-        bf16x8 x[MB], w[NB];
+        bf16x8 x, w[2];
     };
     Ops o[2];
-#pragma unroll
-    for (int j = 0; j < MB; ++j) o[1].x[j] = bf16x8{};
-#pragma unroll
-    for (int i = 0; i < NB; ++i) o[1].w[i] = bf16x8{};
+    o[1].x = o[1].w[0] = o[1].w[1] = bf16x8{};
 
-    constexpr int PX = decltype(x)::PIECES, PW = decltype(w)::PIECES;
-    const int nkt = (p.K + KT - 1) / KT;
-    {
-        const u32x4 xb = x.buffer(), wb = w.buffer();
+    uint32_t rd = 0, wr = 0;
+    auto next_of = [](uint32_t s) { return s + STAGE == STAGES * STAGE ? 0 : s + STAGE; };
+    auto load_x = [&](int q, const u32x4& b) { dma16(b, xoff[q], lds0 + wr + (wave + WAVES * q) * 1024); };
+    auto load_w = [&](int q, const u32x4& b) { dma16(b, woff[q], lds0 + wr + LX::BYTES + (wave + WAVES * q) * 1024); };
 #pragma unroll
-        for (int q = 0; q < PX; ++q) x.load(xb, q, lds0);
+    for (int t = 0; t < STAGES - 1; ++t) {
+        const u32x4 xb = x.buffer(0), wb = w.buffer(0);
 #pragma unroll
-        for (int q = 0; q < PW; ++q) w.load(wb, q, lds0 + BM * KT * 2);
-    }
-    // The k-tiles alternate between two stages.  A step's operands are read
-    // behind the products of the step before, a tile's first ones behind the
-    // last of the tile before it (the first tile's are products with zeros);
-    // the next tile's loads are spread over the steps.
-    uint32_t slot = 0;
-    for (int t = 0; t < nkt; ++t) {
-        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): the tile has landed, the one before has been read
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        for (int q = 0; q < LX::PIECES; ++q) load_x(q, xb);
+#pragma unroll
+        for (int q = 0; q < LW::PIECES; ++q) load_w(q, wb);
         x.advance();
         w.advance();
-        const bool more = t + 1 < nkt;
-        const u32x4 xb = x.buffer(), wb = w.buffer();
-        const uint32_t next = lds0 + (slot ^ STAGE);
+        wr = next_of(wr);
+    }
+    static_assert(LX::PIECES + LW::PIECES == 6, "24 of a wavefront's loads are four k-tiles'");
+    for (int t = 0; t < it.count; ++t) {
+        // The k-tile has landed and the one before has been read, everyone's.
+        asm volatile("s_waitcnt vmcnt(24) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const u32x4 xb = x.buffer(0), wb = w.buffer(0);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             Ops& in = o[s & 1];
             const Ops& use = o[(s & 1) ^ 1];
+            in.x = xv.read(rd, s, 0);
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {  // a row of blocks between the reads and loads
+            for (int i = 0; i < 2; ++i) in.w[i] = wv.read(rd, s, i);
+            if (s < LX::PIECES) load_x(s, xb);
+            load_w(s, wb);
 #pragma unroll
-                for (int j = 0; j < MB; ++j)
-                    if (j * NB / MB == i) in.x[j] = xv.read(slot, s, j);
-                in.w[i] = wv.read(slot, s, i);
-                if (more) {
-#pragma unroll
-                    for (int q = 0; q < PX + PW; ++q)
-                        if (q * 2 * NB / (PX + PW) == s * NB + i) {
-                            if (q < PX)
-                                x.load(xb, q, next);
-                            else
-                                w.load(wb, q - PX, next + BM * KT * 2);
-                        }
-                }
-#pragma unroll
-                for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(use.w[i], use.x[j], acc[i][j]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int i = 0; i < 2; ++i) acc[i][0] = mfma32x32x16(use.w[i], use.x, acc[i][0]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        slot ^= STAGE;
+        x.advance();
+        w.advance();
+        rd = next_of(rd);
+        wr = next_of(wr);
     }
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < MB; ++j) acc[i][j] = mfma32x32x16(o[1].w[i], o[1].x[j], acc[i][j]);
-
-    store_tile<BM, BN, WM, EPI, ACT>(p, acc, m0, n0, lds);
+    for (int i = 0; i < 2; ++i) acc[i][0] = mfma32x32x16(o[1].w[i], o[1].x, acc[i][0]);
+    // Loads past the end are still on their way (zeros) to the stages.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    store_tile<64, 128, 2, EPI, ACT>(p, it, acc, lds);
 }
 
-// One operand of the 256 x 256 tiles: the same layouts in units of 128 rows x
-// KT, half of every wavefront's 128 rows (or columns) in each: unit row r is
-// tile row 128 (r / 64) + r % 64, the second half's 64 rows further on.
-template <bool T>
-struct HalfOperand {
-    static constexpr int PIECES = 4;  // 1 KB loads per wavefront and unit
-    const char* base[2];          // the halves of the k-tile to load next
-    int64_t step;                 // bytes to the next k-tile
-    uint32_t bytes[2], last[2];   // from base to where a load may reach; T: in the last k-tile
-    uint32_t less;                // T = false: what bytes shrinks by per k-tile
-    int32_t tiles;                // k-tiles that are left
-    uint32_t voff[PIECES];
-
-    // row_of as in Operand, half_rows: the rows between a unit and the next.
-    template <typename RowOf>
-    __device__ __forceinline__ void init(const bf16* p, int64_t ld, int64_t rows, int64_t row0, int32_t K, int half_rows,
-                                         int wave, RowOf row_of) {
-        const int lane = threadIdx.x & 63;
-        tiles = (K + KT - 1) / KT;
-        if constexpr (T) {
-            const int64_t half = half_rows * 2;
-            base[0] = (const char*)(p + row0);
-            base[1] = base[0] + half;
-            step = KT * ld * 2;
-            const int64_t end = (K - (int64_t)KT * (tiles - 1)) * ld * 2 - row0 * 2;
-            last[0] = (uint32_t)end;
-            last[1] = (uint32_t)(end > half ? end - half : 0);
-            bytes[0] = tiles == 1 ? last[0] : (uint32_t)(step - row0 * 2);
-            bytes[1] = tiles == 1 ? last[1] : (uint32_t)(step - row0 * 2 - half);
-#pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int k = 4 * (wave + WAVES * q) + (lane >> 4), ch = lane & 15;
-                const int c = 32 * ((ch >> 2) ^ Operand<128, true>::swizzle(k)) + 8 * (ch & 3);
-                voff[q] = (uint32_t)(k * ld * 2) + 2 * (128 * (c >> 6) + (c & 63));
-            }
-        } else {
-            const int64_t left = (rows - row0) * ld * 2, half = half_rows * ld * 2;
-            base[0] = (const char*)(p + row0 * ld);
-            base[1] = base[0] + half;
-            step = KT * 2;
-            bytes[0] = (uint32_t)(left < 0xffffffffll ? left : 0xffffffffll);
-            bytes[1] = (uint32_t)(left - half < 0xffffffffll ? (left > half ? left - half : 0) : 0xffffffffll);
-            less = bytes[1] ? KT * 2 : 0;  // bytes[0] > 0; a row is at least K long
-#pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int r = 8 * (wave + WAVES * q) + (lane >> 3);
-                voff[q] = (uint32_t)(row_of(128 * (r >> 6) + (r & 63)) * ld * 2) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
-            }
-        }
-    }
-    __device__ __forceinline__ u32x4 buffer(int h) const { return buffer_of(base[h], bytes[h]); }
-    // The next k-tile; past the last every load gives zeros.
-    __device__ __forceinline__ void advance() {
-        base[0] += step;
-        base[1] += step;
-        --tiles;
-        if constexpr (T) {
-            bytes[0] = tiles > 1 ? bytes[0] : last[0];
-            bytes[1] = tiles > 1 ? bytes[1] : last[1];
-        } else {
-            bytes[0] -= KT * 2;
-            bytes[1] -= less;
-        }
-        if (tiles <= 0) bytes[0] = bytes[1] = last[0] = last[1] = less = 0;
-    }
-};
-
-// A 256 x 256 tile.  Four wavefronts of 128 x 128, one per SIMD: their sums
-// fill the 256 accumulation registers, and LDS delivers 128 KB per k-tile for
-// 2048 cycles of products.  What a loop over whole k-tiles in two stages is
-// bound by is the wait for the next one: 64 KB take as long to arrive at 33
-// bytes a clock as their products take, and the latency comes on top.  So the
-// ring holds eight units of 16 KB, a k-tile being four: the first halves of X
-// and W, the second halves of W and X.  A k-tile's products are four phases, a
-// quarter of the tile each (X1 W1, X1 W2, X2 W2, X2 W1); each phase reads one
-// unit into registers, the one whose products begin two phases on (one, for
-// W2 and X2), and loads the unit six after it into the slot that the phase
-// before the last has read.  Five units are always in flight, and a phase
-// waits only for a load that was issued five phases (about 2500 cycles) before.
+// A 128 x 256 tile, two workgroups to a compute unit: while one waits at a
+// barrier or for LDS, or is in its epilogue (an exponential, a reciprocal and
+// some 20 operations an output, and up to 8 bytes of memory traffic), the
+// other's products run.  Four wavefronts of 64 x 128, two per SIMD.
+//
+// A loop over whole k-tiles in two stages waits for the next one: its bytes
+// take as long to arrive as its products take, and the latency comes on top.
+// So the ring holds ten units of 8 KB, a k-tile being six in the order W0 X0
+// X1 W1 W2 W3, and a phase is the products of one of the four W units with
+// both of X.  Phase 3 reads the next k-tile's W0 and X0 into registers, phase
+// 0 X1 (used by its second half) and W1, the others one W unit each; a phase
+// loads into the slots that the phase before the last has read.  Five units of
+// a workgroup are always in flight.
 template <bool XT, bool WT, int EPI, int ACT>
-__device__ __forceinline__ void product_tile_256(const FfProduct& p, int tile, char* lds) {
+__device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int item, char* lds) {
     constexpr int BNO = EPI == FF_GATE ? 128 : 256;  // outputs of a tile
-    constexpr uint32_t UNIT = 128 * KT * 2;
+    constexpr uint32_t UNIT = 64 * KT * 2, RING = 10 * UNIT;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
-    int m0, n0;
-    place<256, BNO>(p, tile, m0, n0);
+    const Item it = item_of<128, BNO>(p, item);
 
-    HalfOperand<XT> x;
-    HalfOperand<WT> w;
-    x.init(p.x, p.ldx, p.M, m0, p.K, 64, wave, [](int r) { return (int64_t)r; });
-    if constexpr (EPI == FF_GATE)  // of every 64 rows 32 are values, 32 their gates
-        w.init(p.w, p.ldw, 2 * (int64_t)p.N, n0, p.K, 32, wave,
-               [&](int r) { return (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0); });
-    else
-        w.init(p.w, p.ldw, p.N, n0, p.K, 64, wave, [](int r) { return (int64_t)r; });
+    // Unit i has 32 rows of each of the wavefronts' two runs of rows: tile rows
+    // run (r / 32) + 32 i + r % 32; FF_GATE's W: 32 outputs' values for even i,
+    // their gates for odd.
+    typedef Layout<64, XT> LX;
+    typedef Layout<64, WT> LW;
+    Source<XT> x;
+    Source<WT> w;
+    x.init(p.x, p.ldx, p.M, it.m0, p.K, it.first, it.count);
+    w.init(p.w, p.ldw, EPI == FF_GATE ? 2 * (int64_t)p.N : p.N, it.n0, p.K, it.first, it.count);
+    uint32_t xoff[2], woff[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        xoff[q] = LX::offset(q, wave, p.ldx, [](int r) { return (int64_t)(64 * (r >> 5) + (r & 31)); });
+        woff[q] = LW::offset(q, wave, p.ldw,
+                             [](int r) { return (int64_t)((EPI == FF_GATE ? 64 : 128) * (r >> 5) + (r & 31)); });
+    }
+    const uint32_t x_off = XT ? 64 : (uint32_t)(64 * p.ldx);
+    uint32_t w_off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w_off[i] = EPI == FF_GATE ? (uint32_t)((32 * (i >> 1) + (i & 1 ? (int64_t)p.N : 0)) * p.ldw * 2)
+                   : WT           ? 64 * i
+                                  : (uint32_t)(64 * i * p.ldw);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
-    const View<128, XT> xv(lds0, 64 * wm);
-    const View<128, WT> wv(lds0, 64 * wn);
-    const int nkt = (p.K + KT - 1) / KT;
+    const View<64, XT> xv(lds0, 32 * wm);
+    const View<64, WT> wv(lds0, 32 * wn);
 
-    f32x16 acc[4][4];
+    f32x16 acc[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    const uint32_t dst = lds0 + wave * 1024;
-    auto load = [&](const u32x4& buf, const uint32_t (&voff)[4], int q, uint32_t slot) {
-        dma16(buf, voff[q], dst + slot * UNIT + q * (WAVES * 1024));
-    };
-    // Unit u (0: X1, 1: W1, 2: W2, 3: X2) of the k-tile that x and w stand at.
-    auto buffer_of_unit = [&](int u) { return u == 0 || u == 3 ? x.buffer(u == 3) : w.buffer(u == 2); };
-    auto step_after = [&](int u) {  // X2 and W2 are the last of their operand's k-tile
-        if (u == 3) x.advance();
-        if (u == 2) w.advance();
-    };
-    auto load_unit = [&](int u, uint32_t slot) {
-        const u32x4 b = buffer_of_unit(u);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (u == 0 || u == 3)
-                load(b, x.voff, q, slot);
-            else
-                load(b, w.voff, q, slot);
-        step_after(u);
-    };
-
     struct Frag {
-        bf16x8 v[2][4];  // row block, k-step
+        bf16x8 v[4];  // k-steps
     };
-    Frag xa, xb, wa, wb;
-    // The phase that computes acc[ni ..][mj ..] from xr and wr, reads the unit
-    // in slot `from` into `next` and loads unit `u` into slot `to`.
-    auto phase = [&](const Frag& wr, const Frag& xr, int ni, int mj, Frag& next, bool next_x, uint32_t from, int u,
-                     uint32_t to) {
-        // This wavefront's part of the unit to read has landed (20 younger
-        // loads may be in flight), and it has read the unit of two phases ago
-        // (eight younger reads may be in flight); then everyone's.
-        asm volatile("s_waitcnt vmcnt(20) lgkmcnt(8)\n\ts_barrier" ::: "memory");
-        const u32x4 b = buffer_of_unit(u);
-        // A product occupies the matrix unit for 32 cycles: reads after every
-        // second one, loads after every fourth.
+    uint32_t rd = 0, wr = 0;  // slots to read and to load next
+    auto load = [&](int u, int q, const u32x4& b) {
+        dma16(b, u == 1 || u == 2 ? xoff[q] : woff[q], lds0 + wave * 1024 + wr + q * (WAVES * 1024));
+    };
+    // Unit u in the order of a k-tile.
+    auto buffer_of_unit = [&](int u) {
+        return u == 1 ? x.buffer(0) : u == 2 ? x.buffer(x_off) : w.buffer(w_off[u == 0 ? 0 : u - 2]);
+    };
+    auto loaded = [&](int u) {
+        if (u == 2) x.advance();
+        if (u == 5) w.advance();
+        wr = wr + UNIT == RING ? 0 : wr + UNIT;
+    };
+    auto step_read = [&]() { rd = rd + UNIT == RING ? 0 : rd + UNIT; };
+
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const int s = k >> 2, i = (k >> 1) & 1, j = k & 1;
-            acc[ni + i][mj + j] = mfma32x32x16(wr.v[i][s], xr.v[j][s], acc[ni + i][mj + j]);
+    for (int u = 0; u < 9; ++u) {
+        const u32x4 b = buffer_of_unit(u % 6);
+        load(u % 6, 0, b);
+        load(u % 6, 1, b);
+        loaded(u % 6);
+    }
+    Frag wa, wb, xa, xb, xc;
+    asm volatile("s_waitcnt vmcnt(14)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < 4; ++s) wa.v[s] = wv.read(rd, s, 0);
+    step_read();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) xa.v[s] = xv.read(rd, s, 0);
+    step_read();
+
+    // Phase i: products of wc with x0 and x1; the reads and loads listed above.
+    auto phase = [&](int i, const Frag& wc, Frag& wnext, const Frag& x0, Frag& x1, Frag& x0next) {
+        if (i == 0)
+            asm volatile("s_waitcnt vmcnt(10) lgkmcnt(8)\n\ts_barrier" ::: "memory");
+        else if (i == 1)
+            asm volatile("s_waitcnt vmcnt(10) lgkmcnt(8)\n\ts_barrier" ::: "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(12) lgkmcnt(4)\n\ts_barrier" ::: "memory");
+        // the units to load: W1 | W2 W3 | W0 X0 of the tile after the next | X1
+        const int u0 = i == 0 ? 3 : i == 1 ? 4 : i == 2 ? 0 : 2, nu = i == 1 || i == 2 ? 2 : 1;
+        u32x4 b = buffer_of_unit(u0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            // phase 0 begins with x0 alone: x1 is on its way
+            const int j = i == 0 ? k >> 2 : k & 1, s = i == 0 ? k & 3 : k >> 1;
+            acc[i][j] = mfma32x32x16(wc.v[s], j ? x1.v[s] : x0.v[s], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
-            if (k % 2 == 0) {
-                const int f = k / 2;
-                next.v[f & 1][f >> 1] = next_x ? xv.read(from * UNIT, f >> 1, f & 1) : wv.read(from * UNIT, f >> 1, f & 1);
-            } else if (k % 4 == 1) {
-                if (u == 0 || u == 3)
-                    load(b, x.voff, k / 4, to);
-                else
-                    load(b, w.voff, k / 4, to);
+            if (i == 0) {
+                if (k < 2) {
+                    x1.v[2 * k] = xv.read(rd, 2 * k, 0);
+                    x1.v[2 * k + 1] = xv.read(rd, 2 * k + 1, 0);
+                    if (k == 1) step_read();
+                } else if (k < 6) {
+                    wnext.v[k - 2] = wv.read(rd, k - 2, 0);
+                    if (k == 5) step_read();
+                }
+            } else if (k < 4) {
+                wnext.v[k] = wv.read(rd, k, 0);
+                if (k == 3) step_read();
+            } else if (i == 3) {
+                x0next.v[k - 4] = xv.read(rd, k - 4, 0);
+                if (k == 7) step_read();
+            }
+            if (k % 2 == 1 && (nu == 2 || k > 4)) {
+                const int c = nu == 2 ? k >> 1 : (k - 5) >> 1;  // 0 .. 2 nu - 1
+                if (c == 2) b = buffer_of_unit(u0 + 1);
+                load(u0 + (c >> 1), c & 1, b);
+                if (c & 1) loaded(u0 + (c >> 1));
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        step_after(u);
     };
-
-#pragma unroll
-    for (int u = 0; u < 8; ++u) load_unit(u & 3, u);
-    asm volatile("s_waitcnt vmcnt(24)\n\ts_barrier" ::: "memory");
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            xa.v[r][s] = xv.read(0, s, r);
-            wa.v[r][s] = wv.read(UNIT, s, r);
-        }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    // Two k-tiles a round, so that every slot is a constant; W1 of the second
-    // is read into W2's registers of the first and the other way round.  (An
-    // odd last k-tile runs with one of zeros: leaving the round in its middle
-    // made the compiler spill.)
-    for (int t = 0; t < nkt; t += 2) {
-        phase(wa, xa, 0, 0, wb, false, 2, 0, 0);
-        phase(wb, xa, 2, 0, xb, true, 3, 1, 1);
-        phase(wb, xb, 2, 2, xa, true, 4, 2, 2);
-        phase(wa, xb, 0, 2, wb, false, 5, 3, 3);
-        phase(wb, xa, 0, 0, wa, false, 6, 0, 4);
-        phase(wa, xa, 2, 0, xb, true, 7, 1, 5);
-        phase(wa, xb, 2, 2, xa, true, 0, 2, 6);
-        phase(wb, xb, 0, 2, wa, false, 1, 3, 7);
+    for (int t = 0; t < it.count; t += 2) {  // an odd last k-tile runs with one of zeros
+        phase(0, wa, wb, xa, xb, xc);
+        phase(1, wb, wa, xa, xb, xc);
+        phase(2, wa, wb, xa, xb, xc);
+        phase(3, wb, wa, xa, xb, xc);
+        phase(0, wa, wb, xc, xb, xa);
+        phase(1, wb, wa, xc, xb, xa);
+        phase(2, wa, wb, xc, xb, xa);
+        phase(3, wb, wa, xc, xb, xa);
     }
     // Loads past the end are still on their way (zeros) to the slots.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<256, 256, 2, EPI, ACT>(p, acc, m0, n0, lds);
+    store_tile<128, 256, 2, EPI, ACT>(p, it, acc, lds);
 }
 
-template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
-__global__ __launch_bounds__(THREADS, BM * BN > 128 * 128 ? 1 : 2) void ff_product(FfProduct p) {
-    __shared__ __attribute__((aligned(256))) char lds[2 * (BM + BN) * KT * 2];
-    const int tile = tile_of(p, blockIdx.x);
-    if (tile < 0) return;
-    if constexpr (BM == 256)
-        product_tile_256<XT, WT, EPI, ACT>(p, tile, lds);
+template <int BM, bool XT, bool WT, int EPI, int ACT>
+__device__ __forceinline__ void product_tile(const FfProduct& p, int item, char* lds) {
+    if constexpr (BM == 128)
+        product_tile_128x256<XT, WT, EPI, ACT>(p, item, lds);
     else
-        product_tile<BM, BN, WM, XT, WT, EPI, ACT>(p, tile, lds);
+        product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
 }
 
-// Up to three products of FF_STORE in one launch: first those with both
-// operands across the contraction (the weights' gradients, the longest), then
-// one with W alone across it.  Their tiles together leave fewer compute units
-// idle at the end than three launches do.
+template <int BM, bool XT, bool WT, int EPI, int ACT>
+__global__ __launch_bounds__(THREADS, BM == 128 ? 2 : 1) void ff_product(FfProduct p) {
+    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
+    const int item = (int)(blockIdx.x % p.n_xcd) * p.per_xcd + (int)(blockIdx.x / p.n_xcd);
+    if (item < p.items) product_tile<BM, XT, WT, EPI, ACT>(p, item, lds);
+}
+
+// Up to three products of FF_STORE with W across the contraction in one
+// launch, X across it first (the weights' gradients), then X along it: their
+// items together leave fewer compute units idle at the end than three launches
+// do.
 struct FfGroup {
     FfProduct p[3];
     int32_t n;
 };
-template <int BM, int BN, int WM>
-__global__ __launch_bounds__(THREADS, BM * BN > 128 * 128 ? 1 : 2) void ff_products(FfGroup g) {
-    __shared__ __attribute__((aligned(256))) char lds[2 * (BM + BN) * KT * 2];
-    const int xcd = blockIdx.x % g.p[0].n_xcd;
-    int j = blockIdx.x / g.p[0].n_xcd, which = 0;
+template <int BM>
+__global__ __launch_bounds__(THREADS, BM == 128 ? 2 : 1) void ff_products(FfGroup g) {
+    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
+    const int n_xcd = g.p[0].n_xcd;
+    int j = blockIdx.x / n_xcd, which = 0;
     while (which < g.n - 1 && j >= g.p[which].per_xcd) j -= g.p[which++].per_xcd;
     const FfProduct& p = g.p[which];
-    const int tile = xcd * p.per_xcd + j;
-    if (tile >= p.tiles) return;
-    if (p.x_t) {
-        if constexpr (BM == 256)
-            product_tile_256<true, true, FF_STORE, 0>(p, tile, lds);
-        else
-            product_tile<BM, BN, WM, true, true, FF_STORE, 0>(p, tile, lds);
-    } else {
-        if constexpr (BM == 256)
-            product_tile_256<false, true, FF_STORE, 0>(p, tile, lds);
-        else
-            product_tile<BM, BN, WM, false, true, FF_STORE, 0>(p, tile, lds);
+    const int item = (int)(blockIdx.x % n_xcd) * p.per_xcd + j;
+    if (item >= p.items) return;
+    if (p.x_t)
+        product_tile<BM, true, true, FF_STORE, 0>(p, item, lds);
+    else
+        product_tile<BM, false, true, FF_STORE, 0>(p, item, lds);
+}
+
+// out = the pieces' sums, in their order, + bias: eight outputs a thread.
+struct FfSums {
+    const float* part[3];
+    const bf16* bias[3];
+    bf16* out[3];
+    int64_t n[3];          // outputs of a product, 0: none
+    int32_t N[3], pieces[3];
+};
+__global__ __launch_bounds__(256) void ff_sum_pieces(FfSums a) {
+    const int s = blockIdx.y;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= a.n[s]) return;
+    float v[8], t[8];
+    load8(a.part[s] + i, v);
+    for (int k = 1; k < a.pieces[s]; ++k) {
+        load8(a.part[s] + k * a.n[s] + i, t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += t[e];
+    }
+    if (a.bias[s] != nullptr) {
+        load8(a.bias[s] + i % a.N[s], t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += t[e];
+    }
+    store8(a.out[s] + i, v);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int64_t tiles_of(const FfProduct& p, int bm) {
+    return ceil_div(p.M, bm) * ceil_div(p.N, (p.epilogue == FF_GATE ? 1 : 2) * bm);
+}
+
+// Most pieces of a contraction, and most floats of all pieces' sums of a launch.
+constexpr int kMaxPieces = 32;
+constexpr int64_t kMaxPartFloats = 16 << 20;
+
+// Time in us of n products on tiles of bm x 2 bm, their contractions in runs
+// of at most `run` k-tiles.
+constexpr double kTileUs[2] = {TK0, TK1}, kItemUs[2] = {3.0, 4.0};
+double estimate(const FfProduct* p, int n, int bm, int64_t run, int cus, int64_t& floats) {
+    const int kind = bm == 128;
+    double work = 0, longest = 0;
+    int64_t items = 0;
+    floats = 0;
+    for (int i = 0; i < n; ++i) {
+        const int64_t nkt = ceil_div(p[i].K, KT), pieces = ceil_div(nkt, run), t = tiles_of(p[i], bm) * pieces;
+        const double len = (double)nkt / pieces * kTileUs[kind] + kItemUs[kind];
+        items += t;
+        work += t * len;
+        if (len > longest) longest = len;
+        if (pieces > 1) floats += pieces * p[i].M * p[i].N;
+    }
+    const double spread = work / cus + (items > cus ? longest / 2 : 0);
+    return (spread > longest ? spread : longest) + (floats > 0 ? 4.0 + 8.0 * floats / 4.5e6 : 0);
+}
+
+// The tile and the pieces of the products that are estimated fastest.
+int plan(FfProduct* p, int n) {
+    const int device = device_cus(), cus = device > 0 ? device : 256;
+    int64_t longest = 0;
+    for (int i = 0; i < n; ++i) longest = longest > ceil_div(p[i].K, KT) ? longest : ceil_div(p[i].K, KT);
+    int best_bm = 128;
+    int64_t best_run = longest;
+    double best = 1e30;
+    constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, kMaxPieces};
+    for (int bm = 64; bm <= 128; bm *= 2)
+        for (int cut : kCuts) {
+            if (cut > 1 && p[0].epilogue != FF_STORE) break;
+            const int64_t run = ceil_div(longest, cut);
+            int64_t floats = 0;
+            const double t = estimate(p, n, bm, run, cus, floats);
+            if (floats > kMaxPartFloats || t >= best) continue;
+            best = t;
+            best_bm = bm;
+            best_run = run;
+        }
+    const int n_xcd = layout_for(cus, cus).n_xcd;
+    for (int i = 0; i < n; ++i) {
+        p[i].pieces = (int32_t)ceil_div(ceil_div(p[i].K, KT), best_run);
+        p[i].items = (int32_t)(tiles_of(p[i], best_bm) * p[i].pieces);
+        p[i].n_xcd = n_xcd;
+        p[i].per_xcd = (p[i].items + n_xcd - 1) / n_xcd;
+    }
+    return best_bm;
+}
+
+// Places the sums of pieces in `part`.
+void place_parts(FfProduct* p, int n, float* part) {
+    for (int i = 0; i < n; ++i) {
+        p[i].part = part;
+        if (p[i].pieces > 1) part += (int64_t)p[i].pieces * p[i].M * p[i].N;
     }
 }
 
-// The tiles of p, dealt over the XCDs.
-void set_tiles(FfProduct& p, int bm, int bno) {
-    const int cus = device_cus();
-    p.tiles = (p.M + bm - 1) / bm * ((p.N + bno - 1) / bno);
-    p.n_xcd = layout_for(cus, cus).n_xcd;
-    p.per_xcd = (p.tiles + p.n_xcd - 1) / p.n_xcd;
+hipError_t sum_pieces(const FfProduct* p, int n, hipStream_t s) {
+    FfSums a = {};
+    int k = 0;
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        if (p[i].pieces == 1) continue;
+        a.part[k] = p[i].part;
+        a.bias[k] = p[i].bias;
+        a.out[k] = p[i].out;
+        a.n[k] = (int64_t)p[i].M * p[i].N;
+        a.N[k] = p[i].N;
+        a.pieces[k] = p[i].pieces;
+        most = most > a.n[k] ? most : a.n[k];
+        ++k;
+    }
+    if (k == 0) return hipSuccess;
+    ff_sum_pieces<<<dim3((unsigned)ceil_div(most, 2048), k), 256, 0, s>>>(a);
+    return hipGetLastError();
 }
 
-template <int BM, int BN, int WM>
-hipError_t launch(FfProduct p, hipStream_t s) {
-    set_tiles(p, BM, p.epilogue == FF_GATE ? BN / 2 : BN);
+template <int BM>
+void launch(const FfProduct& p, hipStream_t s) {
     const unsigned grid = (unsigned)p.n_xcd * p.per_xcd;
     const bool silu = p.act == PCPP_ACT_SILU;
     auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p); };
     if (p.epilogue == FF_GATE)
-        run(silu ? ff_product<BM, BN, WM, false, false, FF_GATE, PCPP_ACT_SILU>
-                 : ff_product<BM, BN, WM, false, false, FF_GATE, PCPP_ACT_GELU>);
+        run(silu ? ff_product<BM, false, false, FF_GATE, PCPP_ACT_SILU> : ff_product<BM, false, false, FF_GATE, PCPP_ACT_GELU>);
     else if (p.epilogue == FF_GATE_GRAD)
-        run(silu ? ff_product<BM, BN, WM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
-                 : ff_product<BM, BN, WM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
+        run(silu ? ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
+                 : ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
     else
-        run(ff_product<BM, BN, WM, false, false, FF_STORE, 0>);
-    return hipGetLastError();
+        run(ff_product<BM, false, false, FF_STORE, 0>);
 }
 
-template <int BM, int BN, int WM>
-hipError_t launch_group(const FfProduct* p, int n, hipStream_t s) {
-    FfGroup g = {};
-    g.n = n;
-    unsigned grid = 0;
-    for (int i = 0; i < n; ++i) {
-        g.p[i] = p[i];
-        set_tiles(g.p[i], BM, BN);
-        grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;
-    }
-    ff_products<BM, BN, WM><<<grid, THREADS, 0, s>>>(g);
-    return hipGetLastError();
-}
-
-bool big(int64_t M) { return M > 512; }
+bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && p.epilogue != FF_GATE_GRAD && !p.x_t && !p.w_t; }
 
 }  // namespace
 
-int ff_partial_rows(int64_t M) { return (int)(big(M) ? (M + 255) / 256 * 2 : (M + 127) / 128 * 2); }
-
-hipError_t launch_ff_product(const FfProduct& p, hipStream_t s) {
-    return big(p.M) ? launch<256, 256, 2>(p, s) : launch<128, 128, 2>(p, s);
+int ff_partial_rows(const FfProduct& p) {
+    FfProduct q = p;
+    return (int)(2 * ceil_div(p.M, plan(&q, 1)));
 }
 
-hipError_t launch_ff_products(const FfProduct* p, int n, hipStream_t s) {
-    return big(p[0].M) ? launch_group<256, 256, 2>(p, n, s) : launch_group<128, 128, 2>(p, n, s);
+int64_t ff_part_floats(const FfProduct* p, int n) {
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const int64_t nkt = ceil_div(p[i].K, KT);
+        if (!skinny(p[i])) most += (nkt < kMaxPieces ? nkt : kMaxPieces) * p[i].M * p[i].N;
+    }
+    return most < kMaxPartFloats ? most : kMaxPartFloats;
+}
+
+hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
+    if (skinny(p)) return launch_ff_skinny(p, s);
+    const int bm = plan(&p, 1);
+    place_parts(&p, 1, part);
+    if (bm == 128)
+        launch<128>(p, s);
+    else
+        launch<64>(p, s);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : sum_pieces(&p, 1, s);
+}
+
+hipError_t launch_ff_products(const FfProduct* p, int n, float* part, hipStream_t s) {
+    FfGroup g = {};
+    g.n = n;
+    for (int i = 0; i < n; ++i) g.p[i] = p[i];
+    const int bm = plan(g.p, n);
+    place_parts(g.p, n, part);
+    unsigned grid = 0;
+    for (int i = 0; i < n; ++i) grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;
+    if (bm == 128)
+        ff_products<128><<<grid, THREADS, 0, s>>>(g);
+    else
+        ff_products<64><<<grid, THREADS, 0, s>>>(g);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : sum_pieces(g.p, n, s);
 }
 
 }  // namespace pcpp

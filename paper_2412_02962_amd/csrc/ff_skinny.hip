@@ -1,0 +1,149 @@
+// The gated feed-forward's products on few tokens (see feed_forward.h): at
+// most 128 rows of X, both operands along the contraction.
+//
+// What bounds them is the weights' way from memory, each read once (1 token,
+// 1280 x 5120: 39 MB), and the latency of a load, of which a loop over tiles
+// in LDS pays one per tile.  So a workgroup takes few rows of W (32 outputs'
+// values and gates, or 16 outputs) and its eight wavefronts an eighth of the
+// contraction each; W goes straight from memory into the MFMA's operand
+// registers, a run of k-steps in flight at a time, as does X, which the L2
+// holds.  The wavefronts' sums meet in LDS.
+
+#include "eight_bit.h"
+#include "feed_forward.h"
+#include "ff_act.h"
+
+namespace pcpp {
+
+namespace {
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// MT blocks of 16 tokens; FF_GATE: 32 outputs, W rows n0 .. + 31 and N further
+// on; FF_STORE: 16 outputs.
+template <int MT, int EPI, int ACT>
+__global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
+    constexpr int NB = EPI == FF_GATE ? 4 : 1;             // blocks of 16 W rows
+    constexpr int BNO = EPI == FF_GATE ? 32 : 16;
+    constexpr int U = NB + MT <= 5 ? 8 : NB + MT <= 8 ? 4 : 2;  // k-steps in flight
+    __shared__ f32x4 sums[kWaves][NB][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lr = lane & 15, lq = lane >> 4;
+    const int n0 = blockIdx.x * BNO;
+
+    const bf16* w[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        w[i] = p.w + (int64_t)(n0 + 16 * (i & 1) + (i >= 2 ? p.N : 0) + lr) * p.ldw + 8 * lq;
+    const bf16* x[MT];
+    bool there[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        there[j] = 16 * j + lr < p.M;
+        x[j] = p.x + (int64_t)(there[j] ? 16 * j + lr : 0) * p.ldx + 8 * lq;
+    }
+    f32x4 acc[NB][MT];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const int steps = p.K / 32;  // K % 64 == 0
+    const int s1 = steps * (wave + 1) / kWaves;
+    for (int s = steps * wave / kWaves; s < s1; s += U) {
+        bf16x8 wv[U][NB], xv[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = s + u < s1;  // past the end: zeros
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                wv[u][i] = bf16x8{};
+                if (in) wv[u][i] = *(const bf16x8*)(w[i] + 32 * (s + u));
+            }
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                xv[u][j] = bf16x8{};
+                if (in && there[j]) xv[u][j] = *(const bf16x8*)(x[j] + 32 * (s + u));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) acc[i][j] = mfma16(wv[u][i], xv[u][j], acc[i][j]);
+    }
+
+    // acc[i][j][e]: W row 16 i + 4 lq + e, token 16 j + lr
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        if (j > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NB; ++i) sums[wave][i][lane] = acc[i][j];
+        __syncthreads();
+        const int n = threadIdx.x % BNO, r = threadIdx.x / BNO;  // output, token of the block
+        const int m = 16 * j + r;
+        auto total = [&](int i, int row) {  // of row `row` of block i, the wavefronts in their order
+            float t = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) t += sums[k][i][16 * (row >> 2) + r][row & 3];
+            return t;
+        };
+        if (r >= 16 || m >= p.M) continue;  // a group's 32 lanes together
+        if constexpr (EPI == FF_GATE) {
+            float v = total(n >> 4, n & 15), g = total(2 + (n >> 4), n & 15);
+            if (p.bias != nullptr) {
+                v += bf16_to_f32(p.bias[n0 + n]);
+                g += bf16_to_f32(p.bias[p.N + n0 + n]);
+            }
+            if (p.codes != nullptr) {
+                const int64_t at = (int64_t)m * 2 * p.N + n0 + n;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float a = h ? g : v;
+                    float top = finite_abs(a);
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+                    const int scale = eight_scale(top);
+                    p.codes[at + h * p.N] = (uint8_t)to_e4m3(eight_scaled(a, eight_inverse(scale)), 0.f, 0.f, 0.f);
+                    if (n == 0) p.scales[(at + h * p.N) / EIGHT_GROUP] = (uint8_t)scale;
+                }
+            }
+            p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v * ff_act<ACT>(g));
+        } else {
+            float v = total(0, n);
+            if (p.bias != nullptr) v += bf16_to_f32(p.bias[n0 + n]);
+            p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v);
+        }
+    }
+}
+
+template <int MT>
+void launch(const FfProduct& p, hipStream_t s) {
+    if (p.epilogue == FF_STORE)
+        ff_skinny<MT, FF_STORE, 0><<<p.N / 16, kThreads, 0, s>>>(p);
+    else if (p.act == PCPP_ACT_SILU)
+        ff_skinny<MT, FF_GATE, PCPP_ACT_SILU><<<p.N / 32, kThreads, 0, s>>>(p);
+    else
+        ff_skinny<MT, FF_GATE, PCPP_ACT_GELU><<<p.N / 32, kThreads, 0, s>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s) {
+    if (p.M <= 16)
+        launch<1>(p, s);
+    else if (p.M <= 32)
+        launch<2>(p, s);
+    else if (p.M <= 64)
+        launch<4>(p, s);
+    else
+        launch<8>(p, s);
+    return hipGetLastError();
+}
+
+}  // namespace pcpp
