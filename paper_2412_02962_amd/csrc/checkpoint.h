@@ -6,7 +6,18 @@
 
 namespace pcpp {
 
-// n values (whole groups of 32) of codes and scales as bf16, exactly.
-hipError_t launch_checkpoint_load_bf16(const void* codes, const void* scales, void* y, int64_t n, hipStream_t s);
+// What the feed-forward's backward pass needs before its products, in one
+// launch; either part may be missing (n = 0, partial = null).
+struct FfPrepare {
+    const uint8_t* codes;   // n values (whole groups of 32) of x in 8 bits ...
+    const uint8_t* scales;
+    void* x;                // ... as bf16, exactly
+    int64_t n;
+    const void* dy;         // [rows, C] bf16, C % 64 == 0
+    int64_t rows;
+    int32_t C;
+    float* partial;         // [column_partial_rows(rows)][C]: sums of dy over runs of rows
+};
+hipError_t launch_ff_prepare(const FfPrepare& p, hipStream_t s);
 
 }  // namespace pcpp

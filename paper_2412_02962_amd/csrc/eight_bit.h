@@ -54,16 +54,41 @@ __device__ __forceinline__ f32x4 from_e4m3(uint32_t w) {
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
+// The largest magnitude of eight values; NaN among them may be passed over or
+// come through.
+__device__ __forceinline__ float max_abs8(const float (&v)[8]) {
+    float a, b;
+    asm("v_max_f32 %0, |%1|, |%2|" : "=v"(a) : "v"(v[0]), "v"(v[1]));
+    asm("v_max_f32 %0, |%1|, |%2|" : "=v"(b) : "v"(v[2]), "v"(v[3]));
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(a) : "v"(a), "v"(v[4]), "v"(v[5]));
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(b) : "v"(b), "v"(v[6]), "v"(v[7]));
+    asm("v_max_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+    return a;
+}
+
+// The largest of the four neighbouring lanes' (4k .. 4k + 3), by quad
+// permutations (lanes 1 0 3 2, then 2 3 0 1).
+__device__ __forceinline__ float max_of_quad(float top) {
+    top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0xB1, 0xF, 0xF, true)));
+    return fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xF, 0xF, true)));
+}
+
 // Eight consecutive channels of a lane, its group being four neighbouring
-// lanes (4k .. 4k + 3): the codes, and the scale byte that all four share.
+// lanes (all of them here together): the codes, and the scale byte that all
+// four share.  A group whose largest magnitude is finite has no infinities, and
+// what NaN it has become NaN codes by themselves.
 __device__ __forceinline__ u32x2 to_eight_bits(const float (&v)[8], int& scale) {
-    float top = 0.f;
+    float top = max_of_quad(max_abs8(v));
+    if (is_finite(top)) {
+        scale = eight_scale(top);
+        const float inv = eight_inverse(scale);
+        return u32x2{to_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                     to_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+    }
+    top = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(v[i]));
-    // the other three lanes' by quad permutations (lanes 1 0 3 2, then 2 3 0 1)
-    top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0xB1, 0xF, 0xF, true)));
-    top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xF, 0xF, true)));
-    scale = eight_scale(top);
+    scale = eight_scale(max_of_quad(top));
     const float inv = eight_inverse(scale);
     float t[8];
 #pragma unroll

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "column_sums.h"
 #include "common.h"
 
 namespace pcpp {
@@ -44,9 +45,9 @@ constexpr int FF_SKINNY_ROWS = 32;
 hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s);
 // A product with X along the contraction (W across it for FF_GATE_GRAD alone),
 // and up to three of FF_STORE with w_t = 1, those with x_t = 1 first, in one
-// launch.  part: ff_part_floats of the same products, or of these and others.
+// launch (which also does `sums`).  part: ff_part_floats of the same products, or of these and others.
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s);
-hipError_t launch_ff_products(const FfProduct* p, int n, float* part, hipStream_t s);
+hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const PartialSums& sums, hipStream_t s);
 int64_t ff_part_floats(const FfProduct* p, int n);
 
 }  // namespace pcpp

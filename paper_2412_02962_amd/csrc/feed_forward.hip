@@ -165,6 +165,22 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
     char* ws = (char*)workspace;
     bf16 *dpre = (bf16*)(ws + l.dpre), *h = (bf16*)(ws + l.h);
     float *sums1 = (float*)(ws + l.sums1), *sums2 = (float*)(ws + l.sums2);
+    FfPrepare pre = {};
+    const bf16* x16 = (const bf16*)x;
+    if (d.ff1_w && x_scales) {
+        x16 = (const bf16*)(ws + l.x);
+        pre.codes = (const uint8_t*)x;
+        pre.scales = (const uint8_t*)x_scales;
+        pre.x = ws + l.x;
+        pre.n = M * C;
+    }
+    if (d.ff2_b) {
+        pre.dy = dy;
+        pre.rows = M;
+        pre.C = (int32_t)C;
+        pre.partial = sums2;
+    }
+    if (launch_ff_prepare(pre, s) != hipSuccess) return PCPP_EHIP;
     if (dx || d.ff1_w || d.ff1_b || d.ff2_w) {
         FfProduct p = gate_grad_of(*g);
         p.x = (const bf16*)dy;
@@ -176,22 +192,25 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         p.partial = d.ff1_b ? sums1 : nullptr;
         if (launch_ff_product(p, nullptr, s) != hipSuccess) return PCPP_EHIP;
     }
-    if (d.ff1_b && launch_sum_partials(sums1, ff_partial_rows(gate_grad_of(*g)), (int)(2 * F), d.ff1_b, s) != hipSuccess)
-        return PCPP_EHIP;
-    if (d.ff2_b && (launch_column_partials(dy, M, (int)C, sums2, s) != hipSuccess ||
-                    launch_sum_partials(sums2, column_partial_rows(M), (int)C, d.ff2_b, s) != hipSuccess))
-        return PCPP_EHIP;
+    PartialSums sums = {};
+    if (d.ff1_b) {
+        sums.partial[0] = sums1;
+        sums.out[0] = (bf16*)d.ff1_b;
+        sums.n[0] = ff_partial_rows(gate_grad_of(*g));
+        sums.C[0] = (int32_t)(2 * F);
+    }
+    if (d.ff2_b) {
+        sums.partial[1] = sums2;
+        sums.out[1] = (bf16*)d.ff2_b;
+        sums.n[1] = column_partial_rows(M);
+        sums.C[1] = (int32_t)C;
+    }
     FfProduct group[3] = {};
     int n = 0;
     if (d.ff1_w) {
-        const void* x16 = x;
-        if (x_scales) {
-            if (launch_checkpoint_load_bf16(x, x_scales, ws + l.x, M * C, s) != hipSuccess) return PCPP_EHIP;
-            x16 = ws + l.x;
-        }
         FfProduct& p = group[n++] = w1_grad_of(*g);
         p.x = dpre;
-        p.w = (const bf16*)x16;
+        p.w = x16;
         p.out = (bf16*)d.ff1_w;
     }
     if (d.ff2_w) {
@@ -206,6 +225,5 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         p.w = (const bf16*)w->ff1_w;
         p.out = (bf16*)dx;
     }
-    if (n && launch_ff_products(group, n, (float*)(ws + l.part), s) != hipSuccess) return PCPP_EHIP;
-    return PCPP_OK;
+    return launch_ff_products(group, n, (float*)(ws + l.part), sums, s) == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }

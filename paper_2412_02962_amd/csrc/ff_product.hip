@@ -3,6 +3,7 @@
 // MFMAs, with the activation, its derivative and the 8-bit checkpoint in the
 // epilogue.
 
+#include "column_sums.h"
 #include "eight_bit.h"
 #include "feed_forward.h"
 #include "ff_act.h"
@@ -17,12 +18,16 @@ constexpr int KT = 64;  // contraction per tile
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
 #ifndef TK0
-#define TK0 0.2
-#define TK1 0.5
+#define TK0 0.45
+#define TK1 0.75
+#define TK2 1.25
 #endif
 
-// LDS of a tile of bm x 2 bm: the rings of product_tile_64x128 and product_tile_128x256.
-constexpr int lds_bytes(int bm) { return (bm == 128 ? 80 : 144) * 1024; }
+// A tile's rows of X (64, 128 or 256) say which it is; its rows of W, its ring
+// in LDS and how many of its workgroups share a compute unit.
+constexpr int rows_w(int bm) { return bm == 64 ? 128 : 256; }
+constexpr int lds_bytes(int bm) { return (bm == 64 ? 144 : bm == 128 ? 80 : 128) * 1024; }
+constexpr int per_cu(int bm) { return bm == 128 ? 2 : 1; }
 
 typedef __attribute__((address_space(3))) void* lptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -100,15 +105,14 @@ struct Layout {
     static constexpr __device__ __forceinline__ int swizzle(int k) { return R == 64 ? (k >> 1) & 1 : k & 3; }
 
     // The byte of a k-tile that this lane reads in the wavefront's q-th load;
-    // row_of(r): LDS row r's row, 32 in a run (T: 64 bytes of a k).
+    // row_of(r): LDS row r's row (T: r, whole 128-byte lines of a k).
     template <typename RowOf>
     static __device__ __forceinline__ uint32_t offset(int q, int wave, int64_t ld, RowOf row_of) {
         const int lane = threadIdx.x & 63;
         if constexpr (T) {
             constexpr int CH = R / 8, PER = 64 / CH;  // chunks of an LDS row, rows of a load
             const int k = PER * (wave + WAVES * q) + lane / CH, ch = lane % CH;
-            const int c = 32 * ((ch >> 2) ^ swizzle(k)) + 8 * (ch & 3);
-            return (uint32_t)(k * ld * 2) + 2 * (uint32_t)row_of(c);
+            return (uint32_t)(k * ld * 2) + 64 * ((ch >> 2) ^ swizzle(k)) + 16 * (ch & 3);
         } else {
             const int r = 8 * (wave + WAVES * q) + (lane >> 3);
             return (uint32_t)(row_of(r) * ld * 2) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
@@ -116,8 +120,18 @@ struct Layout {
     }
 };
 
-// A lane's view of an operand in LDS: row block b, k-step s (16 of KT).  The
-// MFMA takes row lane % 32 and contraction 8 (lane / 32) .. + 7 of the step.
+// The 32 rows of a tile that are block b of the w-th of its wavefronts along
+// them: a run of its own rows, or, where the operand lies across the
+// contraction, 32 of every 64 (so that 64 neighbouring rows, a 128-byte line of
+// a k, are read together).
+template <bool T>
+constexpr __device__ __forceinline__ int block_row(int b, int w, int run) {
+    return T ? 64 * b + 32 * w : run * w + 32 * b;
+}
+
+// A lane's view of an operand in LDS: the wavefront's row block b, k-step s (16
+// of KT).  The MFMA takes row lane % 32 and contraction 8 (lane / 32) .. + 7 of
+// the step.
 template <int R, bool T>
 struct View {
     uint32_t at;
@@ -135,7 +149,7 @@ struct View {
     }
     __device__ __forceinline__ bf16x8 read(uint32_t slot, int s, int b) const {
         if constexpr (T) {
-            const uint32_t a = (at ^ (b << 6)) + slot + s * (16 * R * 2);
+            const uint32_t a = (at ^ (b << 7)) + slot + s * (16 * R * 2);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_lds)(uintptr_t)a);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_lds)(uintptr_t)(a + 4 * R * 2));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -152,7 +166,10 @@ struct View {
 // run of items, and those are ordered as pieces of the contraction, then
 // groups of kGroup tiles along the rows, walked along the outputs: what an XCD
 // works on at a time is about square and shares its operands in the L2.
-constexpr int kGroup = 16;
+#ifndef KG
+#define KG 8
+#endif
+constexpr int kGroup = KG;
 struct Item {
     int m0, n0, piece, first, count;  // rows and outputs from; piece; its k-tiles
 };
@@ -173,7 +190,7 @@ __device__ __forceinline__ Item item_of(const FfProduct& p, int item) {
 }
 
 // The outputs of a tile from its wavefronts' sums (BM / WM x BN / WN each).
-template <int BM, int BN, int WM, int EPI, int ACT>
+template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
                                            f32x16 (&acc)[BN * WM / (32 * WAVES)][BM / (32 * WM)], char* lds) {
     const int m0 = it.m0, n0 = it.n0;
@@ -194,7 +211,7 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
     constexpr int C8 = TNO / 8, RPP = 64 / C8, PASSES = 32 / RPP;
     float* tab = (float*)lds + wave * 32 * LDF;
     const int c = 8 * (lane % C8), r0 = lane / C8;
-    const int n = n0 + wn * TNO + c;
+    const int n = n0 + (EPI == FF_GATE ? wn * TNO + c : block_row<WT>(c >> 5, wn, TN) + (c & 31));
     const bool inside = n < p.N;
     // FF_GATE: the column of output c's value in the slab; its gate lies 32 on
     const int col = EPI == FF_GATE ? 64 * (c >> 5) + (c & 31) : c;
@@ -208,8 +225,8 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
     }
     __syncthreads();  // the stages have been read
 #pragma unroll
-    for (int j = 0; j < MB; ++j) {
-        const int mj = m0 + wm * TM + 32 * j + r0;
+    for (int j = 0; j < TM / 32; ++j) {
+        const int mj = m0 + block_row<XT>(j, wm, TM) + r0;
         u32x2 cv[PASSES], cg[PASSES];
         int sv[PASSES], sg[PASSES];
         if constexpr (EPI == FF_GATE_GRAD) {
@@ -334,7 +351,7 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
         });
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
     const View<64, XT> xv(lds0, 32 * wm);
-    const View<128, WT> wv(lds0 + LX::BYTES, 64 * wn);
+    const View<128, WT> wv(lds0 + LX::BYTES, block_row<WT>(0, wn, 64));
 
     f32x16 acc[2][1];
 #pragma unroll
@@ -389,7 +406,7 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     for (int i = 0; i < 2; ++i) acc[i][0] = mfma32x32x16(o[1].w[i], o[1].x, acc[i][0]);
     // Loads past the end are still on their way (zeros) to the stages.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<64, 128, 2, EPI, ACT>(p, it, acc, lds);
+    store_tile<64, 128, 2, XT, WT, EPI, ACT>(p, it, acc, lds);
 }
 
 // A 128 x 256 tile, two workgroups to a compute unit: while one waits at a
@@ -413,9 +430,8 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     const int wm = wave & 1, wn = wave >> 1;
     const Item it = item_of<128, BNO>(p, item);
 
-    // Unit i has 32 rows of each of the wavefronts' two runs of rows: tile rows
-    // run (r / 32) + 32 i + r % 32; FF_GATE's W: 32 outputs' values for even i,
-    // their gates for odd.
+    // Unit i has block i of both wavefronts along the rows; FF_GATE's W: 32
+    // outputs' values for even i, their gates for odd.
     typedef Layout<64, XT> LX;
     typedef Layout<64, WT> LW;
     Source<XT> x;
@@ -425,16 +441,18 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     uint32_t xoff[2], woff[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        xoff[q] = LX::offset(q, wave, p.ldx, [](int r) { return (int64_t)(64 * (r >> 5) + (r & 31)); });
-        woff[q] = LW::offset(q, wave, p.ldw,
-                             [](int r) { return (int64_t)((EPI == FF_GATE ? 64 : 128) * (r >> 5) + (r & 31)); });
+        xoff[q] = LX::offset(q, wave, p.ldx,
+                             [](int r) { return (int64_t)(block_row<XT>(0, r >> 5, 64) + (r & 31)); });
+        woff[q] = LW::offset(q, wave, p.ldw, [](int r) {
+            return (int64_t)(block_row<WT>(0, r >> 5, EPI == FF_GATE ? 64 : 128) + (r & 31));
+        });
     }
-    const uint32_t x_off = XT ? 64 : (uint32_t)(64 * p.ldx);
+    const uint32_t x_off = XT ? 128 : (uint32_t)(64 * p.ldx);
     uint32_t w_off[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         w_off[i] = EPI == FF_GATE ? (uint32_t)((32 * (i >> 1) + (i & 1 ? (int64_t)p.N : 0)) * p.ldw * 2)
-                   : WT           ? 64 * i
+                   : WT           ? 128 * i
                                   : (uint32_t)(64 * i * p.ldw);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
     const View<64, XT> xv(lds0, 32 * wm);
@@ -524,6 +542,14 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // The two workgroups of a compute unit get different priorities here, so
+    // that they do not stay in step, both in their products, then both in
+    // their epilogues (the up product of 32768 x 1280 x 5120: 5 % fewer cycles).
+    // By the wavefront's slot on its SIMD, the low bit of the hardware's id.
+    if (__builtin_amdgcn_s_getreg(4 | (3 << 11)) & 1)
+        __builtin_amdgcn_s_setprio(3);
+    else
+        __builtin_amdgcn_s_setprio(1);
     for (int t = 0; t < it.count; t += 2) {  // an odd last k-tile runs with one of zeros
         phase(0, wa, wb, xa, xb, xc);
         phase(1, wb, wa, xa, xb, xc);
@@ -534,21 +560,144 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
         phase(2, wa, wb, xc, xb, xa);
         phase(3, wb, wa, xc, xb, xa);
     }
+    __builtin_amdgcn_s_setprio(0);
     // Loads past the end are still on their way (zeros) to the slots.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<128, 256, 2, EPI, ACT>(p, it, acc, lds);
+    store_tile<128, 256, 2, XT, WT, EPI, ACT>(p, it, acc, lds);
+}
+
+// A 256 x 256 tile, for the products without an epilogue where there are tiles
+// enough: half the bytes a product of the 128 x 256 tiles, one workgroup to a
+// compute unit.  Four wavefronts of 128 x 128, one per SIMD, whose sums fill
+// the 256 accumulation registers.  The ring holds eight units of 16 KB, a k-tile
+// being four: the first halves of X and W, the second halves of W and X.  A
+// k-tile's products are four phases, a quarter of the tile each (X1 W1, X1 W2,
+// X2 W2, X2 W1); each phase reads one unit into registers, the one whose
+// products begin two phases on (one, for W2 and X2), and loads the unit six
+// after it into the slot that the phase before the last has read.  A phase
+// waits only for a load that was issued five phases (about 2500 cycles) before.
+template <bool XT, bool WT>
+__device__ __forceinline__ void product_tile_256x256(const FfProduct& p, int item, char* lds) {
+    constexpr uint32_t UNIT = 128 * KT * 2;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const Item it = item_of<256, 256>(p, item);
+
+    // Unit h has blocks 2 h and 2 h + 1 of both wavefronts along the rows.
+    typedef Layout<128, XT> LX;
+    typedef Layout<128, WT> LW;
+    Source<XT> x;
+    Source<WT> w;
+    x.init(p.x, p.ldx, p.M, it.m0, p.K, it.first, it.count);
+    w.init(p.w, p.ldw, p.N, it.n0, p.K, it.first, it.count);
+    uint32_t xoff[4], woff[4];
+    auto row_of = [](int r) { return (int64_t)(128 * (r >> 6) + (r & 63)); };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        xoff[q] = LX::offset(q, wave, p.ldx, row_of);
+        woff[q] = LW::offset(q, wave, p.ldw, row_of);
+    }
+    const uint32_t x_half = XT ? 256 : (uint32_t)(128 * p.ldx), w_half = WT ? 256 : (uint32_t)(128 * p.ldw);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)lds);
+    const View<128, XT> xv(lds0, block_row<XT>(0, wm, 64));
+    const View<128, WT> wv(lds0, block_row<WT>(0, wn, 64));
+
+    f32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    // Unit u (0: X1, 1: W1, 2: W2, 3: X2) of the k-tile that x and w stand at.
+    auto buffer_of_unit = [&](int u) {
+        return u == 0 || u == 3 ? x.buffer(u == 3 ? x_half : 0) : w.buffer(u == 2 ? w_half : 0);
+    };
+    auto load = [&](int u, int q, const u32x4& b, uint32_t slot) {
+        dma16(b, u == 0 || u == 3 ? xoff[q] : woff[q], lds0 + slot * UNIT + (wave + WAVES * q) * 1024);
+    };
+    auto loaded = [&](int u) {  // X2 and W2 are the last of their operand's k-tile
+        if (u == 3) x.advance();
+        if (u == 2) w.advance();
+    };
+    struct Frag {
+        bf16x8 v[2][4];  // row block, k-step
+    };
+    Frag xa, xb, wa, wb;
+    // The phase that computes acc[ni ..][mj ..] from xr and wr, reads the unit
+    // in slot `from` into `next` and loads unit `u` into slot `to`.
+    auto phase = [&](const Frag& wr, const Frag& xr, int ni, int mj, Frag& next, bool next_x, uint32_t from, int u,
+                     uint32_t to) {
+        // This wavefront's part of the unit to read has landed (20 younger
+        // loads may be in flight), and it has read the unit of two phases ago
+        // (eight younger reads may be in flight); then everyone's.
+        asm volatile("s_waitcnt vmcnt(20) lgkmcnt(8)\n\ts_barrier" ::: "memory");
+        const u32x4 b = buffer_of_unit(u);
+        // A product occupies the matrix unit for 32 cycles: reads after every
+        // second one, loads after every fourth.
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int s = k >> 2, i = (k >> 1) & 1, j = k & 1;
+            acc[ni + i][mj + j] = mfma32x32x16(wr.v[i][s], xr.v[j][s], acc[ni + i][mj + j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (k % 2 == 0) {
+                const int f = k / 2;
+                next.v[f & 1][f >> 1] = next_x ? xv.read(from * UNIT, f >> 1, f & 1) : wv.read(from * UNIT, f >> 1, f & 1);
+            } else if (k % 4 == 1) {
+                load(u, k / 4, b, to);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        loaded(u);
+    };
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const u32x4 b = buffer_of_unit(u & 3);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load(u & 3, q, b, u);
+        loaded(u & 3);
+    }
+    asm volatile("s_waitcnt vmcnt(24)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            xa.v[r][s] = xv.read(0, s, r);
+            wa.v[r][s] = wv.read(UNIT, s, r);
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // Two k-tiles a round, so that every slot is a constant; W1 of the second
+    // is read into W2's registers of the first and the other way round.  (An
+    // odd last k-tile runs with one of zeros: leaving the round in its middle
+    // made the compiler spill.)
+    for (int t = 0; t < it.count; t += 2) {
+        phase(wa, xa, 0, 0, wb, false, 2, 0, 0);
+        phase(wb, xa, 2, 0, xb, true, 3, 1, 1);
+        phase(wb, xb, 2, 2, xa, true, 4, 2, 2);
+        phase(wa, xb, 0, 2, wb, false, 5, 3, 3);
+        phase(wb, xa, 0, 0, wa, false, 6, 0, 4);
+        phase(wa, xa, 2, 0, xb, true, 7, 1, 5);
+        phase(wa, xb, 2, 2, xa, true, 0, 2, 6);
+        phase(wb, xb, 0, 2, wa, false, 1, 3, 7);
+    }
+    // Loads past the end are still on their way (zeros) to the slots.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    store_tile<256, 256, 2, XT, WT, FF_STORE, 0>(p, it, acc, lds);
 }
 
 template <int BM, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile(const FfProduct& p, int item, char* lds) {
-    if constexpr (BM == 128)
+    if constexpr (BM == 256)
+        product_tile_256x256<XT, WT>(p, item, lds);
+    else if constexpr (BM == 128)
         product_tile_128x256<XT, WT, EPI, ACT>(p, item, lds);
     else
         product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
 }
 
 template <int BM, bool XT, bool WT, int EPI, int ACT>
-__global__ __launch_bounds__(THREADS, BM == 128 ? 2 : 1) void ff_product(FfProduct p) {
+__global__ __launch_bounds__(THREADS, per_cu(BM)) void ff_product(FfProduct p) {
     __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
     const int item = (int)(blockIdx.x % p.n_xcd) * p.per_xcd + (int)(blockIdx.x / p.n_xcd);
     if (item < p.items) product_tile<BM, XT, WT, EPI, ACT>(p, item, lds);
@@ -557,14 +706,20 @@ __global__ __launch_bounds__(THREADS, BM == 128 ? 2 : 1) void ff_product(FfProdu
 // Up to three products of FF_STORE with W across the contraction in one
 // launch, X across it first (the weights' gradients), then X along it: their
 // items together leave fewer compute units idle at the end than three launches
-// do.
+// do.  The sums of the biases' gradients ride along.
 struct FfGroup {
     FfProduct p[3];
     int32_t n;
+    int32_t product_blocks;  // workgroups of the products; those after them do the sums
+    PartialSums sums;
 };
 template <int BM>
-__global__ __launch_bounds__(THREADS, BM == 128 ? 2 : 1) void ff_products(FfGroup g) {
+__global__ __launch_bounds__(THREADS, per_cu(BM)) void ff_products(FfGroup g) {
     __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
+    if ((int)blockIdx.x >= g.product_blocks) {
+        sum_partials(g.sums, blockIdx.x - g.product_blocks, (float*)lds);
+        return;
+    }
     const int n_xcd = g.p[0].n_xcd;
     int j = blockIdx.x / n_xcd, which = 0;
     while (which < g.n - 1 && j >= g.p[which].per_xcd) j -= g.p[which++].per_xcd;
@@ -607,7 +762,7 @@ __global__ __launch_bounds__(256) void ff_sum_pieces(FfSums a) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int64_t tiles_of(const FfProduct& p, int bm) {
-    return ceil_div(p.M, bm) * ceil_div(p.N, (p.epilogue == FF_GATE ? 1 : 2) * bm);
+    return ceil_div(p.M, bm) * ceil_div(p.N, p.epilogue == FF_GATE ? rows_w(bm) / 2 : rows_w(bm));
 }
 
 // Most pieces of a contraction, and most floats of all pieces' sums of a launch.
@@ -616,9 +771,9 @@ constexpr int64_t kMaxPartFloats = 16 << 20;
 
 // Time in us of n products on tiles of bm x 2 bm, their contractions in runs
 // of at most `run` k-tiles.
-constexpr double kTileUs[2] = {TK0, TK1}, kItemUs[2] = {3.0, 4.0};
+constexpr double kTileUs[3] = {TK0, TK1, TK2}, kItemUs[3] = {3.0, 4.0, 5.0};
 double estimate(const FfProduct* p, int n, int bm, int64_t run, int cus, int64_t& floats) {
-    const int kind = bm == 128;
+    const int kind = bm / 128;
     double work = 0, longest = 0;
     int64_t items = 0;
     floats = 0;
@@ -643,7 +798,7 @@ int plan(FfProduct* p, int n) {
     int64_t best_run = longest;
     double best = 1e30;
     constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, kMaxPieces};
-    for (int bm = 64; bm <= 128; bm *= 2)
+    for (int bm = 64; bm <= (p[0].epilogue == FF_STORE ? 256 : 128); bm *= 2)
         for (int cut : kCuts) {
             if (cut > 1 && p[0].epilogue != FF_STORE) break;
             const int64_t run = ceil_div(longest, cut);
@@ -695,15 +850,18 @@ hipError_t sum_pieces(const FfProduct* p, int n, hipStream_t s) {
 template <int BM>
 void launch(const FfProduct& p, hipStream_t s) {
     const unsigned grid = (unsigned)p.n_xcd * p.per_xcd;
-    const bool silu = p.act == PCPP_ACT_SILU;
     auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p); };
-    if (p.epilogue == FF_GATE)
-        run(silu ? ff_product<BM, false, false, FF_GATE, PCPP_ACT_SILU> : ff_product<BM, false, false, FF_GATE, PCPP_ACT_GELU>);
-    else if (p.epilogue == FF_GATE_GRAD)
-        run(silu ? ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
-                 : ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
-    else
+    if (p.epilogue == FF_STORE) {
         run(ff_product<BM, false, false, FF_STORE, 0>);
+    } else if constexpr (BM < 256) {
+        const bool silu = p.act == PCPP_ACT_SILU;
+        if (p.epilogue == FF_GATE)
+            run(silu ? ff_product<BM, false, false, FF_GATE, PCPP_ACT_SILU>
+                     : ff_product<BM, false, false, FF_GATE, PCPP_ACT_GELU>);
+        else
+            run(silu ? ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
+                     : ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
+    }
 }
 
 bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && p.epilogue != FF_GATE_GRAD && !p.x_t && !p.w_t; }
@@ -728,7 +886,9 @@ hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
     if (skinny(p)) return launch_ff_skinny(p, s);
     const int bm = plan(&p, 1);
     place_parts(&p, 1, part);
-    if (bm == 128)
+    if (bm == 256)
+        launch<256>(p, s);
+    else if (bm == 128)
         launch<128>(p, s);
     else
         launch<64>(p, s);
@@ -736,15 +896,21 @@ hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
     return e != hipSuccess ? e : sum_pieces(&p, 1, s);
 }
 
-hipError_t launch_ff_products(const FfProduct* p, int n, float* part, hipStream_t s) {
+hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const PartialSums& sums, hipStream_t s) {
+    if (n == 0) return launch_sum_partials(sums, s);
     FfGroup g = {};
+    g.sums = sums;
     g.n = n;
     for (int i = 0; i < n; ++i) g.p[i] = p[i];
     const int bm = plan(g.p, n);
     place_parts(g.p, n, part);
     unsigned grid = 0;
     for (int i = 0; i < n; ++i) grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;
-    if (bm == 128)
+    g.product_blocks = (int32_t)grid;
+    grid += (unsigned)partial_sum_blocks(sums);
+    if (bm == 256)
+        ff_products<256><<<grid, THREADS, 0, s>>>(g);
+    else if (bm == 128)
         ff_products<128><<<grid, THREADS, 0, s>>>(g);
     else
         ff_products<64><<<grid, THREADS, 0, s>>>(g);

@@ -315,6 +315,6 @@ PCPP_EXPORT int pcpp_rms_norm_backward(int64_t rows, int32_t channels, float eps
     });
     if (hipGetLastError() != hipSuccess) return PCPP_EHIP;
     if (!dgamma) return PCPP_OK;
-    return launch_sum_partials(p.partial, blocks, channels, dgamma, (hipStream_t)stream) == hipSuccess ? PCPP_OK
-                                                                                                       : PCPP_EHIP;
+    const PartialSums sums = {{p.partial, nullptr}, {(bf16*)dgamma, nullptr}, {blocks, 0}, {channels, 0}};
+    return launch_sum_partials(sums, (hipStream_t)stream) == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }
