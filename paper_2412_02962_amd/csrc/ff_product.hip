@@ -17,17 +17,14 @@ namespace {
 constexpr int KT = 64;  // contraction per tile
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
-#ifndef TK0
-#define TK0 0.45
-#define TK1 0.75
-#define TK2 1.25
-#endif
 
-// A tile's rows of X (64, 128 or 256) say which it is; its rows of W, its ring
-// in LDS and how many of its workgroups share a compute unit.
-constexpr int rows_w(int bm) { return bm == 64 ? 128 : 256; }
-constexpr int lds_bytes(int bm) { return (bm == 64 ? 144 : bm == 128 ? 80 : 128) * 1024; }
-constexpr int per_cu(int bm) { return bm == 128 ? 2 : 1; }
+// The kinds of tile: their rows of X and W, ring in LDS, and how many of their
+// workgroups share a compute unit.
+enum { TILE_64, TILE_128, TILE_256, TILE_KINDS };
+constexpr int rows_x(int kind) { return 64 << kind; }
+constexpr int rows_w(int kind) { return kind == TILE_64 ? 128 : 256; }
+constexpr int lds_bytes(int kind) { return (kind == TILE_64 ? 72 : kind == TILE_128 ? 80 : 128) * 1024; }
+constexpr int per_cu(int kind) { return kind == TILE_256 ? 1 : 2; }
 
 typedef __attribute__((address_space(3))) void* lptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -166,10 +163,7 @@ struct View {
 // run of items, and those are ordered as pieces of the contraction, then
 // groups of kGroup tiles along the rows, walked along the outputs: what an XCD
 // works on at a time is about square and shares its operands in the L2.
-#ifndef KG
-#define KG 8
-#endif
-constexpr int kGroup = KG;
+constexpr int kGroup = 4;
 struct Item {
     int m0, n0, piece, first, count;  // rows and outputs from; piece; its k-tiles
 };
@@ -189,24 +183,24 @@ __device__ __forceinline__ Item item_of(const FfProduct& p, int item) {
     return it;
 }
 
-// The outputs of a tile from its wavefronts' sums (BM / WM x BN / WN each).
-template <int BM, int BN, int WM, bool XT, bool WT, int EPI, int ACT>
+// The outputs of a tile from its wavefronts' sums: two wavefronts along X's
+// rows, two along W's.
+template <int KIND, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
-                                           f32x16 (&acc)[BN * WM / (32 * WAVES)][BM / (32 * WM)], char* lds) {
+                                           f32x16 (&acc)[rows_w(KIND) / 64][rows_x(KIND) / 64], char* lds) {
     const int m0 = it.m0, n0 = it.n0;
-    constexpr int WN = WAVES / WM;
-    constexpr int TM = BM / WM, TN = BN / WN;
-    constexpr int MB = TM / 32, NB = TN / 32;
+    constexpr int TM = rows_x(KIND) / 2, TN = rows_w(KIND) / 2;  // of a wavefront
+    constexpr int NB = TN / 32;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % WM, wn = wave / WM;
+    const int wm = wave & 1, wn = wave >> 1;
     // acc[i][j][e]: W row 32 i + 8 (e / 4) + 4 (lane / 32) + e % 4 of the
     // wavefront, X row 32 j + lane % 32.  The sums go through LDS, 32 X rows
     // of the wavefront at a time, so that a lane then has eight consecutive
     // outputs of a row: loads and stores run along the rows, and a lane's
     // columns are the same in every pass.
     constexpr int LDF = TN + 4;  // floats per row: 16 rows written at one column on distinct banks
-    static_assert(WAVES * 32 * LDF * 4 <= lds_bytes(BM), "a slab of every wavefront fits the stages");
+    static_assert(WAVES * 32 * LDF * 4 <= lds_bytes(KIND), "a slab of every wavefront fits the stages");
     constexpr int TNO = EPI == FF_GATE ? TN / 2 : TN;  // outputs of a wavefront's row
     constexpr int C8 = TNO / 8, RPP = 64 / C8, PASSES = 32 / RPP;
     float* tab = (float*)lds + wave * 32 * LDF;
@@ -322,14 +316,16 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
     }
 }
 
-// A 64 x 128 tile, for few tiles: four wavefronts of 32 x 64 and a ring of six
-// stages of 24 KB, so that five k-tiles are on their way while one is worked
-// on.  A step's operands are read behind the products of the step before, a
-// k-tile's first ones behind the last of the one before it (the first
-// k-tile's are products with zeros).
+// A 64 x 128 tile, for few tiles: four wavefronts of 32 x 64 and a ring of
+// three stages of 24 KB, two workgroups to a compute unit (six stages and one
+// workgroup were no faster alone, 0.3 us a k-tile, about what 24 KB take from
+// the L2, and left the epilogue uncovered: the up product of 2093 x 640 x 2560
+// 45 us, now 31).  A step's operands are read behind the products of the step
+// before, a k-tile's first ones behind the last of the one before it (the
+// first k-tile's are products with zeros).
 template <bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item, char* lds) {
-    constexpr int STAGES = 6, STAGE = (64 + 128) * KT * 2;
+    constexpr int STAGES = 3, STAGE = (64 + 128) * KT * 2;
     typedef Layout<64, XT> LX;
     typedef Layout<128, WT> LW;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -379,10 +375,10 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
         w.advance();
         wr = next_of(wr);
     }
-    static_assert(LX::PIECES + LW::PIECES == 6, "24 of a wavefront's loads are four k-tiles'");
+    static_assert(LX::PIECES + LW::PIECES == 6, "six of a wavefront's loads are a k-tile's");
     for (int t = 0; t < it.count; ++t) {
         // The k-tile has landed and the one before has been read, everyone's.
-        asm volatile("s_waitcnt vmcnt(24) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(6 * (STAGES - 2)) : "memory");
         const u32x4 xb = x.buffer(0), wb = w.buffer(0);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -406,7 +402,7 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     for (int i = 0; i < 2; ++i) acc[i][0] = mfma32x32x16(o[1].w[i], o[1].x, acc[i][0]);
     // Loads past the end are still on their way (zeros) to the stages.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<64, 128, 2, XT, WT, EPI, ACT>(p, it, acc, lds);
+    store_tile<TILE_64, XT, WT, EPI, ACT>(p, it, acc, lds);
 }
 
 // A 128 x 256 tile, two workgroups to a compute unit: while one waits at a
@@ -563,7 +559,7 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     __builtin_amdgcn_s_setprio(0);
     // Loads past the end are still on their way (zeros) to the slots.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<128, 256, 2, XT, WT, EPI, ACT>(p, it, acc, lds);
+    store_tile<TILE_128, XT, WT, EPI, ACT>(p, it, acc, lds);
 }
 
 // A 256 x 256 tile, for the products without an epilogue where there are tiles
@@ -683,39 +679,38 @@ __device__ __forceinline__ void product_tile_256x256(const FfProduct& p, int ite
     }
     // Loads past the end are still on their way (zeros) to the slots.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<256, 256, 2, XT, WT, FF_STORE, 0>(p, it, acc, lds);
+    store_tile<TILE_256, XT, WT, FF_STORE, 0>(p, it, acc, lds);
 }
 
-template <int BM, bool XT, bool WT, int EPI, int ACT>
+template <int KIND, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile(const FfProduct& p, int item, char* lds) {
-    if constexpr (BM == 256)
+    if constexpr (KIND == TILE_256)
         product_tile_256x256<XT, WT>(p, item, lds);
-    else if constexpr (BM == 128)
+    else if constexpr (KIND == TILE_128)
         product_tile_128x256<XT, WT, EPI, ACT>(p, item, lds);
     else
         product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
 }
 
-template <int BM, bool XT, bool WT, int EPI, int ACT>
-__global__ __launch_bounds__(THREADS, per_cu(BM)) void ff_product(FfProduct p) {
-    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
+template <int KIND, bool XT, bool WT, int EPI, int ACT>
+__global__ __launch_bounds__(THREADS, per_cu(KIND)) void ff_product(FfProduct p) {
+    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(KIND)];
     const int item = (int)(blockIdx.x % p.n_xcd) * p.per_xcd + (int)(blockIdx.x / p.n_xcd);
-    if (item < p.items) product_tile<BM, XT, WT, EPI, ACT>(p, item, lds);
+    if (item < p.items) product_tile<KIND, XT, WT, EPI, ACT>(p, item, lds);
 }
 
 // Up to three products of FF_STORE with W across the contraction in one
-// launch, X across it first (the weights' gradients), then X along it: their
-// items together leave fewer compute units idle at the end than three launches
-// do.  The sums of the biases' gradients ride along.
+// launch (X across it too: the weights' gradients; or along it): their items
+// together leave fewer compute units idle at the end than three launches do.  The sums of the biases' gradients ride along.
 struct FfGroup {
     FfProduct p[3];
     int32_t n;
     int32_t product_blocks;  // workgroups of the products; those after them do the sums
     PartialSums sums;
 };
-template <int BM>
-__global__ __launch_bounds__(THREADS, per_cu(BM)) void ff_products(FfGroup g) {
-    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(BM)];
+template <int KIND>
+__global__ __launch_bounds__(THREADS, per_cu(KIND)) void ff_products(FfGroup g) {
+    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(KIND)];
     if ((int)blockIdx.x >= g.product_blocks) {
         sum_partials(g.sums, blockIdx.x - g.product_blocks, (float*)lds);
         return;
@@ -727,9 +722,9 @@ __global__ __launch_bounds__(THREADS, per_cu(BM)) void ff_products(FfGroup g) {
     const int item = (int)(blockIdx.x % n_xcd) * p.per_xcd + j;
     if (item >= p.items) return;
     if (p.x_t)
-        product_tile<BM, true, true, FF_STORE, 0>(p, item, lds);
+        product_tile<KIND, true, true, FF_STORE, 0>(p, item, lds);
     else
-        product_tile<BM, false, true, FF_STORE, 0>(p, item, lds);
+        product_tile<KIND, false, true, FF_STORE, 0>(p, item, lds);
 }
 
 // out = the pieces' sums, in their order, + bias: eight outputs a thread.
@@ -761,32 +756,45 @@ __global__ __launch_bounds__(256) void ff_sum_pieces(FfSums a) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int64_t tiles_of(const FfProduct& p, int bm) {
-    return ceil_div(p.M, bm) * ceil_div(p.N, p.epilogue == FF_GATE ? rows_w(bm) / 2 : rows_w(bm));
+int64_t tiles_of(const FfProduct& p, int kind) {
+    return ceil_div(p.M, rows_x(kind)) * ceil_div(p.N, p.epilogue == FF_GATE ? rows_w(kind) / 2 : rows_w(kind));
 }
 
 // Most pieces of a contraction, and most floats of all pieces' sums of a launch.
 constexpr int kMaxPieces = 32;
 constexpr int64_t kMaxPartFloats = 16 << 20;
 
-// Time in us of n products on tiles of bm x 2 bm, their contractions in runs
-// of at most `run` k-tiles.
-constexpr double kTileUs[3] = {TK0, TK1, TK2}, kItemUs[3] = {3.0, 4.0, 5.0};
-double estimate(const FfProduct* p, int n, int bm, int64_t run, int cus, int64_t& floats) {
-    const int kind = bm / 128;
+// Pieces of a contraction in runs of about `run` k-tiles.
+int64_t pieces_of(const FfProduct& p, int64_t run) {
+    const int64_t n = (ceil_div(p.K, KT) + run / 2) / run;
+    return n > 1 ? n : 1;
+}
+
+// Time in us of n products on a kind of tile, their contractions in runs
+// of about `run` k-tiles; floats: the pieces' sums.  Per k-tile and per item
+// (its start and epilogue), alone on a compute unit and when all of them have
+// all the workgroups that fit, as measured (300 to 16385 tokens at 640 x 2560
+// and 1280 x 5120).
+struct TileCost {
+    double tile, item[3];  // item: by epilogue
+};
+constexpr TileCost kAlone[TILE_KINDS] = {{0.31, {5, 6.5, 10}}, {0.72, {7, 12, 18}}, {1.08, {8}}};
+constexpr TileCost kFull[TILE_KINDS] = {{0.40, {1.5, 2, 4.3}}, {0.95, {4, 6, 18}}, {1.45, {8}}};
+double estimate(const FfProduct* p, int n, int kind, int64_t run, int cus, int64_t& floats) {
     double work = 0, longest = 0;
     int64_t items = 0;
     floats = 0;
     for (int i = 0; i < n; ++i) {
-        const int64_t nkt = ceil_div(p[i].K, KT), pieces = ceil_div(nkt, run), t = tiles_of(p[i], bm) * pieces;
-        const double len = (double)nkt / pieces * kTileUs[kind] + kItemUs[kind];
+        const int64_t nkt = ceil_div(p[i].K, KT), pieces = pieces_of(p[i], run), t = tiles_of(p[i], kind) * pieces;
+        const double len = (double)nkt / pieces;
+        const double alone = len * kAlone[kind].tile + kAlone[kind].item[p[i].epilogue];
         items += t;
-        work += t * len;
-        if (len > longest) longest = len;
+        work += t * (len * kFull[kind].tile + kFull[kind].item[p[i].epilogue]);
+        if (alone > longest) longest = alone;
         if (pieces > 1) floats += pieces * p[i].M * p[i].N;
     }
-    const double spread = work / cus + (items > cus ? longest / 2 : 0);
-    return (spread > longest ? spread : longest) + (floats > 0 ? 4.0 + 8.0 * floats / 4.5e6 : 0);
+    const double spread = work / cus + (items > cus * per_cu(kind) ? longest / 4 : 0);
+    return (spread > longest ? spread : longest) + (floats > 0 ? 5.0 + 8.0 * floats / 3.5e6 : 0);
 }
 
 // The tile and the pieces of the products that are estimated fastest.
@@ -794,29 +802,29 @@ int plan(FfProduct* p, int n) {
     const int device = device_cus(), cus = device > 0 ? device : 256;
     int64_t longest = 0;
     for (int i = 0; i < n; ++i) longest = longest > ceil_div(p[i].K, KT) ? longest : ceil_div(p[i].K, KT);
-    int best_bm = 128;
+    int best_kind = TILE_128;
     int64_t best_run = longest;
     double best = 1e30;
     constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, kMaxPieces};
-    for (int bm = 64; bm <= (p[0].epilogue == FF_STORE ? 256 : 128); bm *= 2)
+    for (int kind = 0; kind <= (p[0].epilogue == FF_STORE ? TILE_256 : TILE_128); ++kind)
         for (int cut : kCuts) {
             if (cut > 1 && p[0].epilogue != FF_STORE) break;
             const int64_t run = ceil_div(longest, cut);
             int64_t floats = 0;
-            const double t = estimate(p, n, bm, run, cus, floats);
+            const double t = estimate(p, n, kind, run, cus, floats);
             if (floats > kMaxPartFloats || t >= best) continue;
             best = t;
-            best_bm = bm;
+            best_kind = kind;
             best_run = run;
         }
     const int n_xcd = layout_for(cus, cus).n_xcd;
     for (int i = 0; i < n; ++i) {
-        p[i].pieces = (int32_t)ceil_div(ceil_div(p[i].K, KT), best_run);
-        p[i].items = (int32_t)(tiles_of(p[i], best_bm) * p[i].pieces);
+        p[i].pieces = (int32_t)pieces_of(p[i], best_run);
+        p[i].items = (int32_t)(tiles_of(p[i], best_kind) * p[i].pieces);
         p[i].n_xcd = n_xcd;
         p[i].per_xcd = (p[i].items + n_xcd - 1) / n_xcd;
     }
-    return best_bm;
+    return best_kind;
 }
 
 // Places the sums of pieces in `part`.
@@ -847,20 +855,20 @@ hipError_t sum_pieces(const FfProduct* p, int n, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int BM>
+template <int KIND>
 void launch(const FfProduct& p, hipStream_t s) {
     const unsigned grid = (unsigned)p.n_xcd * p.per_xcd;
     auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p); };
     if (p.epilogue == FF_STORE) {
-        run(ff_product<BM, false, false, FF_STORE, 0>);
-    } else if constexpr (BM < 256) {
+        run(ff_product<KIND, false, false, FF_STORE, 0>);
+    } else if constexpr (KIND != TILE_256) {
         const bool silu = p.act == PCPP_ACT_SILU;
         if (p.epilogue == FF_GATE)
-            run(silu ? ff_product<BM, false, false, FF_GATE, PCPP_ACT_SILU>
-                     : ff_product<BM, false, false, FF_GATE, PCPP_ACT_GELU>);
+            run(silu ? ff_product<KIND, false, false, FF_GATE, PCPP_ACT_SILU>
+                     : ff_product<KIND, false, false, FF_GATE, PCPP_ACT_GELU>);
         else
-            run(silu ? ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
-                     : ff_product<BM, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
+            run(silu ? ff_product<KIND, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
+                     : ff_product<KIND, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
     }
 }
 
@@ -870,7 +878,7 @@ bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && p.epilogue != 
 
 int ff_partial_rows(const FfProduct& p) {
     FfProduct q = p;
-    return (int)(2 * ceil_div(p.M, plan(&q, 1)));
+    return (int)(2 * ceil_div(p.M, rows_x(plan(&q, 1))));
 }
 
 int64_t ff_part_floats(const FfProduct* p, int n) {
@@ -884,14 +892,14 @@ int64_t ff_part_floats(const FfProduct* p, int n) {
 
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
     if (skinny(p)) return launch_ff_skinny(p, s);
-    const int bm = plan(&p, 1);
+    const int kind = plan(&p, 1);
     place_parts(&p, 1, part);
-    if (bm == 256)
-        launch<256>(p, s);
-    else if (bm == 128)
-        launch<128>(p, s);
+    if (kind == TILE_256)
+        launch<TILE_256>(p, s);
+    else if (kind == TILE_128)
+        launch<TILE_128>(p, s);
     else
-        launch<64>(p, s);
+        launch<TILE_64>(p, s);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : sum_pieces(&p, 1, s);
 }
@@ -901,19 +909,23 @@ hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const Part
     FfGroup g = {};
     g.sums = sums;
     g.n = n;
-    for (int i = 0; i < n; ++i) g.p[i] = p[i];
-    const int bm = plan(g.p, n);
+    for (int i = 0; i < n; ++i) {  // the longest contractions first
+        int at = i;
+        for (; at > 0 && g.p[at - 1].K < p[i].K; --at) g.p[at] = g.p[at - 1];
+        g.p[at] = p[i];
+    }
+    const int kind = plan(g.p, n);
     place_parts(g.p, n, part);
     unsigned grid = 0;
     for (int i = 0; i < n; ++i) grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;
     g.product_blocks = (int32_t)grid;
     grid += (unsigned)partial_sum_blocks(sums);
-    if (bm == 256)
-        ff_products<256><<<grid, THREADS, 0, s>>>(g);
-    else if (bm == 128)
-        ff_products<128><<<grid, THREADS, 0, s>>>(g);
+    if (kind == TILE_256)
+        ff_products<TILE_256><<<grid, THREADS, 0, s>>>(g);
+    else if (kind == TILE_128)
+        ff_products<TILE_128><<<grid, THREADS, 0, s>>>(g);
     else
-        ff_products<64><<<grid, THREADS, 0, s>>>(g);
+        ff_products<TILE_64><<<grid, THREADS, 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : sum_pieces(g.p, n, s);
 }

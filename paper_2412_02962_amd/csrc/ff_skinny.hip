@@ -1,5 +1,5 @@
 // The gated feed-forward's products on few tokens (see feed_forward.h): at
-// most 128 rows of X, both operands along the contraction.
+// most 16 rows of X, both operands along the contraction.
 //
 // What bounds them is the weights' way from memory, each read once (1 token,
 // 1280 x 5120: 39 MB), and the latency of a load, of which a loop over tiles
@@ -23,13 +23,12 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// MT blocks of 16 tokens; FF_GATE: 32 outputs, W rows n0 .. + 31 and N further
-// on; FF_STORE: 16 outputs.
-template <int MT, int EPI, int ACT>
+// FF_GATE: 32 outputs, W rows n0 .. + 31 and N further on; FF_STORE: 16 outputs.
+template <int EPI, int ACT>
 __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
     constexpr int NB = EPI == FF_GATE ? 4 : 1;             // blocks of 16 W rows
     constexpr int BNO = EPI == FF_GATE ? 32 : 16;
-    constexpr int U = NB + MT <= 5 ? 8 : NB + MT <= 8 ? 4 : 2;  // k-steps in flight
+    constexpr int U = 8;  // k-steps in flight
     __shared__ f32x4 sums[kWaves][NB][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lr = lane & 15, lq = lane >> 4;
@@ -39,23 +38,16 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
         w[i] = p.w + (int64_t)(n0 + 16 * (i & 1) + (i >= 2 ? p.N : 0) + lr) * p.ldw + 8 * lq;
-    const bf16* x[MT];
-    bool there[MT];
+    const bool there = lr < p.M;
+    const bf16* x = p.x + (int64_t)(there ? lr : 0) * p.ldx + 8 * lq;
+    f32x4 acc[NB];
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        there[j] = 16 * j + lr < p.M;
-        x[j] = p.x + (int64_t)(there[j] ? 16 * j + lr : 0) * p.ldx + 8 * lq;
-    }
-    f32x4 acc[NB][MT];
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     const int steps = p.K / 32;  // K % 64 == 0
     const int s1 = steps * (wave + 1) / kWaves;
     for (int s = steps * wave / kWaves; s < s1; s += U) {
-        bf16x8 wv[U][NB], xv[U][MT];
+        bf16x8 wv[U][NB], xv[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const bool in = s + u < s1;  // past the end: zeros
@@ -64,85 +56,63 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
                 wv[u][i] = bf16x8{};
                 if (in) wv[u][i] = *(const bf16x8*)(w[i] + 32 * (s + u));
             }
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                xv[u][j] = bf16x8{};
-                if (in && there[j]) xv[u][j] = *(const bf16x8*)(x[j] + 32 * (s + u));
-            }
+            xv[u] = bf16x8{};
+            if (in && there) xv[u] = *(const bf16x8*)(x + 32 * (s + u));
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-                for (int j = 0; j < MT; ++j) acc[i][j] = mfma16(wv[u][i], xv[u][j], acc[i][j]);
+            for (int i = 0; i < NB; ++i) acc[i] = mfma16(wv[u][i], xv[u], acc[i]);
     }
 
-    // acc[i][j][e]: W row 16 i + 4 lq + e, token 16 j + lr
+    // acc[i][e]: W row 16 i + 4 lq + e, token lr
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        if (j > 0) __syncthreads();
+    for (int i = 0; i < NB; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    const int n = threadIdx.x % BNO, m = threadIdx.x / BNO;  // output, token
+    auto total = [&](int i, int row) {  // of row `row` of block i, the wavefronts in their order
+        float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) sums[wave][i][lane] = acc[i][j];
-        __syncthreads();
-        const int n = threadIdx.x % BNO, r = threadIdx.x / BNO;  // output, token of the block
-        const int m = 16 * j + r;
-        auto total = [&](int i, int row) {  // of row `row` of block i, the wavefronts in their order
-            float t = 0.f;
-#pragma unroll
-            for (int k = 0; k < kWaves; ++k) t += sums[k][i][16 * (row >> 2) + r][row & 3];
-            return t;
-        };
-        if (r >= 16 || m >= p.M) continue;  // a group's 32 lanes together
-        if constexpr (EPI == FF_GATE) {
-            float v = total(n >> 4, n & 15), g = total(2 + (n >> 4), n & 15);
-            if (p.bias != nullptr) {
-                v += bf16_to_f32(p.bias[n0 + n]);
-                g += bf16_to_f32(p.bias[p.N + n0 + n]);
-            }
-            if (p.codes != nullptr) {
-                const int64_t at = (int64_t)m * 2 * p.N + n0 + n;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float a = h ? g : v;
-                    float top = finite_abs(a);
-#pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-                    const int scale = eight_scale(top);
-                    p.codes[at + h * p.N] = (uint8_t)to_e4m3(eight_scaled(a, eight_inverse(scale)), 0.f, 0.f, 0.f);
-                    if (n == 0) p.scales[(at + h * p.N) / EIGHT_GROUP] = (uint8_t)scale;
-                }
-            }
-            p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v * ff_act<ACT>(g));
-        } else {
-            float v = total(0, n);
-            if (p.bias != nullptr) v += bf16_to_f32(p.bias[n0 + n]);
-            p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v);
+        for (int k = 0; k < kWaves; ++k) t += sums[k][i][16 * (row >> 2) + m][row & 3];
+        return t;
+    };
+    if (m >= 16 || m >= p.M) return;  // a group's 32 lanes together
+    if constexpr (EPI == FF_GATE) {
+        float v = total(n >> 4, n & 15), g = total(2 + (n >> 4), n & 15);
+        if (p.bias != nullptr) {
+            v += bf16_to_f32(p.bias[n0 + n]);
+            g += bf16_to_f32(p.bias[p.N + n0 + n]);
         }
+        if (p.codes != nullptr) {
+            const int64_t at = (int64_t)m * 2 * p.N + n0 + n;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float a = h ? g : v;
+                float top = finite_abs(a);
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+                const int scale = eight_scale(top);
+                p.codes[at + h * p.N] = (uint8_t)to_e4m3(eight_scaled(a, eight_inverse(scale)), 0.f, 0.f, 0.f);
+                if (n == 0) p.scales[(at + h * p.N) / EIGHT_GROUP] = (uint8_t)scale;
+            }
+        }
+        p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v * ff_act<ACT>(g));
+    } else {
+        float v = total(0, n);
+        if (p.bias != nullptr) v += bf16_to_f32(p.bias[n0 + n]);
+        p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v);
     }
-}
-
-template <int MT>
-void launch(const FfProduct& p, hipStream_t s) {
-    if (p.epilogue == FF_STORE)
-        ff_skinny<MT, FF_STORE, 0><<<p.N / 16, kThreads, 0, s>>>(p);
-    else if (p.act == PCPP_ACT_SILU)
-        ff_skinny<MT, FF_GATE, PCPP_ACT_SILU><<<p.N / 32, kThreads, 0, s>>>(p);
-    else
-        ff_skinny<MT, FF_GATE, PCPP_ACT_GELU><<<p.N / 32, kThreads, 0, s>>>(p);
 }
 
 }  // namespace
 
 hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s) {
-    if (p.M <= 16)
-        launch<1>(p, s);
-    else if (p.M <= 32)
-        launch<2>(p, s);
-    else if (p.M <= 64)
-        launch<4>(p, s);
+    if (p.epilogue == FF_STORE)
+        ff_skinny<FF_STORE, 0><<<p.N / 16, kThreads, 0, s>>>(p);
+    else if (p.act == PCPP_ACT_SILU)
+        ff_skinny<FF_GATE, PCPP_ACT_SILU><<<p.N / 32, kThreads, 0, s>>>(p);
     else
-        launch<8>(p, s);
+        ff_skinny<FF_GATE, PCPP_ACT_GELU><<<p.N / 32, kThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 
