@@ -793,8 +793,8 @@ double estimate(const FfProduct* p, int n, int kind, int64_t run, int cus, int64
         if (alone > longest) longest = alone;
         if (pieces > 1) floats += pieces * p[i].M * p[i].N;
     }
-    const double spread = work / cus + (items > cus * per_cu(kind) ? longest / 4 : 0);
-    return (spread > longest ? spread : longest) + (floats > 0 ? 5.0 + 8.0 * floats / 3.5e6 : 0);
+    const double busiest = work / items * ceil_div(items, cus);  // of the compute units
+    return (busiest > longest ? busiest : longest) + (floats > 0 ? 5.0 + 8.0 * floats / 3.5e6 : 0);
 }
 
 // The tile and the pieces of the products that are estimated fastest.
