@@ -838,6 +838,23 @@ int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w,
                   void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * Launch plan of one of the block's products (host only, no GPU work; for
+ * diagnostics and tests), the weights' gradients and dx as one launch has all
+ * three of them; cus > 0: a device of `cus` compute units, 0: the current one
+ * (PCPP_EHIP if it cannot be queried).  Outputs (any may be NULL): rows and
+ * outputs of a workgroup's tile and the pieces the contraction is worked in.
+ */
+#define PCPP_FF_UP        0   /* x ff1_w^T                                   */
+#define PCPP_FF_DOWN      1   /* h ff2_w^T                                   */
+#define PCPP_FF_GATE_GRAD 2   /* dy ff2_w                                    */
+#define PCPP_FF_W1_GRAD   3   /* [dv, dg]^T x                                */
+#define PCPP_FF_W2_GRAD   4   /* dy^T h                                      */
+#define PCPP_FF_X_GRAD    5   /* [dv, dg] ff1_w                              */
+int pcpp_gated_ff_plan(const pcpp_ff_geom_t* g, int32_t which, int32_t cus,
+                       int32_t* tile_rows, int32_t* tile_outputs,
+                       int32_t* pieces);
+
+/*
  * Backward, from the 8-bit checkpoint of v and g (no product is computed
  * again):
  *   dh = dy ff2_w;  dv = dh * act(g);  dg = dh * v * act'(g);  h = v * act(g)

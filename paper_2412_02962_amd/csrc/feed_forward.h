@@ -39,15 +39,21 @@ struct FfProduct {
     int32_t items, n_xcd, per_xcd;
 };
 int ff_partial_rows(const FfProduct& p);  // of a product's sizes and epilogue
-// FF_STORE or FF_GATE on at most FF_SKINNY_ROWS rows of X, both operands along
-// the contraction (ff_skinny.hip); launch_ff_product calls it for these.
+// FF_GATE, and FF_STORE of what it wrote, on at most FF_SKINNY_ROWS rows of X,
+// both operands along the contraction (ff_skinny.hip); launch_ff_product calls
+// it for these.  On at most FF_SPLIT_ROWS FF_GATE's out and FF_STORE's x are
+// [2][M][F], two bf16 whose sum is h.
+constexpr int FF_SPLIT_ROWS = 8;
 constexpr int FF_SKINNY_ROWS = 16;
 hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s);
 // A product with X along the contraction (W across it for FF_GATE_GRAD alone),
-// and up to three of FF_STORE with w_t = 1 in one launch
-// (which also does `sums`).  part: ff_part_floats of the same products, or of these and others.
+// and up to three of FF_STORE with w_t = 1 in one launch (which also does
+// `sums`).  part: ff_part_floats of the same products, or of these and others.
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s);
 hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const PartialSums& sums, hipStream_t s);
 int64_t ff_part_floats(const FfProduct* p, int n);
+// What they run on with `cus` compute units (0: the current device's): the
+// tile, and the pieces in p.
+void ff_plan(FfProduct* p, int n, int cus, int32_t* tile_rows, int32_t* tile_outputs);
 
 }  // namespace pcpp

@@ -15,6 +15,7 @@
 #include "checkpoint.h"
 #include "column_sums.h"
 #include "eight_bit.h"
+#include "kernels.h"
 
 #define PCPP_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -73,7 +74,7 @@ FfProduct x_grad_of(const pcpp_ff_geom_t& g) {
 struct ForwardLayout : Layout {
     size_t h, part;
     explicit ForwardLayout(const pcpp_ff_geom_t& g) {
-        h = add(2 * g.tokens * g.ff_inner);
+        h = add((g.tokens <= FF_SPLIT_ROWS ? 4 : 2) * g.tokens * g.ff_inner);
         const FfProduct down = down_of(g);
         part = add(4 * ff_part_floats(&down, 1));
     }
@@ -108,6 +109,27 @@ using namespace pcpp;
 PCPP_EXPORT size_t pcpp_gated_ff_workspace_size(const pcpp_ff_geom_t* g) {
     if (check_geom(g) != PCPP_OK) return 0;
     return ForwardLayout(*g).size;
+}
+
+PCPP_EXPORT int pcpp_gated_ff_plan(const pcpp_ff_geom_t* g, int32_t which, int32_t cus, int32_t* tile_rows,
+                                   int32_t* tile_outputs, int32_t* pieces) {
+    const int st = check_geom(g);
+    if (st != PCPP_OK) return st;
+    if (which < PCPP_FF_UP || which > PCPP_FF_X_GRAD || cus < 0) return PCPP_EINVAL;
+    if (cus == 0 && device_cus() == 0) return PCPP_EHIP;
+    FfProduct p[] = {w1_grad_of(*g), w2_grad_of(*g), x_grad_of(*g)};
+    int n = 3, at = which - PCPP_FF_W1_GRAD;
+    if (which < PCPP_FF_W1_GRAD) {
+        p[0] = which == PCPP_FF_UP ? up_of(*g) : which == PCPP_FF_DOWN ? down_of(*g) : gate_grad_of(*g);
+        n = 1;
+        at = 0;
+    }
+    int32_t rows, outputs;
+    ff_plan(p, n, cus, &rows, &outputs);
+    if (tile_rows) *tile_rows = rows;
+    if (tile_outputs) *tile_outputs = outputs;
+    if (pieces) *pieces = p[at].pieces;
+    return PCPP_OK;
 }
 
 PCPP_EXPORT int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w, const void* x, void* y,

@@ -339,9 +339,8 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     uint32_t xoff[LX::PIECES], woff[LW::PIECES];
 #pragma unroll
     for (int q = 0; q < LX::PIECES; ++q) xoff[q] = LX::offset(q, wave, p.ldx, [](int r) { return (int64_t)r; });
-    // FF_GATE: of every 64 rows 32 are values, 32 their gates
 #pragma unroll
-    for (int q = 0; q < LW::PIECES; ++q)
+    for (int q = 0; q < LW::PIECES; ++q)  // FF_GATE: of every 64 rows 32 are values, 32 their gates
         woff[q] = LW::offset(q, wave, p.ldw, [&](int r) {
             return EPI == FF_GATE ? (int64_t)(32 * (r >> 6) + (r & 31)) + ((r & 32) ? p.N : 0) : (int64_t)r;
         });
@@ -497,10 +496,12 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     step_read();
 
     // Phase i: products of wc with x0 and x1; the reads and loads listed above.
+    // Before it, this wavefront's part of the units to read has landed (five or
+    // six younger units, two loads each, may be in flight) and it has read
+    // those of two phases ago (the phase before read two units, or one, of at
+    // least four reads each); then everyone's.
     auto phase = [&](int i, const Frag& wc, Frag& wnext, const Frag& x0, Frag& x1, Frag& x0next) {
-        if (i == 0)
-            asm volatile("s_waitcnt vmcnt(10) lgkmcnt(8)\n\ts_barrier" ::: "memory");
-        else if (i == 1)
+        if (i < 2)
             asm volatile("s_waitcnt vmcnt(10) lgkmcnt(8)\n\ts_barrier" ::: "memory");
         else
             asm volatile("s_waitcnt vmcnt(12) lgkmcnt(4)\n\ts_barrier" ::: "memory");
@@ -797,9 +798,13 @@ double estimate(const FfProduct* p, int n, int kind, int64_t run, int cus, int64
     return (busiest > longest ? busiest : longest) + (floats > 0 ? 5.0 + 8.0 * floats / 3.5e6 : 0);
 }
 
+int cus_here() {
+    const int cus = device_cus();
+    return cus > 0 ? cus : 256;
+}
+
 // The tile and the pieces of the products that are estimated fastest.
-int plan(FfProduct* p, int n) {
-    const int device = device_cus(), cus = device > 0 ? device : 256;
+int plan(FfProduct* p, int n, int cus) {
     int64_t longest = 0;
     for (int i = 0; i < n; ++i) longest = longest > ceil_div(p[i].K, KT) ? longest : ceil_div(p[i].K, KT);
     int best_kind = TILE_128;
@@ -878,7 +883,7 @@ bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && p.epilogue != 
 
 int ff_partial_rows(const FfProduct& p) {
     FfProduct q = p;
-    return (int)(2 * ceil_div(p.M, rows_x(plan(&q, 1))));
+    return (int)(2 * ceil_div(p.M, rows_x(plan(&q, 1, cus_here()))));
 }
 
 int64_t ff_part_floats(const FfProduct* p, int n) {
@@ -890,9 +895,21 @@ int64_t ff_part_floats(const FfProduct* p, int n) {
     return most < kMaxPartFloats ? most : kMaxPartFloats;
 }
 
+void ff_plan(FfProduct* p, int n, int cus, int32_t* tile_rows, int32_t* tile_outputs) {
+    if (skinny(p[0])) {
+        p[0].pieces = 1;
+        *tile_rows = FF_SKINNY_ROWS;
+        *tile_outputs = p[0].epilogue == FF_GATE ? 32 : 16;
+        return;
+    }
+    const int kind = plan(p, n, cus > 0 ? cus : cus_here());
+    *tile_rows = rows_x(kind);
+    *tile_outputs = p[0].epilogue == FF_GATE ? rows_w(kind) / 2 : rows_w(kind);
+}
+
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
     if (skinny(p)) return launch_ff_skinny(p, s);
-    const int kind = plan(&p, 1);
+    const int kind = plan(&p, 1, cus_here());
     place_parts(&p, 1, part);
     if (kind == TILE_256)
         launch<TILE_256>(p, s);
@@ -914,7 +931,7 @@ hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const Part
         for (; at > 0 && g.p[at - 1].K < p[i].K; --at) g.p[at] = g.p[at - 1];
         g.p[at] = p[i];
     }
-    const int kind = plan(g.p, n);
+    const int kind = plan(g.p, n, cus_here());
     place_parts(g.p, n, part);
     unsigned grid = 0;
     for (int i = 0; i < n; ++i) grid += (unsigned)g.p[i].n_xcd * g.p[i].per_xcd;

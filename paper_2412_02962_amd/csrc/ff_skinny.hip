@@ -8,6 +8,14 @@
 // contraction each; W goes straight from memory into the MFMA's operand
 // registers, a run of k-steps in flight at a time, as does X, which the L2
 // holds.  The wavefronts' sums meet in LDS.
+//
+// Between the two products of up to eight tokens, h's values are sums of two
+// bf16, 16 significant bits, so that y is rounded once: the matrix unit takes
+// 16 tokens, the second halves go where the other eight would be, at no cost.
+//
+// 1 token 1280 x 5120: 8.4 and 7.5 us, 39 MB; other splits of the contraction
+// and of the outputs (16 wavefronts, 16 or 32 outputs, 4 to 20 k-steps in
+// flight) were within 5 % of it at 640 x 2560, 1280 x 5120 and 2048 x 5504.
 
 #include "eight_bit.h"
 #include "feed_forward.h"
@@ -38,8 +46,12 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
         w[i] = p.w + (int64_t)(n0 + 16 * (i & 1) + (i >= 2 ? p.N : 0) + lr) * p.ldw + 8 * lq;
-    const bool there = lr < p.M;
-    const bf16* x = p.x + (int64_t)(there ? lr : 0) * p.ldx + 8 * lq;
+    // FF_STORE of at most eight tokens: lanes 8 .. 15 take the second halves of
+    // the sums that X's values are, [2][M][K].
+    const bool two = EPI != FF_GATE && p.M <= FF_SPLIT_ROWS;
+    const int row = two ? lr & 7 : lr;
+    const bool there = row < p.M;
+    const bf16* x = p.x + (int64_t)(there ? row + (two && lr >= 8 ? p.M : 0) : 0) * p.ldx + 8 * lq;
     f32x4 acc[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -65,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
             for (int i = 0; i < NB; ++i) acc[i] = mfma16(wv[u][i], xv[u], acc[i]);
     }
 
-    // acc[i][e]: W row 16 i + 4 lq + e, token lr
+    // acc[i][e]: W row 16 i + 4 lq + e, token (or half of its sum) lr
 #pragma unroll
     for (int i = 0; i < NB; ++i) sums[wave][i][lane] = acc[i];
     __syncthreads();
@@ -73,7 +85,10 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
     auto total = [&](int i, int row) {  // of row `row` of block i, the wavefronts in their order
         float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) t += sums[k][i][16 * (row >> 2) + m][row & 3];
+        for (int k = 0; k < kWaves; ++k) {
+            t += sums[k][i][16 * (row >> 2) + m][row & 3];
+            if (two) t += sums[k][i][16 * (row >> 2) + 8 + (m & 7)][row & 3];
+        }
         return t;
     };
     if (m >= 16 || m >= p.M) return;  // a group's 32 lanes together
@@ -96,7 +111,11 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
                 if (n == 0) p.scales[(at + h * p.N) / EIGHT_GROUP] = (uint8_t)scale;
             }
         }
-        p.out[(int64_t)m * p.N + n0 + n] = f32_to_bf16(v * ff_act<ACT>(g));
+        const float h = v * ff_act<ACT>(g);
+        const bf16 high = f32_to_bf16(h);
+        bf16* out = p.out + (int64_t)m * p.N + n0 + n;
+        out[0] = high;
+        if (p.M <= FF_SPLIT_ROWS) out[(int64_t)p.M * p.N] = f32_to_bf16(h - bf16_to_f32(high));
     } else {
         float v = total(0, n);
         if (p.bias != nullptr) v += bf16_to_f32(p.bias[n0 + n]);

@@ -119,6 +119,7 @@ class pcpp_step_params_t(ctypes.Structure):
 
 PCPP_ACT_GELU = 0
 PCPP_ACT_SILU = 1
+PCPP_FF_UP, PCPP_FF_DOWN, PCPP_FF_GATE_GRAD, PCPP_FF_W1_GRAD, PCPP_FF_W2_GRAD, PCPP_FF_X_GRAD = range(6)
 
 
 class pcpp_ff_geom_t(ctypes.Structure):
@@ -195,6 +196,7 @@ def _load():
         "pcpp_rms_norm_backward_workspace_size": (sz, [ctypes.c_int64, i32]),
         "pcpp_rms_norm_backward": (ctypes.c_int, [ctypes.c_int64, i32, ctypes.c_float, i32] + [vp] * 7 + [sz, vp]),
         "pcpp_gated_ff_workspace_size": (sz, [fp]),
+        "pcpp_gated_ff_plan": (ctypes.c_int, [fp, i32, i32, i32p, i32p, i32p]),
         "pcpp_gated_ff": (ctypes.c_int, [fp, fwp] + [vp] * 5 + [sz, vp]),
         "pcpp_gated_ff_backward_workspace_size": (sz, [fp]),
         "pcpp_gated_ff_backward": (ctypes.c_int, [fp, fwp] + [vp] * 6 + [ctypes.POINTER(pcpp_ff_grads_t), vp, sz, vp]),
@@ -220,7 +222,7 @@ EXPORTED = (
     "pcpp_transformer_module_workspace_size", "pcpp_transformer_module",
     "pcpp_concat_channels", "pcpp_layer_norm", "pcpp_group_norm_workspace_size", "pcpp_group_norm",
     "pcpp_checkpoint_save", "pcpp_checkpoint_load", "pcpp_rms_norm", "pcpp_rms_norm_backward_workspace_size",
-    "pcpp_rms_norm_backward", "pcpp_gated_ff_workspace_size", "pcpp_gated_ff",
+    "pcpp_rms_norm_backward", "pcpp_gated_ff_workspace_size", "pcpp_gated_ff_plan", "pcpp_gated_ff",
     "pcpp_gated_ff_backward_workspace_size", "pcpp_gated_ff_backward",
 )
 
@@ -563,6 +565,16 @@ def make_ff_grads(tensors: dict) -> pcpp_ff_grads_t:
 
 def pcpp_gated_ff_workspace_size(g) -> int:
     return _lib.pcpp_gated_ff_workspace_size(ctypes.byref(g))
+
+
+def pcpp_gated_ff_plan(g, which, cus=0):
+    """(rows, outputs, pieces of the contraction) of the tiles of one of the
+    block's products, PCPP_FF_*, on a device of `cus` compute units or (0) on
+    the current device."""
+    bm, bn, k = (ctypes.c_int32() for _ in range(3))
+    _check("pcpp_gated_ff_plan", _lib.pcpp_gated_ff_plan(ctypes.byref(g), which, cus, ctypes.byref(bm), ctypes.byref(bn),
+                                                          ctypes.byref(k)))
+    return bm.value, bn.value, k.value
 
 
 def pcpp_gated_ff(g, w, x, y, pre_codes, pre_scales, workspace, ws_bytes, stream=None):

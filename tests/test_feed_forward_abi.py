@@ -152,3 +152,38 @@ def test_workspace_sizes():
     assert pcpp.pcpp_rms_norm_backward_workspace_size(100, 640) >= 640 * 4
     assert pcpp.pcpp_rms_norm_backward_workspace_size(0, 640) == 0
     assert pcpp.pcpp_rms_norm_backward_workspace_size(100, 12) == 0
+
+
+def test_plan():
+    """Few tokens straight from memory, few tiles in pieces, many on the largest
+    tiles; a plan's queries never need more workspace than the size says."""
+    from paper_2412_02962_amd import pcpp
+    plan = lambda M, C, F, which: pcpp.pcpp_gated_ff_plan(pcpp.make_ff_geom(M, C, F), which, cus=256)
+    assert plan(1, 640, 2560, pcpp.PCPP_FF_UP) == (16, 32, 1)
+    assert plan(16, 640, 2560, pcpp.PCPP_FF_DOWN) == (16, 16, 1)
+    rows, outputs, pieces = plan(77, 1280, 5120, pcpp.PCPP_FF_DOWN)
+    assert rows == 64 and pieces > 1
+    assert plan(77, 1280, 5120, pcpp.PCPP_FF_UP)[2] == 1
+    assert plan(32768, 1280, 5120, pcpp.PCPP_FF_UP)[0] == 128
+    for which in (pcpp.PCPP_FF_W1_GRAD, pcpp.PCPP_FF_W2_GRAD, pcpp.PCPP_FF_X_GRAD):
+        assert plan(16384, 1280, 5120, which) == (256, 256, 1)
+    assert plan(77, 1280, 5120, pcpp.PCPP_FF_X_GRAD)[2] > plan(77, 1280, 5120, pcpp.PCPP_FF_W1_GRAD)[2] == 1
+    for M in (17, 77, 300, 2093):
+        for C, F in ((64, 8192), (640, 2560), (1280, 5120)):
+            g = pcpp.make_ff_geom(M, C, F)
+            pieces = pcpp.pcpp_gated_ff_plan(g, pcpp.PCPP_FF_DOWN, cus=256)[2]
+            sums = 4 * M * C * pieces if pieces > 1 else 0
+            assert pcpp.pcpp_gated_ff_workspace_size(g) >= 2 * M * F + sums
+            need = 6 * M * F + 2 * M * C
+            for which, size in ((pcpp.PCPP_FF_W1_GRAD, 2 * F * C), (pcpp.PCPP_FF_W2_GRAD, C * F), (pcpp.PCPP_FF_X_GRAD, M * C)):
+                pieces = pcpp.pcpp_gated_ff_plan(g, which, cus=256)[2]
+                need += 4 * size * pieces if pieces > 1 else 0
+            assert pcpp.pcpp_gated_ff_backward_workspace_size(g) >= need
+
+
+@pytest.mark.parametrize("which,cus", [(-1, 256), (6, 256), (0, -1)])
+def test_plan_refusals(which, cus):
+    from paper_2412_02962_amd import pcpp
+    with pytest.raises(pcpp.PcppError) as e:
+        pcpp.pcpp_gated_ff_plan(pcpp.make_ff_geom(70, 128, 192), which, cus=cus)
+    assert e.value.status == pcpp.PCPP_EINVAL

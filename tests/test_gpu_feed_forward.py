@@ -127,6 +127,34 @@ def test_backward(M, C, F, kind):
             _check(got, want[k], bound[k], f"{k} {'8-bit x' if eight else ''}")
 
 
+@pytest.mark.parametrize("M,C,F,tiles", [
+    (2570, 1280, 2560, (128, 256)),    # the gate's and its gradient's wide tiles, ragged rows
+    (5000, 1344, 2624, (128, 128)),    # and widths that no tile divides
+])
+def test_wide_tiles(M, C, F, tiles):
+    """Sizes whose products run on the wide tiles, forward and backward; the
+    reference in float64 on the GPU."""
+    from paper_2412_02962_amd import pcpp
+    _say("wide tiles", M, C, F)
+    kind = "gelu"
+    x, w, dy = _inputs(M, C, F, 71)
+    c = Call(M, C, F, kind, _dev(w))
+    got = [pcpp.pcpp_gated_ff_plan(c.g, k)[0] for k in (pcpp.PCPP_FF_UP, pcpp.PCPP_FF_GATE_GRAD, pcpp.PCPP_FF_X_GRAD)]
+    assert got[0] == got[1] == tiles[0] and got[2] == tiles[1], got
+    c.forward(x.to(DEV))
+    torch.cuda.synchronize()
+    x64, w64, dy64 = x.to(DEV, F64), _f64(c.wd), dy.to(DEV, F64)
+    _check(c.y, ref.gated_ff(x64, w64, kind)[2].cpu(), ref.gated_ff_bound(x64, w64, kind).cpu(), "y")
+    kept = ref.from_8bit(c.codes.cpu(), c.scales.cpu())
+    _check(kept, ref.gated_ff(x64, w64, kind)[0].cpu(), ref.pre_bound(x64, w64).cpu(), "value and gate in 8 bits")
+    c.backward(x.to(DEV), dy.to(DEV))
+    torch.cuda.synchronize()
+    want = ref.gated_ff_backward(x64, w64, kept.to(DEV), dy64, kind)
+    bound = ref.gated_ff_backward_bound(x64, w64, kept.to(DEV), dy64, kind)
+    for k, t in dict(dx=c.dx, **c.grads).items():
+        _check(t, want[k].cpu(), bound[k].cpu(), k)
+
+
 def test_no_biases():
     _say("no biases")
     M, C, F = 70, 128, 192
