@@ -37,12 +37,17 @@ __device__ __forceinline__ void dma16(u32x4 buffer, uint32_t voff, uint32_t lds)
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(buffer), "{m0}"(lds) : "memory");
 }
 
-// Buffer descriptor of `bytes` at p (both wave-uniform).
+// Buffer descriptor of `bytes` at p (both wave-uniform).  A scalar register that
+// a vector instruction (readfirstlane) wrote may be read by a memory
+// instruction only five wait states later.  The compiler keeps to that for
+// instructions it knows, not for dma16's, so the wait is here.
 __device__ __forceinline__ u32x4 buffer_of(const char* p, uint32_t bytes) {
     const uint64_t a = (uint64_t)(uintptr_t)p;
-    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
-                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xffffu,
-                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+    u32x4 b = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xffffu,
+               (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+    asm volatile("s_nop 4" : "+s"(b));
+    return b;
 }
 
 // Where the k-tiles of an operand's rows are read from: what lies past the
