@@ -37,17 +37,21 @@ __device__ __forceinline__ void dma16(u32x4 buffer, uint32_t voff, uint32_t lds)
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(buffer), "{m0}"(lds) : "memory");
 }
 
-// Buffer descriptor of `bytes` at p (both wave-uniform).  A scalar register that
-// a vector instruction (readfirstlane) wrote may be read by a memory
-// instruction only five wait states later.  The compiler keeps to that for
-// instructions it knows, not for dma16's, so the wait is here.
+// v in a scalar register that a scalar instruction wrote.  A memory instruction
+// may read one that a vector instruction wrote (readfirstlane) only five wait
+// states later; the compiler keeps to that for instructions it knows, not for
+// dma16's, whose buffers' words therefore all pass through here.  (Waiting the
+// five states instead: 1 % more time at 32768 x 1280 x 5120.)
+__device__ __forceinline__ uint32_t scalar(uint32_t v) {
+    uint32_t s;
+    asm("s_mov_b32 %0, %1" : "=s"(s) : "s"(__builtin_amdgcn_readfirstlane(v)));
+    return s;
+}
+
+// Buffer descriptor of `bytes` at p (both wave-uniform).
 __device__ __forceinline__ u32x4 buffer_of(const char* p, uint32_t bytes) {
     const uint64_t a = (uint64_t)(uintptr_t)p;
-    u32x4 b = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
-               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xffffu,
-               (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
-    asm volatile("s_nop 4" : "+s"(b));
-    return b;
+    return u32x4{scalar((uint32_t)a), scalar((uint32_t)(a >> 32) & 0xffffu), scalar(bytes), 0x00020000u};
 }
 
 // Where the k-tiles of an operand's rows are read from: what lies past the
