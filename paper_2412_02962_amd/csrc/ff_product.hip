@@ -18,11 +18,15 @@ constexpr int KT = 64;  // contraction per tile
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
 
-// The kinds of tile: their rows of X and W, ring in LDS, and how many of their
-// workgroups share a compute unit.
+// The kinds of tile: their rows of X and W (wider with an epilogue that halves
+// the outputs or whose operations cover the wait for operands), ring in LDS, and
+// how many of their workgroups share a compute unit.
 enum { TILE_64, TILE_128, TILE_256, TILE_KINDS };
-constexpr int rows_x(int kind) { return 64 << kind; }
-constexpr int rows_w(int kind) { return kind == TILE_64 ? 128 : 256; }
+constexpr int rows_x(int kind) { return kind == TILE_64 ? 64 : kind == TILE_128 ? 128 : 256; }
+constexpr int rows_w(int kind, int epilogue) {
+    return kind == TILE_64 || (kind == TILE_128 && epilogue == FF_STORE) ? 128 : 256;
+}
+constexpr int outputs_of(int kind, int epilogue) { return rows_w(kind, epilogue) / (epilogue == FF_GATE ? 2 : 1); }
 constexpr int lds_bytes(int kind) { return (kind == TILE_64 ? 72 : kind == TILE_128 ? 80 : 128) * 1024; }
 constexpr int per_cu(int kind) { return kind == TILE_256 ? 1 : 2; }
 
@@ -196,9 +200,9 @@ __device__ __forceinline__ Item item_of(const FfProduct& p, int item) {
 // rows, two along W's.
 template <int KIND, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
-                                           f32x16 (&acc)[rows_w(KIND) / 64][rows_x(KIND) / 64], char* lds) {
+                                           f32x16 (&acc)[rows_w(KIND, EPI) / 64][rows_x(KIND) / 64], char* lds) {
     const int m0 = it.m0, n0 = it.n0;
-    constexpr int TM = rows_x(KIND) / 2, TN = rows_w(KIND) / 2;  // of a wavefront
+    constexpr int TM = rows_x(KIND) / 2, TN = rows_w(KIND, EPI) / 2;  // of a wavefront
     constexpr int NB = TN / 32;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -339,7 +343,7 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     typedef Layout<128, WT> LW;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
-    const Item it = item_of<64, EPI == FF_GATE ? 64 : 128>(p, item);
+    const Item it = item_of<64, outputs_of(TILE_64, EPI)>(p, item);
 
     Source<XT> x;
     Source<WT> w;
@@ -413,26 +417,28 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     store_tile<TILE_64, XT, WT, EPI, ACT>(p, it, acc, lds);
 }
 
-// A 128 x 256 tile, two workgroups to a compute unit: while one waits at a
-// barrier or for LDS, or is in its epilogue (an exponential, a reciprocal and
-// some 20 operations an output, and up to 8 bytes of memory traffic), the
-// other's products run.  Four wavefronts of 64 x 128, two per SIMD.
+// A 128 x 256 tile (FF_STORE: 128 x 128), two workgroups to a compute unit: while one
+// waits at a barrier or for LDS, or is in its epilogue (an exponential, a
+// reciprocal and some 20 operations an output, and up to 8 bytes of memory
+// traffic), the other's products run.  Four wavefronts of 64 x 128 (64 x 64),
+// two per SIMD.
 //
 // A loop over whole k-tiles in two stages waits for the next one: its bytes
 // take as long to arrive as its products take, and the latency comes on top.
-// So the ring holds ten units of 8 KB, a k-tile being six in the order W0 X0
-// X1 W1 W2 W3, and a phase is the products of one of the four W units with
-// both of X.  Phase 3 reads the next k-tile's W0 and X0 into registers, phase
+// So the ring holds ten units of 8 KB, a k-tile being six (four) in the order
+// W0 X0 X1 W1 .., and a phase is the products of one of the W units with both
+// of X.  The last phase reads the next k-tile's W0 and X0 into registers, phase
 // 0 X1 (used by its second half) and W1, the others one W unit each; a phase
-// loads into the slots that the phase before the last has read.  Five units of
-// a workgroup are always in flight.
+// loads into the slots that the phase before the last has read.  Four to six
+// units of a workgroup are always in flight.
 template <bool XT, bool WT, int EPI, int ACT>
-__device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int item, char* lds) {
-    constexpr int BNO = EPI == FF_GATE ? 128 : 256;  // outputs of a tile
+__device__ __forceinline__ void product_tile_128(const FfProduct& p, int item, char* lds) {
+    constexpr int TN = rows_w(TILE_128, EPI) / 2;          // W rows of a wavefront
+    constexpr int NW = TN / 32, UNITS = NW + 2;            // W units, units of a k-tile
     constexpr uint32_t UNIT = 64 * KT * 2, RING = 10 * UNIT;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
-    const Item it = item_of<128, BNO>(p, item);
+    const Item it = item_of<128, outputs_of(TILE_128, EPI)>(p, item);
 
     // Unit i has block i of both wavefronts along the rows; FF_GATE's W: 32
     // outputs' values for even i, their gates for odd.
@@ -448,13 +454,13 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
         xoff[q] = LX::offset(q, wave, p.ldx,
                              [](int r) { return (int64_t)(block_row<XT>(0, r >> 5, 64) + (r & 31)); });
         woff[q] = LW::offset(q, wave, p.ldw, [](int r) {
-            return (int64_t)(block_row<WT>(0, r >> 5, EPI == FF_GATE ? 64 : 128) + (r & 31));
+            return (int64_t)(block_row<WT>(0, r >> 5, EPI == FF_GATE ? TN / 2 : TN) + (r & 31));
         });
     }
     const uint32_t x_off = XT ? 128 : (uint32_t)(64 * p.ldx);
-    uint32_t w_off[4];
+    uint32_t w_off[NW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NW; ++i)
         w_off[i] = EPI == FF_GATE ? (uint32_t)((32 * (i >> 1) + (i & 1 ? (int64_t)p.N : 0)) * p.ldw * 2)
                    : WT           ? 128 * i
                                   : (uint32_t)(64 * i * p.ldw);
@@ -462,9 +468,9 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     const View<64, XT> xv(lds0, 32 * wm);
     const View<64, WT> wv(lds0, 32 * wn);
 
-    f32x16 acc[4][2];
+    f32x16 acc[NW][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NW; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -483,20 +489,21 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     };
     auto loaded = [&](int u) {
         if (u == 2) x.advance();
-        if (u == 5) w.advance();
+        if (u == UNITS - 1) w.advance();
         wr = wr + UNIT == RING ? 0 : wr + UNIT;
     };
     auto step_read = [&]() { rd = rd + UNIT == RING ? 0 : rd + UNIT; };
 
+    constexpr int AHEAD = NW == 4 ? 9 : 8;  // units loaded before the first phase
 #pragma unroll
-    for (int u = 0; u < 9; ++u) {
-        const u32x4 b = buffer_of_unit(u % 6);
-        load(u % 6, 0, b);
-        load(u % 6, 1, b);
-        loaded(u % 6);
+    for (int u = 0; u < AHEAD; ++u) {
+        const u32x4 b = buffer_of_unit(u % UNITS);
+        load(u % UNITS, 0, b);
+        load(u % UNITS, 1, b);
+        loaded(u % UNITS);
     }
     Frag wa, wb, xa, xb, xc;
-    asm volatile("s_waitcnt vmcnt(14)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * (AHEAD - 2)) : "memory");
 #pragma unroll
     for (int s = 0; s < 4; ++s) wa.v[s] = wv.read(rd, s, 0);
     step_read();
@@ -505,17 +512,21 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     step_read();
 
     // Phase i: products of wc with x0 and x1; the reads and loads listed above.
-    // Before it, this wavefront's part of the units to read has landed (five or
+    // Before it, this wavefront's part of the units to read has landed (four to
     // six younger units, two loads each, may be in flight) and it has read
     // those of two phases ago (the phase before read two units, or one, of at
     // least four reads each); then everyone's.
     auto phase = [&](int i, const Frag& wc, Frag& wnext, const Frag& x0, Frag& x1, Frag& x0next) {
-        if (i < 2)
+        if (NW == 2)
+            asm volatile("s_waitcnt vmcnt(8) lgkmcnt(8)\n\ts_barrier" ::: "memory");
+        else if (i < 2)
             asm volatile("s_waitcnt vmcnt(10) lgkmcnt(8)\n\ts_barrier" ::: "memory");
         else
             asm volatile("s_waitcnt vmcnt(12) lgkmcnt(4)\n\ts_barrier" ::: "memory");
-        // the units to load: W1 | W2 W3 | W0 X0 of the tile after the next | X1
-        const int u0 = i == 0 ? 3 : i == 1 ? 4 : i == 2 ? 0 : 2, nu = i == 1 || i == 2 ? 2 : 1;
+        // the units to load: W1 | W2 W3 | W0 X0 of the k-tile after the next |
+        // X1; of four units W0 X0 | X1 W1, both of the k-tile after the next
+        const int u0 = NW == 2 ? 2 * i : i == 0 ? 3 : i == 1 ? 4 : i == 2 ? 0 : 2;
+        const int nu = NW == 2 || i == 1 || i == 2 ? 2 : 1;
         u32x4 b = buffer_of_unit(u0);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -535,7 +546,7 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
             } else if (k < 4) {
                 wnext.v[k] = wv.read(rd, k, 0);
                 if (k == 3) step_read();
-            } else if (i == 3) {
+            } else if (i == NW - 1) {
                 x0next.v[k - 4] = xv.read(rd, k - 4, 0);
                 if (k == 7) step_read();
             }
@@ -557,14 +568,16 @@ __device__ __forceinline__ void product_tile_128x256(const FfProduct& p, int ite
     else
         __builtin_amdgcn_s_setprio(1);
     for (int t = 0; t < it.count; t += 2) {  // an odd last k-tile runs with one of zeros
-        phase(0, wa, wb, xa, xb, xc);
-        phase(1, wb, wa, xa, xb, xc);
-        phase(2, wa, wb, xa, xb, xc);
-        phase(3, wb, wa, xa, xb, xc);
-        phase(0, wa, wb, xc, xb, xa);
-        phase(1, wb, wa, xc, xb, xa);
-        phase(2, wa, wb, xc, xb, xa);
-        phase(3, wb, wa, xc, xb, xa);
+#pragma unroll
+        for (int i = 0; i < NW; i += 2) {
+            phase(i, wa, wb, xa, xb, xc);
+            phase(i + 1, wb, wa, xa, xb, xc);
+        }
+#pragma unroll
+        for (int i = 0; i < NW; i += 2) {
+            phase(i, wa, wb, xc, xb, xa);
+            phase(i + 1, wb, wa, xc, xb, xa);
+        }
     }
     __builtin_amdgcn_s_setprio(0);
     // Loads past the end are still on their way (zeros) to the slots.
@@ -697,7 +710,7 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int item, char*
     if constexpr (KIND == TILE_256)
         product_tile_256x256<XT, WT>(p, item, lds);
     else if constexpr (KIND == TILE_128)
-        product_tile_128x256<XT, WT, EPI, ACT>(p, item, lds);
+        product_tile_128<XT, WT, EPI, ACT>(p, item, lds);
     else
         product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
 }
@@ -767,7 +780,7 @@ __global__ __launch_bounds__(256) void ff_sum_pieces(FfSums a) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int64_t tiles_of(const FfProduct& p, int kind) {
-    return ceil_div(p.M, rows_x(kind)) * ceil_div(p.N, p.epilogue == FF_GATE ? rows_w(kind) / 2 : rows_w(kind));
+    return ceil_div(p.M, rows_x(kind)) * ceil_div(p.N, outputs_of(kind, p.epilogue));
 }
 
 // Most pieces of a contraction, and most floats of all pieces' sums of a launch.
@@ -783,28 +796,41 @@ int64_t pieces_of(const FfProduct& p, int64_t run) {
 // Time in us of n products on a kind of tile, their contractions in runs
 // of about `run` k-tiles; floats: the pieces' sums.  Per k-tile and per item
 // (its start and epilogue), alone on a compute unit and when all of them have
-// all the workgroups that fit, as measured (300 to 16385 tokens at 640 x 2560
-// and 1280 x 5120).
+// all the workgroups that fit; by epilogue.  FF_STORE's, and the pieces' cost,
+// are those whose choices came out fastest over the kinds and cuts measured for
+// 39 sizes (77 to 16385 tokens, 320 x 1280 to 2048 x 8192): the choices are
+// within 2 % of the best ones in the mean, within 12 % each.  kSlower: what
+// many k-tiles add to a k-tile's time, by lower clocks at the power limit.
 struct TileCost {
-    double tile, item[3];  // item: by epilogue
+    double tile, item;
 };
-constexpr TileCost kAlone[TILE_KINDS] = {{0.31, {5, 6.5, 10}}, {0.72, {7, 12, 18}}, {1.08, {8}}};
-constexpr TileCost kFull[TILE_KINDS] = {{0.40, {1.5, 2, 4.3}}, {0.95, {4, 6, 18}}, {1.45, {8}}};
+constexpr TileCost kAlone[3][TILE_KINDS] = {{{0.307, 4.06}, {0.67, 4.24}, {1.55, 8.25}},
+                                            {{0.31, 6.5}, {0.72, 12}},
+                                            {{0.31, 10}, {0.72, 18}}};
+constexpr TileCost kFull[3][TILE_KINDS] = {{{0.391, 1.74}, {0.548, 1.40}, {0.826, 10.8}},
+                                           {{0.40, 2}, {0.95, 6}},
+                                           {{0.40, 4.3}, {0.95, 18}}};
+constexpr double kSlower[TILE_KINDS] = {0.067, 0.186, 0.412};
+constexpr double kManyOutputs = 150.0 * 128 * 128;  // outputs x k-tiles of a compute unit
 double estimate(const FfProduct* p, int n, int kind, int64_t run, int cus, int64_t& floats) {
-    double work = 0, longest = 0;
+    double work = 0, longest = 0, k_tiles = 0;
     int64_t items = 0;
     floats = 0;
+    for (int i = 0; i < n; ++i) k_tiles += (double)ceil_div(p[i].K, KT) * tiles_of(p[i], kind);
+    const double load = k_tiles * rows_x(kind) * rows_w(kind, p[0].epilogue) / cus / kManyOutputs;
+    const double slower = p[0].epilogue == FF_STORE ? 1 + kSlower[kind] * (load < 1 ? load : 1) : 1;
     for (int i = 0; i < n; ++i) {
         const int64_t nkt = ceil_div(p[i].K, KT), pieces = pieces_of(p[i], run), t = tiles_of(p[i], kind) * pieces;
         const double len = (double)nkt / pieces;
-        const double alone = len * kAlone[kind].tile + kAlone[kind].item[p[i].epilogue];
+        const TileCost &one = kAlone[p[i].epilogue][kind], &full = kFull[p[i].epilogue][kind];
+        const double alone = len * one.tile + one.item;
         items += t;
-        work += t * (len * kFull[kind].tile + kFull[kind].item[p[i].epilogue]);
+        work += t * (len * full.tile * slower + full.item);
         if (alone > longest) longest = alone;
         if (pieces > 1) floats += pieces * p[i].M * p[i].N;
     }
     const double busiest = work / items * ceil_div(items, cus);  // of the compute units
-    return (busiest > longest ? busiest : longest) + (floats > 0 ? 5.0 + 8.0 * floats / 3.5e6 : 0);
+    return (busiest > longest ? busiest : longest) + (floats > 0 ? 5.2 + 2.96e-6 * floats : 0);
 }
 
 int cus_here() {
@@ -913,7 +939,7 @@ void ff_plan(FfProduct* p, int n, int cus, int32_t* tile_rows, int32_t* tile_out
     }
     const int kind = plan(p, n, cus > 0 ? cus : cus_here());
     *tile_rows = rows_x(kind);
-    *tile_outputs = p[0].epilogue == FF_GATE ? rows_w(kind) / 2 : rows_w(kind);
+    *tile_outputs = outputs_of(kind, p[0].epilogue);
 }
 
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {

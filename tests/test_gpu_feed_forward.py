@@ -129,7 +129,9 @@ def test_backward(M, C, F, kind):
 
 @pytest.mark.parametrize("M,C,F,tiles", [
     (2570, 1280, 2560, (128, 256)),    # the gate's and its gradient's wide tiles, ragged rows
-    (5000, 1344, 2624, (128, 128)),    # and widths that no tile divides
+    (5000, 1344, 2624, (128, 256)),    # and widths that no tile divides
+    (4100, 448, 1472, (128, 128)),     # the gradients' square tiles
+    (2570, 192, 2368, (128, 128)),     # and in pieces of the contraction
 ])
 def test_wide_tiles(M, C, F, tiles):
     """Sizes whose products run on the wide tiles, forward and backward; the
