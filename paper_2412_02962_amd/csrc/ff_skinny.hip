@@ -116,7 +116,10 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
         const bf16 high = f32_to_bf16(h);
         bf16* out = p.out + (int64_t)m * p.N + n0 + n;
         out[0] = high;
-        if (p.M <= FF_SPLIT_ROWS) out[(int64_t)p.M * p.N] = f32_to_bf16(h - bf16_to_f32(high));
+        if (p.M <= FF_SPLIT_ROWS) {  // nothing is left of what is infinite in bf16
+            const float top = bf16_to_f32(high);
+            out[(int64_t)p.M * p.N] = f32_to_bf16(fabsf(top) < INFINITY ? h - top : 0.f);
+        }
     } else {
         float v = total(0, n);
         if (p.bias != nullptr) v += bf16_to_f32(p.bias[n0 + n]);
