@@ -164,8 +164,9 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward(RmsBackwardParams 
             }
         }
         const float rstd = 1.f / sqrtf(row_sum<WPR>(sq, lds) / (float)p.C + p.eps);
-        // rstd (w - n mean(w n)) = rstd w - k s
-        const float k = rstd * rstd * rstd * (row_sum<WPR>(dot, lds) / (float)p.C);
+        // rstd (w - n mean(w n)) = rstd w - k n (not by rstd^3, which overflows for
+        // rows below 10^-13 where eps lets them)
+        const float k = rstd * (row_sum<WPR>(dot, lds) / (float)p.C) * rstd;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int c = c0 + 512 * WPR * j;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward(RmsBackwardParams 
             for (int e = 0; e < 8; ++e) {
                 const float dr = d[j][e] * rstd;
                 dg[j][e] = __builtin_fmaf(dr, s[j][e], dg[j][e]);
-                o[e] += __builtin_fmaf(dr, g[e], -k * s[j][e]);
+                o[e] += __builtin_fmaf(dr, g[e], -k * (s[j][e] * rstd));
             }
             store8((T*)p.ds + at + c, o);
         }
