@@ -842,7 +842,8 @@ int pcpp_gated_ff(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w,
  * diagnostics and tests), the weights' gradients and dx as one launch has all
  * three of them; cus > 0: a device of `cus` compute units, 0: the current one
  * (PCPP_EHIP if it cannot be queried).  Outputs (any may be NULL): rows and
- * outputs of a workgroup's tile and the pieces the contraction is worked in.
+ * outputs of a workgroup's tile and the pieces the contraction is worked in
+ * (PCPP_FF_UP: without the checkpoint).
  */
 #define PCPP_FF_UP        0   /* x ff1_w^T                                   */
 #define PCPP_FF_DOWN      1   /* h ff2_w^T                                   */

@@ -45,7 +45,8 @@ int ff_partial_rows(const FfProduct& p);  // of a product's sizes and epilogue
 // [2][M][F], two bf16 whose sum is h.
 constexpr int FF_SPLIT_ROWS = 8;
 constexpr int FF_SKINNY_ROWS = 16;
-hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s);
+hipError_t launch_ff_skinny(const FfProduct& p, int cus, hipStream_t s);
+int ff_skinny_outputs(const FfProduct& p, int cus);  // of a workgroup
 // A product with X along the contraction (W across it for FF_GATE_GRAD alone),
 // and up to three of FF_STORE with w_t = 1 in one launch (which also does
 // `sums`).  part: ff_part_floats of the same products, or of these and others.

@@ -942,19 +942,20 @@ int64_t ff_part_floats(const FfProduct* p, int n) {
 }
 
 void ff_plan(FfProduct* p, int n, int cus, int32_t* tile_rows, int32_t* tile_outputs) {
+    if (cus <= 0) cus = cus_here();
     if (skinny(p[0])) {
         p[0].pieces = 1;
         *tile_rows = FF_SKINNY_ROWS;
-        *tile_outputs = p[0].epilogue == FF_GATE ? 32 : 16;
+        *tile_outputs = ff_skinny_outputs(p[0], cus);
         return;
     }
-    const int kind = plan(p, n, cus > 0 ? cus : cus_here());
+    const int kind = plan(p, n, cus);
     *tile_rows = rows_x(kind);
     *tile_outputs = outputs_of(kind, p[0].epilogue);
 }
 
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
-    if (skinny(p)) return launch_ff_skinny(p, s);
+    if (skinny(p)) return launch_ff_skinny(p, cus_here(), s);
     const int kind = plan(&p, 1, cus_here());
     place_parts(&p, 1, part);
     if (kind == TILE_256)

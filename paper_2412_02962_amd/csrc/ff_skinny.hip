@@ -7,16 +7,21 @@
 // values and gates, or 16 outputs) and its eight wavefronts an eighth of the
 // contraction each; W goes straight from memory into the MFMA's operand
 // registers, a run of k-steps in flight at a time, as does X, which the L2
-// holds.  The wavefronts' sums meet in LDS.
+// holds.  The wavefronts' sums meet in LDS.  A compute unit takes in some 40
+// bytes a cycle, so that half as many outputs go to a workgroup as long as each
+// still has a compute unit to itself (FF_GATE, without the checkpoint, whose
+// groups are 32 outputs: 16; FF_STORE: 8, half the matrix unit's rows).  1 token:
+// 640 x 2560 11.9 -> 10.5 us, 1280 x 5120 16.9 -> 15.0; with more workgroups than
+// compute units it is the other way, 4096 x 8192 58 -> 61.
 //
 // Between the two products of up to eight tokens, h's values are sums of two
 // bf16, 16 significant bits, so that y is rounded once: the matrix unit takes
 // 16 tokens, the second halves go where the other eight would be, at no cost.
 //
-// 1 token 1280 x 5120: 8.3 and 8.7 us, 26 and 13 MB, where a launch alone is
-// about 5 and the bytes take 5.0 and 2.5; other splits of the contraction and of
-// the outputs (16 wavefronts, 16 or 32 outputs, 4 to 20 k-steps in flight) were
-// within 5 % of it at 640 x 2560, 1280 x 5120 and 2048 x 5504.
+// 1 token 1280 x 5120: 8.3 and 6.0 to 7.0 us, 26 and 13 MB, where a launch alone is
+// about 5 and the bytes take 5.0 and 2.5; other splits of the contraction (16
+// wavefronts, 4 to 20 k-steps in flight) were within 5 % of it at 640 x 2560,
+// 1280 x 5120 and 2048 x 5504.
 
 #include "eight_bit.h"
 #include "feed_forward.h"
@@ -32,11 +37,10 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// FF_GATE: 32 outputs, W rows n0 .. + 31 and N further on; FF_STORE: 16 outputs.
-template <int EPI, int ACT>
+// BNO outputs: W rows n0 .. and, FF_GATE, N further on.
+template <int EPI, int ACT, int BNO>
 __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
-    constexpr int NB = EPI == FF_GATE ? 4 : 1;             // blocks of 16 W rows
-    constexpr int BNO = EPI == FF_GATE ? 32 : 16;
+    constexpr int NV = (BNO + 15) / 16, NB = EPI == FF_GATE ? 2 * NV : NV;  // blocks of 16 W rows: values, gates
     constexpr int U = 8;  // k-steps in flight
     __shared__ f32x4 sums[kWaves][NB][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -46,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
     const bf16* w[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
-        w[i] = p.w + (int64_t)(n0 + 16 * (i & 1) + (i >= 2 ? p.N : 0) + lr) * p.ldw + 8 * lq;
+        w[i] = p.w + (int64_t)(n0 + 16 * (i % NV) + (i >= NV ? p.N : 0) + lr % BNO) * p.ldw + 8 * lq;
     // FF_STORE of at most eight tokens: lanes 8 .. 15 take the second halves of
     // the sums that X's values are, [2][M][K].
     const bool two = EPI != FF_GATE && p.M <= FF_SPLIT_ROWS;
@@ -67,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 wv[u][i] = bf16x8{};
-                if (in) wv[u][i] = *(const bf16x8*)(w[i] + 32 * (s + u));
+                if (in && lr < BNO) wv[u][i] = *(const bf16x8*)(w[i] + 32 * (s + u));
             }
             xv[u] = bf16x8{};
             if (in && there) xv[u] = *(const bf16x8*)(x + 32 * (s + u));
@@ -92,14 +96,14 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
         }
         return t;
     };
-    if (m >= 16 || m >= p.M) return;  // a group's 32 lanes together
+    if (m >= 16 || m >= p.M) return;  // a group's 32 lanes together (BNO = 32)
     if constexpr (EPI == FF_GATE) {
-        float v = total(n >> 4, n & 15), g = total(2 + (n >> 4), n & 15);
+        float v = total(n >> 4, n & 15), g = total(NV + (n >> 4), n & 15);
         if (p.bias != nullptr) {
             v += bf16_to_f32(p.bias[n0 + n]);
             g += bf16_to_f32(p.bias[p.N + n0 + n]);
         }
-        if (p.codes != nullptr) {
+        if (BNO == EIGHT_GROUP && p.codes != nullptr) {
             const int64_t at = (int64_t)m * 2 * p.N + n0 + n;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -129,13 +133,21 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
 
 }  // namespace
 
-hipError_t launch_ff_skinny(const FfProduct& p, hipStream_t s) {
+int ff_skinny_outputs(const FfProduct& p, int cus) {
+    const int few = p.epilogue == FF_GATE ? 16 : 8;
+    return p.N / few <= cus && (p.epilogue != FF_GATE || p.codes == nullptr) ? few : 2 * few;
+}
+
+hipError_t launch_ff_skinny(const FfProduct& p, int cus, hipStream_t s) {
+    const int outputs = ff_skinny_outputs(p, cus);
+    auto run = [&](auto kernel) { kernel<<<p.N / outputs, kThreads, 0, s>>>(p); };
+    const bool silu = p.act == PCPP_ACT_SILU;
     if (p.epilogue == FF_STORE)
-        ff_skinny<FF_STORE, 0><<<p.N / 16, kThreads, 0, s>>>(p);
-    else if (p.act == PCPP_ACT_SILU)
-        ff_skinny<FF_GATE, PCPP_ACT_SILU><<<p.N / 32, kThreads, 0, s>>>(p);
+        run(outputs == 8 ? ff_skinny<FF_STORE, 0, 8> : ff_skinny<FF_STORE, 0, 16>);
+    else if (outputs == 16)
+        run(silu ? ff_skinny<FF_GATE, PCPP_ACT_SILU, 16> : ff_skinny<FF_GATE, PCPP_ACT_GELU, 16>);
     else
-        ff_skinny<FF_GATE, PCPP_ACT_GELU><<<p.N / 32, kThreads, 0, s>>>(p);
+        run(silu ? ff_skinny<FF_GATE, PCPP_ACT_SILU, 32> : ff_skinny<FF_GATE, PCPP_ACT_GELU, 32>);
     return hipGetLastError();
 }
 

@@ -159,8 +159,10 @@ def test_plan():
     tiles; a plan's queries never need more workspace than the size says."""
     from paper_2412_02962_amd import pcpp
     plan = lambda M, C, F, which: pcpp.pcpp_gated_ff_plan(pcpp.make_ff_geom(M, C, F), which, cus=256)
-    assert plan(1, 640, 2560, pcpp.PCPP_FF_UP) == (16, 32, 1)
-    assert plan(16, 640, 2560, pcpp.PCPP_FF_DOWN) == (16, 16, 1)
+    assert plan(1, 640, 2560, pcpp.PCPP_FF_UP) == (16, 16, 1)
+    assert plan(1, 640, 5120, pcpp.PCPP_FF_UP) == (16, 32, 1)   # 320 workgroups of 16 outputs on 256 units
+    assert plan(16, 640, 2560, pcpp.PCPP_FF_DOWN) == (16, 8, 1)
+    assert plan(16, 2112, 2560, pcpp.PCPP_FF_DOWN) == (16, 16, 1)
     rows, outputs, pieces = plan(77, 1280, 5120, pcpp.PCPP_FF_DOWN)
     assert rows == 64 and pieces > 1
     assert plan(77, 1280, 5120, pcpp.PCPP_FF_UP)[2] == 1

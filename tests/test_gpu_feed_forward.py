@@ -18,8 +18,8 @@ F64, BF16, U8 = torch.float64, torch.bfloat16, torch.uint8
 
 # tokens, channels, inner width: single tokens, a few, ragged and whole tiles
 # of every size the products use, a long contraction, widths that no tile divides
-SHAPES = [(1, 64, 64), (1, 1280, 5120), (2, 640, 2560), (5, 64, 8192), (8, 2048, 64), (16, 320, 832), (17, 128, 192),
-          (31, 1280, 320), (32, 192, 1088), (33, 640, 704), (64, 64, 128), (77, 704, 1920), (129, 192, 320),
+SHAPES = [(1, 64, 64), (1, 1280, 5120), (2, 640, 2560), (3, 2112, 4160), (5, 64, 8192), (8, 2048, 64), (16, 320, 832),
+          (17, 128, 192), (31, 1280, 320), (32, 192, 1088), (33, 640, 704), (64, 64, 128), (77, 704, 1920), (129, 192, 320),
           (200, 2560, 256), (256, 256, 256), (333, 640, 1280), (513, 448, 576), (1025, 128, 512), (2049, 320, 384)]
 
 
