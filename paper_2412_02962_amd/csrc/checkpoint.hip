@@ -10,7 +10,6 @@
 #include "../../include/pcpp.h"
 #include "args.h"
 #include "checkpoint.h"
-#include "column_sums.h"
 #include "common.h"
 #include "eight_bit.h"
 #include "rows8.h"
@@ -21,8 +20,7 @@ namespace pcpp {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
+constexpr int kThreads = CHUNK_THREADS, kUnroll = CHUNK_UNROLL;
 
 // Both kernels see the rows as one run of n8 chunks of eight channels (a
 // row's channels are a multiple of 32, so no group crosses its end).
@@ -46,95 +44,12 @@ __global__ __launch_bounds__(kThreads) void checkpoint_save(const T* x, uint8_t*
 }
 
 template <typename T>
-__device__ __forceinline__ void load_chunks(const uint8_t* codes, const uint8_t* scales, T* y, int64_t n8,
-                                            int64_t block) {
-    const int64_t i0 = block * (kThreads * kUnroll) + threadIdx.x;
-    u32x2 c[kUnroll];
-    int s[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int64_t i = i0 + u * kThreads;
-        if (i < n8) {
-            c[u] = *(const u32x2*)(codes + i * 8);
-            s[u] = scales[i >> 2];
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int64_t i = i0 + u * kThreads;
-        if (i >= n8) break;
-        const float f = eight_value(s[u]);
-        const f32x4 a = from_e4m3(c[u][0]), b = from_e4m3(c[u][1]);
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = a[e] * f;
-            v[4 + e] = b[e] * f;
-        }
-        store8(y + i * 8, v);
-    }
-}
-
-template <typename T>
 __global__ __launch_bounds__(kThreads) void checkpoint_load(const uint8_t* codes, const uint8_t* scales, T* y,
                                                             int64_t n8) {
     load_chunks(codes, scales, y, n8, blockIdx.x);
 }
 
-// Sums of 64 columns of x over one of column_partial_rows(rows) runs of rows,
-// eight columns a lane.
-__device__ __forceinline__ void column_partials(const bf16* x, int64_t rows, int C, float* partial, int64_t block,
-                                                int runs) {
-    constexpr int kLaneRows = kThreads / 8;
-    __shared__ float lds[kLaneRows][64 + 4];
-    const int l = threadIdx.x & 7, r = threadIdx.x >> 3;
-    const int run = (int)(block / (C / 64)), c0 = 64 * (int)(block % (C / 64));
-    const int64_t lo = rows * run / runs, hi = rows * (run + 1) / runs;
-    float a[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = 0.f;
-    for (int64_t i = lo + r; i < hi; i += 4 * kLaneRows) {
-        float v[4][8];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
-            if (i + u * kLaneRows < hi) load8(x + (i + u * kLaneRows) * C + c0 + 8 * l, v[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] += v[u][e];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) lds[r][8 * l + e] = a[e];
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        float t = 0.f;
-#pragma unroll
-        for (int i = 0; i < kLaneRows; ++i) t += lds[i][threadIdx.x];
-        partial[(int64_t)run * C + c0 + threadIdx.x] = t;
-    }
-}
-
-__global__ __launch_bounds__(kThreads) void ff_prepare(FfPrepare p, int64_t sum_blocks, int runs) {
-    if (blockIdx.x < sum_blocks)
-        column_partials((const bf16*)p.dy, p.rows, p.C, p.partial, blockIdx.x, runs);
-    else
-        load_chunks(p.codes, p.scales, (bf16*)p.x, p.n / 8, blockIdx.x - sum_blocks);
-}
-
-unsigned blocks_of(int64_t n8) { return (unsigned)((n8 + kThreads * kUnroll - 1) / (kThreads * kUnroll)); }
-
 }  // namespace
-
-hipError_t launch_ff_prepare(const FfPrepare& p, hipStream_t s) {
-    const int64_t sums = p.partial ? column_partial_blocks(p.rows, p.C) : 0;
-    const int64_t blocks = sums + (p.n > 0 ? blocks_of(p.n / 8) : 0);
-    if (blocks == 0) return hipSuccess;
-    ff_prepare<<<(unsigned)blocks, kThreads, 0, s>>>(p, sums, p.partial ? column_partial_rows(p.rows) : 1);
-    return hipGetLastError();
-}
 
 }  // namespace pcpp
 
@@ -159,10 +74,10 @@ PCPP_EXPORT int pcpp_checkpoint_save(int64_t rows, int32_t channels, int32_t dty
     if (st != PCPP_OK) return st;
     const int64_t n8 = rows * channels / 8;
     if (dtype == PCPP_DTYPE_F32)
-        checkpoint_save<<<blocks_of(n8), kThreads, 0, (hipStream_t)stream>>>((const float*)x, (uint8_t*)codes,
+        checkpoint_save<<<chunk_blocks(n8), kThreads, 0, (hipStream_t)stream>>>((const float*)x, (uint8_t*)codes,
                                                                              (uint8_t*)scales, n8);
     else
-        checkpoint_save<<<blocks_of(n8), kThreads, 0, (hipStream_t)stream>>>((const bf16*)x, (uint8_t*)codes,
+        checkpoint_save<<<chunk_blocks(n8), kThreads, 0, (hipStream_t)stream>>>((const bf16*)x, (uint8_t*)codes,
                                                                              (uint8_t*)scales, n8);
     return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }
@@ -172,7 +87,7 @@ PCPP_EXPORT int pcpp_checkpoint_load(int64_t rows, int32_t channels, int32_t dty
     const int st = check_checkpoint(rows, channels, dtype, y, codes, scales);
     if (st != PCPP_OK) return st;
     const int64_t n = rows * channels;
-    const unsigned blocks = blocks_of(n / 8);
+    const unsigned blocks = chunk_blocks(n / 8);
     if (dtype == PCPP_DTYPE_BF16)
         checkpoint_load<<<blocks, kThreads, 0, (hipStream_t)stream>>>((const uint8_t*)codes, (const uint8_t*)scales,
                                                                       (bf16*)y, n / 8);

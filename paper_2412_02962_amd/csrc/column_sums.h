@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "rows8.h"
 
 namespace pcpp {
 
@@ -48,8 +49,45 @@ __device__ __forceinline__ void sum_partials(const PartialSums& a, int block, fl
 }
 hipError_t launch_sum_partials(const PartialSums& a, hipStream_t s);
 
-// Partial rows of column_partials for `rows` rows, and its workgroups for C columns.
+// Sums of 64 columns of x over one of column_partial_rows(rows) runs of rows,
+// eight columns a lane; a workgroup of 256, lds: COLUMN_LDS floats.
+constexpr int COLUMN_LDS = 32 * (64 + 4);
+__device__ __forceinline__ void column_partials(const bf16* x, int64_t rows, int C, float* partial, int64_t block,
+                                                int runs, float* lds) {
+    constexpr int kLaneRows = 256 / 8, LD = COLUMN_LDS / kLaneRows;
+    const int l = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int run = (int)(block / (C / 64)), c0 = 64 * (int)(block % (C / 64));
+    const int64_t lo = rows * run / runs, hi = rows * (run + 1) / runs;
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = 0.f;
+    for (int64_t i = lo + r; i < hi; i += 4 * kLaneRows) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+            if (i + u * kLaneRows < hi) load8(x + (i + u * kLaneRows) * C + c0 + 8 * l, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] += v[u][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lds[LD * r + 8 * l + e] = a[e];
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < kLaneRows; ++i) t += lds[LD * i + threadIdx.x];
+        partial[(int64_t)run * C + c0 + threadIdx.x] = t;
+    }
+}
+// Its partial rows for `rows` rows, its workgroups for C columns (a multiple of
+// 64), and a launch of its own.
 int column_partial_rows(int64_t rows);
-inline int64_t column_partial_blocks(int64_t rows, int C) { return (int64_t)((C + 63) / 64) * column_partial_rows(rows); }
+inline int column_partial_blocks(int64_t rows, int C) { return C / 64 * column_partial_rows(rows); }
+hipError_t launch_column_partials(const bf16* x, int64_t rows, int C, float* partial, hipStream_t s);
 
 }  // namespace pcpp

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "checkpoint.h"
 #include "column_sums.h"
 #include "common.h"
 
@@ -47,10 +48,12 @@ constexpr int FF_SPLIT_ROWS = 8;
 constexpr int FF_SKINNY_ROWS = 16;
 hipError_t launch_ff_skinny(const FfProduct& p, int cus, hipStream_t s);
 int ff_skinny_outputs(const FfProduct& p, int cus);  // of a workgroup
-// A product with X along the contraction (W across it for FF_GATE_GRAD alone),
-// and up to three of FF_STORE with w_t = 1 in one launch (which also does
-// `sums`).  part: ff_part_floats of the same products, or of these and others.
+// A product of FF_STORE or FF_GATE with both operands along the contraction, one
+// of FF_GATE_GRAD with W across it (the launch also does `pre`), and up to three
+// of FF_STORE with W across it (which also does `sums`).  part: ff_part_floats of
+// the same products, or of these and others.
 hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s);
+hipError_t launch_ff_gate_grad(FfProduct p, const FfPrepare& pre, hipStream_t s);
 hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const PartialSums& sums, hipStream_t s);
 int64_t ff_part_floats(const FfProduct* p, int n);
 // What they run on with `cus` compute units (0: the current device's): the

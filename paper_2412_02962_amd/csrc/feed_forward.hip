@@ -193,16 +193,17 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         x16 = (const bf16*)(ws + l.x);
         pre.codes = (const uint8_t*)x;
         pre.scales = (const uint8_t*)x_scales;
-        pre.x = ws + l.x;
+        pre.x = (bf16*)(ws + l.x);
         pre.n = M * C;
     }
     if (d.ff2_b) {
-        pre.dy = dy;
+        pre.dy = (const bf16*)dy;
         pre.rows = M;
         pre.C = (int32_t)C;
         pre.partial = sums2;
+        pre.runs = column_partial_rows(M);
+        pre.sum_blocks = column_partial_blocks(M, (int)C);
     }
-    if (launch_ff_prepare(pre, s) != hipSuccess) return PCPP_EHIP;
     if (dx || d.ff1_w || d.ff1_b || d.ff2_w) {
         FfProduct p = gate_grad_of(*g);
         p.x = (const bf16*)dy;
@@ -212,7 +213,9 @@ PCPP_EXPORT int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_we
         p.scales = (uint8_t*)const_cast<void*>(pre_scales);
         p.h = d.ff2_w ? h : nullptr;
         p.partial = d.ff1_b ? sums1 : nullptr;
-        if (launch_ff_product(p, nullptr, s) != hipSuccess) return PCPP_EHIP;
+        if (launch_ff_gate_grad(p, pre, s) != hipSuccess) return PCPP_EHIP;
+    } else if (launch_column_partials(pre.dy, M, (int)C, sums2, s) != hipSuccess) {  // ff2_b alone
+        return PCPP_EHIP;
     }
     PartialSums sums = {};
     if (d.ff1_b) {

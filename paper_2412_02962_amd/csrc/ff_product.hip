@@ -3,6 +3,7 @@
 // MFMAs, with the activation, its derivative and the 8-bit checkpoint in the
 // epilogue.
 
+#include "checkpoint.h"
 #include "column_sums.h"
 #include "eight_bit.h"
 #include "feed_forward.h"
@@ -725,11 +726,26 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int item, char*
         product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
 }
 
-template <int KIND, bool XT, bool WT, int EPI, int ACT>
+// FF_STORE or FF_GATE with both operands along the contraction.
+template <int KIND, int EPI, int ACT>
 __global__ __launch_bounds__(THREADS, per_cu(KIND)) void ff_product(FfProduct p) {
     __shared__ __attribute__((aligned(256))) char lds[lds_bytes(KIND)];
     const int item = (int)(blockIdx.x % p.n_xcd) * p.per_xcd + (int)(blockIdx.x / p.n_xcd);
-    if (item < p.items) product_tile<KIND, XT, WT, EPI, ACT>(p, item, lds);
+    if (item < p.items) product_tile<KIND, false, false, EPI, ACT>(p, item, lds);
+}
+
+// The gate's gradient; the workgroups after the product's prepare the next
+// launch, in the time that the last tiles leave compute units idle.
+template <int KIND, int ACT>
+__global__ __launch_bounds__(THREADS, per_cu(KIND)) void ff_gate_grad(FfProduct p, int32_t product_blocks, FfPrepare pre) {
+    __shared__ __attribute__((aligned(256))) char lds[lds_bytes(KIND)];
+    static_assert(COLUMN_LDS * 4 <= lds_bytes(KIND), "prepare_block's");
+    if ((int)blockIdx.x >= product_blocks) {
+        prepare_block(pre, (int)blockIdx.x - product_blocks, (float*)lds);
+        return;
+    }
+    const int item = (int)(blockIdx.x % p.n_xcd) * p.per_xcd + (int)(blockIdx.x / p.n_xcd);
+    if (item < p.items) product_tile<KIND, false, true, FF_GATE_GRAD, ACT>(p, item, lds);
 }
 
 // Up to three products of FF_STORE with W across the contraction in one
@@ -910,20 +926,13 @@ template <int KIND>
 void launch(const FfProduct& p, hipStream_t s) {
     const unsigned grid = (unsigned)p.n_xcd * p.per_xcd;
     auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p); };
-    if (p.epilogue == FF_STORE) {
-        run(ff_product<KIND, false, false, FF_STORE, 0>);
-    } else if constexpr (KIND != TILE_256) {
-        const bool silu = p.act == PCPP_ACT_SILU;
-        if (p.epilogue == FF_GATE)
-            run(silu ? ff_product<KIND, false, false, FF_GATE, PCPP_ACT_SILU>
-                     : ff_product<KIND, false, false, FF_GATE, PCPP_ACT_GELU>);
-        else
-            run(silu ? ff_product<KIND, false, true, FF_GATE_GRAD, PCPP_ACT_SILU>
-                     : ff_product<KIND, false, true, FF_GATE_GRAD, PCPP_ACT_GELU>);
-    }
+    if (p.epilogue == FF_STORE)
+        run(ff_product<KIND, FF_STORE, 0>);
+    else if constexpr (KIND != TILE_256)
+        run(p.act == PCPP_ACT_SILU ? ff_product<KIND, FF_GATE, PCPP_ACT_SILU> : ff_product<KIND, FF_GATE, PCPP_ACT_GELU>);
 }
 
-bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && p.epilogue != FF_GATE_GRAD && !p.x_t && !p.w_t; }
+bool skinny(const FfProduct& p) { return p.M <= FF_SKINNY_ROWS && !p.x_t && !p.w_t; }
 
 }  // namespace
 
@@ -966,6 +975,18 @@ hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
         launch<TILE_64>(p, s);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : sum_pieces(&p, 1, s);
+}
+
+hipError_t launch_ff_gate_grad(FfProduct p, const FfPrepare& pre, hipStream_t s) {
+    const int kind = plan(&p, 1, cus_here());
+    const unsigned blocks = (unsigned)p.n_xcd * p.per_xcd, grid = blocks + (unsigned)prepare_blocks(pre);
+    auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p, (int32_t)blocks, pre); };
+    const bool silu = p.act == PCPP_ACT_SILU;
+    if (kind == TILE_128)
+        run(silu ? ff_gate_grad<TILE_128, PCPP_ACT_SILU> : ff_gate_grad<TILE_128, PCPP_ACT_GELU>);
+    else
+        run(silu ? ff_gate_grad<TILE_64, PCPP_ACT_SILU> : ff_gate_grad<TILE_64, PCPP_ACT_GELU>);
+    return hipGetLastError();
 }
 
 hipError_t launch_ff_products(const FfProduct* p, int n, float* part, const PartialSums& sums, hipStream_t s) {

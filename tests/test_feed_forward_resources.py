@@ -18,7 +18,7 @@ def test_products_fit_a_compute_unit():
     seen = set()
     for doc in re.split(r"\n  - \.agpr_count:", r.stdout)[1:]:
         field = lambda f: int(re.search(rf"\.{f}:\s+(\d+)", doc).group(1))
-        kind = re.search(r"\.name:\s+_Z\S*ff_products?ILi(\d)E", doc)
+        kind = re.search(r"\.name:\s+_Z\S*ff_(?:products?|gate_grad)ILi(\d)E", doc)
         if not kind:
             continue
         threads, regs, lds = field("max_flat_workgroup_size"), field("vgpr_count"), field("group_segment_fixed_size")
