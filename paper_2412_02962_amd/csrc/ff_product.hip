@@ -435,8 +435,8 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
 //
 // The up product of 32768 x 1280 x 5120 (859 GF): 800 to 980 us, 1.37 M cycles
 // at the 1.5 GHz that the power limit leaves, MFMA busy in 60 % of them; with
-// its checkpoint, 16385 tokens, 435 to 480 us.  The gate's gradient there: 330
-// to 370 us, 34 %, of which about 100 are its 520 MB of results.
+// its checkpoint, 16385 tokens, 435 to 480 us.  The gate's gradient there: 345
+// to 380 us, 32 %, of which about 100 are its 520 MB of results.
 template <bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile_128(const FfProduct& p, int item, char* lds) {
     constexpr int TN = rows_w(TILE_128, EPI) / 2;          // W rows of a wavefront
