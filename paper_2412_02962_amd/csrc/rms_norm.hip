@@ -217,8 +217,11 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward(RmsBackwardParams 
     }
 }
 
-// Wavefronts per row: one up to 2048 channels unless the rows are so few that
-// four a row still leave compute units without work.
+// Wavefronts per row: one up to 2048 channels (what its registers hold) unless
+// the rows are so few that four a row still leave compute units without work.
+// One and four, bf16: 256 x 1280 forward 5.6 and 5.3 us, backward 9.1 and 8.4;
+// 2048 x 1280 backward 11.3 and 14.8 (more partial sums of dgamma), 8192 x 640
+// forward 7.8 and 10.5.
 int waves_per_row(int64_t rows, int C) { return C > 2048 || (C > 512 && rows <= 256) ? kWaves : 1; }
 
 // f(template arguments) for the wavefronts and chunks of a row of C channels.
