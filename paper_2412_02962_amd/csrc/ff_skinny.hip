@@ -20,7 +20,7 @@
 // their way into the compute unit, 8 tokens 1280 x 5120 19.0 us, 9 tokens 17.3;
 // error against float64 0.0016, not 0.0023.
 //
-// More than 16 tokens take the tiles: 16 tokens 1280 x 5120 19.6 us, by tiles 22.5;
+// More than 16 tokens take the tiles: 16 tokens 1280 x 5120 19.6 us, 17 by tiles 23.5;
 // two columns of tokens here would read twice as much of X per compute unit.
 //
 // 1 token 1280 x 5120: 8.3 and 6.0 to 7.0 us, 26 and 13 MB, where a launch alone is
