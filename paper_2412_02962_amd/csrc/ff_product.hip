@@ -565,11 +565,12 @@ __device__ __forceinline__ void product_tile_128(const FfProduct& p, int item, c
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // The two workgroups of a compute unit get different priorities here, so
-    // that they do not stay in step, both in their products, then both in
-    // their epilogues (the up product of 32768 x 1280 x 5120: 5 % fewer cycles).
-    // By the wavefront's slot on its SIMD, the low bit of the hardware's id.
-    if (__builtin_amdgcn_s_getreg(4 | (3 << 11)) & 1)
+    // Products before the other workgroup's epilogue; without much of one the two
+    // also get different priorities, so that they do not stay in step, by the
+    // wavefront's slot on its SIMD, the low bit of the hardware's id (the training
+    // step of 8192 x 640 x 2560: 336 us, all equal 355; with an epilogue it costs,
+    // forward 32768 x 1280 x 5120 1228, all equal 1192).
+    if (EPI == FF_STORE && __builtin_amdgcn_s_getreg(4 | (3 << 11)) & 1)
         __builtin_amdgcn_s_setprio(3);
     else
         __builtin_amdgcn_s_setprio(1);
