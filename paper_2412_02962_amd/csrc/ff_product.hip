@@ -433,10 +433,11 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
 // loads into the slots that the phase before the last has read.  Four to six
 // units of a workgroup are always in flight.
 //
-// The up product of 32768 x 1280 x 5120 (859 GF): 800 to 980 us, 1.37 M cycles
-// at the 1.5 GHz that the power limit leaves, MFMA busy in 60 % of them; with
-// its checkpoint, 16385 tokens, 435 to 480 us.  The gate's gradient there: 345
-// to 380 us, 32 %, of which about 100 are its 520 MB of results.
+// The up product of 32768 x 1280 x 5120 (859 GF): 780 to 980 us, 1.30 M cycles
+// at the 1.4 to 1.5 GHz that the power limit leaves, MFMA busy in 63 % of them
+// (one workgroup to a compute unit: 1.98 M, 41 %); with its checkpoint, 16385
+// tokens, 430 to 495 us.  The gate's gradient there: 335 to 380 us, 34 %, of
+// which about 100 are its 520 MB of results.
 template <bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile_128(const FfProduct& p, int item, char* lds) {
     constexpr int TN = rows_w(TILE_128, EPI) / 2;          // W rows of a wavefront
