@@ -22,14 +22,18 @@ constexpr int THREADS = 64 * WAVES;
 // The kinds of tile: their rows of X and W (wider with an epilogue that halves
 // the outputs or whose operations cover the wait for operands), ring in LDS, and
 // how many of their workgroups share a compute unit.
-enum { TILE_64, TILE_128, TILE_256, TILE_KINDS };
-constexpr int rows_x(int kind) { return kind == TILE_64 ? 64 : kind == TILE_128 ? 128 : 256; }
+// TILE_64_THREE, FF_GATE_GRAD's alone, is TILE_64 with a ring of two stages.
+enum { TILE_64, TILE_128, TILE_256, TILE_KINDS, TILE_64_THREE = TILE_KINDS };
+constexpr bool is_64(int kind) { return kind == TILE_64 || kind == TILE_64_THREE; }
+constexpr int rows_x(int kind) { return is_64(kind) ? 64 : kind == TILE_128 ? 128 : 256; }
 constexpr int rows_w(int kind, int epilogue) {
-    return kind == TILE_64 || (kind == TILE_128 && epilogue == FF_STORE) ? 128 : 256;
+    return is_64(kind) || (kind == TILE_128 && epilogue == FF_STORE) ? 128 : 256;
 }
 constexpr int outputs_of(int kind, int epilogue) { return rows_w(kind, epilogue) / (epilogue == FF_GATE ? 2 : 1); }
-constexpr int lds_bytes(int kind) { return (kind == TILE_64 ? 72 : kind == TILE_128 ? 80 : 128) * 1024; }
-constexpr int per_cu(int kind) { return kind == TILE_256 ? 1 : 2; }
+constexpr int lds_bytes(int kind) {
+    return (kind == TILE_64 ? 72 : kind == TILE_128 ? 80 : kind == TILE_256 ? 128 : 48) * 1024;
+}
+constexpr int per_cu(int kind) { return kind == TILE_64_THREE ? 3 : kind == TILE_256 ? 1 : 2; }
 
 typedef __attribute__((address_space(3))) void* lptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -337,14 +341,19 @@ __device__ __forceinline__ void store_tile(const FfProduct& p, const Item& it,
 // 45 us, now 31).  A step's operands are read behind the products of the step
 // before, a k-tile's first ones behind the last of the one before it (the
 // first k-tile's are products with zeros).
-template <bool XT, bool WT, int EPI, int ACT>
+//
+// Two stages and three workgroups cover more of the epilogues and less of the
+// loads: the gate's gradient takes them where there are tiles for all three.
+// 2093 x 640 x 2560 (660 tiles) 25.5 -> 22.9 us; with fewer, a training step of
+// 1024 x 640 x 2560 (320 tiles) 84.2 -> 85.0, of 77 x 2048 x 5504 92 -> 99.
+template <int KIND, bool XT, bool WT, int EPI, int ACT>
 __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item, char* lds) {
-    constexpr int STAGES = 3, STAGE = (64 + 128) * KT * 2;
+    constexpr int STAGE = (64 + 128) * KT * 2, STAGES = lds_bytes(KIND) / STAGE;
     typedef Layout<64, XT> LX;
     typedef Layout<128, WT> LW;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
-    const Item it = item_of<64, outputs_of(TILE_64, EPI)>(p, item);
+    const Item it = item_of<64, outputs_of(KIND, EPI)>(p, item);
 
     Source<XT> x;
     Source<WT> w;
@@ -415,7 +424,7 @@ __device__ __forceinline__ void product_tile_64x128(const FfProduct& p, int item
     for (int i = 0; i < 2; ++i) acc[i][0] = mfma32x32x16(o[1].w[i], o[1].x, acc[i][0]);
     // Loads past the end are still on their way (zeros) to the stages.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_tile<TILE_64, XT, WT, EPI, ACT>(p, it, acc, lds);
+    store_tile<KIND, XT, WT, EPI, ACT>(p, it, acc, lds);
 }
 
 // A 128 x 256 tile (FF_STORE: 128 x 128), two workgroups to a compute unit:
@@ -725,7 +734,7 @@ __device__ __forceinline__ void product_tile(const FfProduct& p, int item, char*
     else if constexpr (KIND == TILE_128)
         product_tile_128<XT, WT, EPI, ACT>(p, item, lds);
     else
-        product_tile_64x128<XT, WT, EPI, ACT>(p, item, lds);
+        product_tile_64x128<KIND, XT, WT, EPI, ACT>(p, item, lds);
 }
 
 // FF_STORE or FF_GATE with both operands along the contraction.
@@ -980,12 +989,14 @@ hipError_t launch_ff_product(FfProduct p, float* part, hipStream_t s) {
 }
 
 hipError_t launch_ff_gate_grad(FfProduct p, const FfPrepare& pre, hipStream_t s) {
-    const int kind = plan(&p, 1, cus_here());
+    const int cus = cus_here(), kind = plan(&p, 1, cus);
     const unsigned blocks = (unsigned)p.n_xcd * p.per_xcd, grid = blocks + (unsigned)prepare_blocks(pre);
     auto run = [&](auto kernel) { kernel<<<grid, THREADS, 0, s>>>(p, (int32_t)blocks, pre); };
     const bool silu = p.act == PCPP_ACT_SILU;
     if (kind == TILE_128)
         run(silu ? ff_gate_grad<TILE_128, PCPP_ACT_SILU> : ff_gate_grad<TILE_128, PCPP_ACT_GELU>);
+    else if (p.items > per_cu(TILE_64) * cus)
+        run(silu ? ff_gate_grad<TILE_64_THREE, PCPP_ACT_SILU> : ff_gate_grad<TILE_64_THREE, PCPP_ACT_GELU>);
     else
         run(silu ? ff_gate_grad<TILE_64, PCPP_ACT_SILU> : ff_gate_grad<TILE_64, PCPP_ACT_GELU>);
     return hipGetLastError();

@@ -7,7 +7,7 @@ import subprocess
 
 from paper_2412_02962_amd import build
 
-PER_CU = {"0": 2, "1": 2, "2": 1}  # 64 x 128, 128 x 256, 256 x 256 tiles
+PER_CU = {"0": 2, "1": 2, "2": 1, "3": 3}  # 64 x 128, 128 x 256, 256 x 256 tiles, 64 x 128 in two stages
 
 
 def test_products_fit_a_compute_unit():

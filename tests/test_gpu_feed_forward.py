@@ -127,22 +127,8 @@ def test_backward(M, C, F, kind):
             _check(got, want[k], bound[k], f"{k} {'8-bit x' if eight else ''}")
 
 
-@pytest.mark.parametrize("M,C,F,tiles", [
-    (2570, 1280, 2560, (128, 256)),    # the gate's and its gradient's wide tiles, ragged rows
-    (5000, 1344, 2624, (128, 256)),    # and widths that no tile divides
-    (4100, 448, 1472, (128, 128)),     # the gradients' square tiles
-    (2570, 192, 2368, (128, 128)),     # and in pieces of the contraction
-])
-def test_wide_tiles(M, C, F, tiles):
-    """Sizes whose products run on the wide tiles, forward and backward; the
-    reference in float64 on the GPU."""
-    from paper_2412_02962_amd import pcpp
-    _say("wide tiles", M, C, F)
-    kind = "gelu"
-    x, w, dy = _inputs(M, C, F, 71)
-    c = Call(M, C, F, kind, _dev(w))
-    got = [pcpp.pcpp_gated_ff_plan(c.g, k)[0] for k in (pcpp.PCPP_FF_UP, pcpp.PCPP_FF_GATE_GRAD, pcpp.PCPP_FF_X_GRAD)]
-    assert got[0] == got[1] == tiles[0] and got[2] == tiles[1], got
+def _check_on_gpu(c, x, dy, kind):
+    """Forward and backward against the reference in float64 on the GPU."""
     c.forward(x.to(DEV))
     torch.cuda.synchronize()
     x64, w64, dy64 = x.to(DEV, F64), _f64(c.wd), dy.to(DEV, F64)
@@ -155,6 +141,36 @@ def test_wide_tiles(M, C, F, tiles):
     bound = ref.gated_ff_backward_bound(x64, w64, kept.to(DEV), dy64, kind)
     for k, t in dict(dx=c.dx, **c.grads).items():
         _check(t, want[k].cpu(), bound[k].cpu(), k)
+
+
+@pytest.mark.parametrize("M,C,F,tiles", [
+    (2570, 1280, 2560, (128, 256)),    # the gate's and its gradient's wide tiles, ragged rows
+    (5000, 1344, 2624, (128, 256)),    # and widths that no tile divides
+    (4100, 448, 1472, (128, 128)),     # the gradients' square tiles
+    (2570, 192, 2368, (128, 128)),     # and in pieces of the contraction
+])
+def test_wide_tiles(M, C, F, tiles):
+    """Sizes whose products run on the wide tiles, forward and backward."""
+    from paper_2412_02962_amd import pcpp
+    _say("wide tiles", M, C, F)
+    kind = "gelu"
+    x, w, dy = _inputs(M, C, F, 71)
+    c = Call(M, C, F, kind, _dev(w))
+    got = [pcpp.pcpp_gated_ff_plan(c.g, k)[0] for k in (pcpp.PCPP_FF_UP, pcpp.PCPP_FF_GATE_GRAD, pcpp.PCPP_FF_X_GRAD)]
+    assert got[0] == got[1] == tiles[0] and got[2] == tiles[1], got
+    _check_on_gpu(c, x, dy, kind)
+
+
+@pytest.mark.parametrize("M,C,F,kind", [(2093, 640, 2560, "gelu"), (2570, 320, 1728, "silu"), (4999, 64, 960, "gelu")])
+def test_many_small_tiles(M, C, F, kind):
+    """The gate's gradient on small tiles, more than two for each of 256 compute units."""
+    from paper_2412_02962_amd import pcpp
+    _say("many small tiles", M, C, F)
+    x, w, dy = _inputs(M, C, F, 73)
+    c = Call(M, C, F, kind, _dev(w))
+    rows, outputs, _ = pcpp.pcpp_gated_ff_plan(c.g, pcpp.PCPP_FF_GATE_GRAD)
+    assert (rows, outputs) == (64, 128) and -(-M // rows) * -(-F // outputs) > 2 * 256
+    _check_on_gpu(c, x, dy, kind)
 
 
 def test_no_biases():
