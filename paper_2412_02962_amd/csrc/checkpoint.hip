@@ -37,6 +37,8 @@ __global__ __launch_bounds__(kThreads) void checkpoint_save(const T* x, uint8_t*
     for (int u = 0; u < kUnroll; ++u) {
         const int64_t i = i0 + u * kThreads;
         if (i >= n8) break;  // n8 is a multiple of four: a group's lanes leave together
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = quieted(v[u][e]);  // the caller's bits, of no arithmetic
         int scale;
         *(u32x2*)(codes + i * 8) = to_eight_bits(v[u], scale);
         if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)scale;

@@ -37,6 +37,9 @@ __device__ __forceinline__ int eight_scale(float top) {
 __device__ __forceinline__ float eight_inverse(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 __device__ __forceinline__ float eight_value(int scale) { return __uint_as_float((uint32_t)scale << 23); }
 
+// v, a signalling NaN as a quiet one.
+__device__ __forceinline__ float quieted(float v) { return __builtin_canonicalizef(v); }
+
 // Four values, already divided by the scale, as four codes.
 __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -54,8 +57,9 @@ __device__ __forceinline__ f32x4 from_e4m3(uint32_t w) {
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-// The largest magnitude of eight values; NaN among them may be passed over or
-// come through.
+// The largest magnitude of eight values; quiet NaN among them may be passed over
+// or come through.  (A signalling NaN, which no arithmetic leaves, would come
+// through as a quiet one and hide a larger value: quieted() before.)
 __device__ __forceinline__ float max_abs8(const float (&v)[8]) {
     float a, b;
     asm("v_max_f32 %0, |%1|, |%2|" : "=v"(a) : "v"(v[0]), "v"(v[1]));
