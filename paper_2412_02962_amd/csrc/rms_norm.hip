@@ -119,8 +119,9 @@ __global__ __launch_bounds__(kThreads) void rms_norm(RmsParams p) {
             if (p.sum != nullptr) store8((T*)p.sum + at + c, s[j]);
             float g[8];
             load8(p.gamma + c, g);
+            // n = s rstd first, at most sqrt(C): rstd gamma may be no float32
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[j][e] *= rstd * g[e];
+            for (int e = 0; e < 8; ++e) s[j][e] = s[j][e] * rstd * g[e];
             if (p.y != nullptr) store8(p.y + at + c, s[j]);
             if (p.codes != nullptr) {
                 int scale;

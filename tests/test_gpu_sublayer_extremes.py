@@ -1,4 +1,5 @@
-"""Signalling NaN in the feed-forward sub-layer's operators."""
+"""Signalling NaN, and products that pass float32's range on the way to a value
+within it, in the feed-forward sub-layer's operators."""
 
 import pytest
 import torch
@@ -6,11 +7,17 @@ import torch
 from tests import ff_reference as ref
 
 pytestmark = pytest.mark.gpu
-DEV, BF16, U8 = "cuda", torch.bfloat16, torch.uint8
+DEV, F64, BF16, U8 = "cuda", torch.float64, torch.bfloat16, torch.uint8
 
 
 def _say(*a):
     print("[case]", *a, flush=True)
+
+
+def _worst(err, bound):
+    worst = float((err / bound).nan_to_num(float("inf")).max())
+    print(f"worst err/bound {worst:.3f}", flush=True)
+    assert worst <= 1.0
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -43,3 +50,31 @@ def test_a_signalling_nan_leaves_its_group_as_it_is(dtype):
     got, nan = codes.cpu(), (want_c & 127) == 127
     assert torch.equal(scales.cpu(), want_s)
     assert ((got & 127) == 127)[nan].all() and torch.equal(got[~nan], want_c[~nan])
+
+
+# rows and channels of one wavefront a row, of four, and of four for few rows
+NORM_SHAPES = [(3, 64), (300, 1280), (9, 640), (2, 4096)]
+
+
+def _small_rows(R, C, eps):
+    gen = torch.Generator().manual_seed(R + C)
+    s = torch.randn(R, C, generator=gen) * eps ** 0.5
+    s[R // 2] = 0
+    return gen, s, float(torch.tensor(eps))  # eps as the call has it
+
+
+@pytest.mark.parametrize("R,C", NORM_SHAPES)
+def test_the_norm_with_a_large_gamma(R, C):
+    """rstd about 2^49 and gamma about 2^100: s rstd gamma is finite, and zero
+    where s is; rstd gamma is not a float32.  y is its own rounding and that of
+    a few float32 operations, whose errors are relative: 2^-18."""
+    from paper_2412_02962_amd import pcpp
+    _say("large gamma", R, C)
+    gen, s, eps = _small_rows(R, C, 1e-30)
+    gamma = (2.0 ** 100 * (1 + 0.1 * torch.randn(C, generator=gen))).to(BF16)
+    y = torch.empty(R, C, device=DEV, dtype=BF16)
+    sd, gd = s.to(DEV), gamma.to(DEV)
+    pcpp.pcpp_rms_norm(R, C, eps, pcpp.PCPP_DTYPE_F32, sd, None, gd, None, y)
+    torch.cuda.synchronize()
+    want = ref.rms_norm(s.to(F64), gamma.to(F64), eps)
+    _worst((y.cpu().to(F64) - want).abs(), (ref.HALF_BF16 + 2.0 ** -18) * want.abs() + 1e-30)
