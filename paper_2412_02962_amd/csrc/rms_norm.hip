@@ -165,9 +165,9 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward(RmsBackwardParams 
             }
         }
         const float rstd = 1.f / sqrtf(row_sum<WPR>(sq, lds) / (float)p.C + p.eps);
-        // rstd (w - n mean(w n)) = rstd w - k n (not by rstd^3, which overflows for
-        // rows below 10^-13 where eps lets them)
-        const float k = rstd * (row_sum<WPR>(dot, lds) / (float)p.C) * rstd;
+        // mean(w n); rstd (w - n mean(w n)) by n and w, not by rstd^3 or dy rstd,
+        // which overflow for small rows where eps lets them
+        const float mean = rstd * (row_sum<WPR>(dot, lds) / (float)p.C);
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int c = c0 + 512 * WPR * j;
@@ -179,9 +179,9 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward(RmsBackwardParams 
             if (p.ds_in != nullptr) load8((const T*)p.ds_in + at + c, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float dr = d[j][e] * rstd;
-                dg[j][e] = __builtin_fmaf(dr, s[j][e], dg[j][e]);
-                o[e] += __builtin_fmaf(dr, g[e], -k * (s[j][e] * rstd));
+                const float n = s[j][e] * rstd;
+                dg[j][e] = __builtin_fmaf(d[j][e], n, dg[j][e]);
+                o[e] = __builtin_fmaf(rstd, __builtin_fmaf(-mean, n, d[j][e] * g[e]), o[e]);
             }
             store8((T*)p.ds + at + c, o);
         }

@@ -78,3 +78,29 @@ def test_the_norm_with_a_large_gamma(R, C):
     torch.cuda.synchronize()
     want = ref.rms_norm(s.to(F64), gamma.to(F64), eps)
     _worst((y.cpu().to(F64) - want).abs(), (ref.HALF_BF16 + 2.0 ** -18) * want.abs() + 1e-30)
+
+
+@pytest.mark.parametrize("R,C", NORM_SHAPES)
+def test_the_norms_gradient_with_a_large_dy(R, C):
+    """rstd about 2^49, dy about 2^100 and gamma about 2^-70: dy n and dy gamma
+    rstd are finite, dy rstd is not.  What cancels carries 2^-18 of its size, as
+    do dgamma's terms, whose float32 sum adds them in any order."""
+    from paper_2412_02962_amd import pcpp
+    _say("large dy", R, C)
+    gen, s, eps = _small_rows(R, C, 1e-30)
+    gamma = (2.0 ** -70 * (1 + 0.1 * torch.randn(C, generator=gen))).to(BF16)
+    dy = (2.0 ** 100 * torch.randn(R, C, generator=gen)).to(BF16)
+    ds, dgamma = torch.empty(R, C, device=DEV), torch.empty(C, device=DEV, dtype=BF16)
+    n = pcpp.pcpp_rms_norm_backward_workspace_size(R, C)
+    ws = torch.empty(n, dtype=U8, device=DEV)
+    sd, gd, dyd = s.to(DEV), gamma.to(DEV), dy.to(DEV)
+    pcpp.pcpp_rms_norm_backward(R, C, eps, pcpp.PCPP_DTYPE_F32, sd, gd, dyd, None, ds, dgamma, ws, n)
+    torch.cuda.synchronize()
+    s, dy, gamma = s.to(F64), dy.to(F64), gamma.to(F64)
+    want, want_g = ref.rms_norm_backward(s, gamma, dy, None, eps)
+    rstd = 1 / torch.sqrt(s.square().mean(-1, keepdim=True) + eps)
+    w = (dy * gamma).abs()
+    part = rstd * (w + (s * rstd).abs() * w.square().mean(-1, keepdim=True).sqrt())
+    _worst((ds.cpu().to(F64) - want).abs(), 2.0 ** -24 * want.abs() + 2.0 ** -18 * part)
+    terms = (dy * s * rstd).abs().sum(0)
+    _worst((dgamma.cpu().to(F64) - want_g).abs(), ref.HALF_BF16 * want_g.abs() + 2.0 ** -18 * terms)
