@@ -93,13 +93,15 @@ __global__ __launch_bounds__(kThreads) void ff_skinny(FfProduct p) {
     __syncthreads();
     const int n = threadIdx.x % BNO, m = threadIdx.x / BNO;  // output, token
     auto total = [&](int i, int row) {  // of row `row` of block i, the wavefronts in their order
-        float t = 0.f;
+        float t = 0.f, second = 0.f;
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) {
             t += sums[k][i][16 * (row >> 2) + m][row & 3];
-            if (two) t += sums[k][i][16 * (row >> 2) + 8 + (m & 7)][row & 3];
+            if (two) second += sums[k][i][16 * (row >> 2) + 8 + (m & 7)][row & 3];
         }
-        return t;
+        // an infinite weight times a second half, zero or of the other sign, is
+        // no part of the sum
+        return two && is_finite(t) ? t + second : t;
     };
     if (m >= 16 || m >= p.M) return;  // a group's 32 lanes together (BNO = 32)
     if constexpr (EPI == FF_GATE) {

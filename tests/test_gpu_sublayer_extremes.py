@@ -1,5 +1,5 @@
-"""Signalling NaN, and products that pass float32's range on the way to a value
-within it, in the feed-forward sub-layer's operators."""
+"""Signalling NaN, products that pass float32's range on the way to a value
+within it, and infinite weights in the feed-forward sub-layer's operators."""
 
 import pytest
 import torch
@@ -104,3 +104,37 @@ def test_the_norms_gradient_with_a_large_dy(R, C):
     _worst((ds.cpu().to(F64) - want).abs(), 2.0 ** -24 * want.abs() + 2.0 ** -18 * part)
     terms = (dy * s * rstd).abs().sum(0)
     _worst((dgamma.cpu().to(F64) - want_g).abs(), ref.HALF_BF16 * want_g.abs() + 2.0 ** -18 * terms)
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 9, 16, 17, 130])
+@pytest.mark.parametrize("kind", ["gelu", "silu"])
+def test_an_infinite_weight(M, kind):
+    """An infinity in ff2_w makes its column of y infinite with h's sign, however
+    many tokens a call has; the other columns stay as they are without it."""
+    from paper_2412_02962_amd import pcpp
+    _say("infinite weight", M, kind)
+    C, F = 64, 128
+    gen = torch.Generator().manual_seed(M)
+    x = torch.randn(M, C, generator=gen).to(BF16)
+    w = dict(ff1_w=(torch.randn(2 * F, C, generator=gen) * C ** -0.5).to(BF16), ff1_b=torch.zeros(2 * F, dtype=BF16),
+             ff2_w=torch.randn(C, F, generator=gen).to(BF16), ff2_b=torch.zeros(C, dtype=BF16))
+    # a whole h, and one that bf16 holds exactly (its second half is zero)
+    w["ff1_w"][40], w["ff1_w"][F + 40] = 0, 0
+    w["ff1_b"][40], w["ff1_b"][F + 40] = 1.0, 100.0
+    outs = []
+    g = pcpp.make_ff_geom(M, C, F, pcpp.PCPP_ACT_SILU if kind == "silu" else pcpp.PCPP_ACT_GELU)
+    n = pcpp.pcpp_gated_ff_workspace_size(g)
+    ws = torch.empty(n, dtype=U8, device=DEV)
+    for infinite in (False, True):
+        if infinite:
+            w["ff2_w"][5, 17], w["ff2_w"][30, 40] = float("inf"), -float("inf")
+        wd, y = {k: v.to(DEV) for k, v in w.items()}, torch.empty(M, C, device=DEV, dtype=BF16)
+        pcpp.pcpp_gated_ff(g, pcpp.make_ff_weights(wd), x.to(DEV), y, None, None, ws, n)
+        torch.cuda.synchronize()
+        outs.append(y.cpu())
+    h = ref.gated_ff(x.to(F64), {k: v.to(F64) for k, v in w.items()}, kind)[1]
+    assert bool((h[:, 17].abs() > 1e-6).all()) and bool((h[:, 40] == 100).all())
+    keep = [c for c in range(C) if c not in (5, 30)]
+    assert torch.equal(outs[0][:, keep], outs[1][:, keep])
+    assert torch.equal(outs[1][:, 5].to(F64), torch.sign(h[:, 17]) * float("inf"))
+    assert bool((outs[1][:, 30] == -float("inf")).all())
