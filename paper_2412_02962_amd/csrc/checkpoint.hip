@@ -2,8 +2,8 @@
 //   pcpp_checkpoint_save, pcpp_checkpoint_load
 // Both are bound by the memory: eight channels a lane, a group's scale by two
 // permutations within its four lanes, several chunks in flight.  Measured, both
-// ways: 2048 x 640 bf16 9.8 us (two launches), 16384 x 5120 float32 131 us
-// (671 MB, 5.1 TB/s).
+// ways: 2048 x 640 bf16 9.8 us (two launches), 16384 x 5120 float32 133 us
+// (671 MB, 5.0 TB/s; 131 before the values were quieted).
 
 #include <stdint.h>
 

@@ -614,7 +614,7 @@ __device__ __forceinline__ void product_tile_128(const FfProduct& p, int item, c
 // waits only for a load that was issued five phases (about 2500 cycles) before.
 //
 // The down product of 32768 x 1280 x 5120 (429 GF): 365 to 435 us, 0.65 M cycles
-// at 1.5 GHz, MFMA busy in 63 %; the gradients of 16385 tokens (859 GF): 870 to
+// at 1.5 GHz, MFMA busy in 63 %; the gradients of 16385 tokens (1074 GF): 870 to
 // 1000 us, 68 %, 1.7 GHz.  A k-tile takes 2700 cycles, 2480 without its loads,
 // 2270 without its reads too, 2048 of MFMA.
 template <bool XT, bool WT>
@@ -831,14 +831,18 @@ int64_t pieces_of(const FfProduct& p, int64_t run) {
     return n > 1 ? n : 1;
 }
 
-// Time in us of n products on a kind of tile, their contractions in runs
-// of about `run` k-tiles; floats: the pieces' sums.  Per k-tile and per item
-// (its start and epilogue), alone on a compute unit and when all of them have
-// all the workgroups that fit; by epilogue.  FF_STORE's, and the pieces' cost,
-// are those whose choices came out fastest over the kinds and cuts measured for
-// 39 sizes (77 to 16385 tokens, 320 x 1280 to 2048 x 8192): the choices are
-// within 2 % of the best ones in the mean, within 12 % each.  kSlower: what
-// many k-tiles add to a k-tile's time, by lower clocks at the power limit.
+// Estimated us of n products on a kind of tile, their contractions in runs of
+// about `run` k-tiles; floats: the pieces' sums.  By epilogue and kind: what a
+// k-tile and an item (its start and epilogue) add to the longest item
+// (kAlone) and to the busiest compute unit (kFull).
+//
+// These are weights for choosing, no times of a k-tile: FF_STORE's, kSlower (more
+// k-tiles, lower clocks) and the pieces' cost were fitted until their choices
+// came out fastest over the kinds and cuts measured for 39 sizes (77 to 16385
+// tokens, 320 x 1280 to 2048 x 8192), 2 % above the best ones in the mean, 12 %
+// at most.  (So the 256 x 256 tile's k-tile is 0.826 here, less than its 2048
+// cycles of products.)  FF_GATE's and FF_GATE_GRAD's are round numbers set by
+// hand; the latter's are TILE_64's, also where it runs as TILE_64_THREE.
 struct TileCost {
     double tile, item;
 };

@@ -14,7 +14,7 @@
 // nothing but s is kept from the forward pass.
 //
 // Measured: forward 2 x 1280 5.4 us (a launch), 115200 x 640 with a float32
-// stream and an addend 155 us (958 MB, 6.2 TB/s: a copy of 2 GiB reaches 5.2,
+// stream and an addend 155 us (885 MB, 5.7 TB/s: a copy of 1 GiB reaches 5.2,
 // part of the stream comes from the last-level cache), 8192 x 1280 with 8 bits
 // too 41 us (168 MB, two calls); backward 777 x 1088 9.2 us (two launches, the
 // second sums dgamma), 57600 x 640 100 us (516 MB, 5.2 TB/s).
