@@ -885,6 +885,184 @@ int pcpp_gated_ff_backward(const pcpp_ff_geom_t* g, const pcpp_ff_weights_t* w,
                            const pcpp_ff_grads_t* grads, void* workspace,
                            size_t ws_bytes, void* stream);
 
+/*
+ * Dropout.  Whether an element is kept is a function of the generator's state
+ * and the element's place, computed wherever it is needed and never stored:
+ * the backward pass asks again.  The generator is Philox 4x32-10 (J. Salmon et
+ * al., Parallel random numbers: as easy as 1, 2, 3, SC 2011) with the key =
+ * seed and the counter = (place / 8 in its low, the stream in its high 64
+ * bits); element `place` takes the 16 bits place % 8 of the block's 128, from
+ * the lowest.  It is kept where they are at least t = round(65536 p) (ties to
+ * even), and then scaled by 65536 / (65536 - t): p is applied in steps of
+ * 2^-16, and a p below 2^-17 drops nothing.
+ *   rng   device, two uint64, 8-byte aligned: seed, first stream.  On the
+ *         device so that a captured graph takes new masks at every replay
+ *         when the program advances it there.  Not read when p = 0 (may then
+ *         be NULL)
+ *   draw  added to the first stream (mod 2^64): a number for each place in
+ *         the program, forward and backward alike
+ */
+
+/*
+ * y = residual + (kept ? x / (1 - p) : 0), in float32, rounded once.
+ *   x         n elements of x_dtype
+ *   residual  n elements of y_dtype, or NULL; y  n elements of y_dtype
+ * A dropped element counts as 0 whatever it is (infinities and NaN).  y may be
+ * the residual, or x when the types are the same; no other overlap.  The
+ * gradient of x is this call on y's gradient with residual NULL; the
+ * residual's is y's.  1 <= n <= 2^36, p in [0, 1]; x, residual and y 16-byte
+ * aligned (PCPP_EINVAL); types PCPP_DTYPE_F32 or PCPP_DTYPE_BF16
+ * (PCPP_ENOTSUP).  Asynchronous on `stream`.
+ */
+int pcpp_dropout(int64_t n, int32_t x_dtype, int32_t y_dtype, float p,
+                 const void* rng, uint64_t draw, const void* x,
+                 const void* residual, void* y, void* stream);
+
+/*
+ * GroupNorm with its activation and dropout for training, channels last: the
+ * first half of a ResNet's branch before each convolution.
+ *   n = (x - mean) rstd;  z = n gamma + beta;  y = dropped(act(z))
+ * mean and rstd = 1 / sqrt(variance + eps) over a group's channels and the
+ * image's tokens.  (pcpp_group_norm is the inference form with the bands'
+ * synchronized statistics.)
+ */
+#define PCPP_ACT_NONE 2   /* besides PCPP_ACT_GELU and PCPP_ACT_SILU         */
+
+typedef struct {
+    int32_t batch;         /* images, 1 .. 65535                             */
+    int32_t tokens;        /* of an image, >= 1                              */
+    int32_t channels;      /* a multiple of 8, <= 2560                       */
+    int32_t groups;        /* dividing the channels, <= 256                  */
+    int32_t act;           /* PCPP_ACT_GELU, PCPP_ACT_SILU or PCPP_ACT_NONE  */
+    int32_t dtype;         /* of x, y, dy and dx: PCPP_DTYPE_F32 or _BF16    */
+    float eps;             /* > 0                                            */
+    float drop;            /* dropout's p, in [0, 1]; 0: none                */
+    int32_t reserved;      /* must be 0                                      */
+} pcpp_norm_act_geom_t;
+
+/* Bytes of device workspace of either call (0 if g is invalid).  It needs no
+ * clearing; nothing in it survives a call. */
+size_t pcpp_group_norm_act_workspace_size(const pcpp_norm_act_geom_t* g);
+
+/*
+ *   x, y         [batch, tokens, channels] of dtype
+ *   gamma, beta  [channels] bf16
+ *   rng, draw    dropout's, above; an element's place is its index in y
+ *   stats        NULL, or [batch][groups] x (mean, rstd) float32: what the
+ *                backward pass reads
+ * The statistics are float32, by means and squared deviations of runs of
+ * tokens merged in a fixed order.  Errors: PCPP_EINVAL (sizes, eps, drop, NULL
+ * or misaligned pointers - 16 bytes, stats 4, rng 8 - overlaps, more than 2^36
+ * elements), PCPP_ENOTSUP (types, act, channels or groups), PCPP_EWORKSPACE.
+ * Asynchronous on `stream`.
+ */
+int pcpp_group_norm_act(const pcpp_norm_act_geom_t* g, const void* x,
+                        const void* gamma, const void* beta, const void* rng,
+                        uint64_t draw, void* y, float* stats, void* workspace,
+                        size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass: with g = dropped(dy) act'(z) and w = g gamma,
+ *   dx = rstd (w - mean(w) - n mean(w n));  dgamma = sum g n;  dbeta = sum g
+ * the means over a group's channels and the image's tokens, the sums over all
+ * images.
+ *   stats          the forward pass's;  rng, draw  the same as there
+ *   dy, dx         [batch, tokens, channels] of dtype; dx may be dy
+ *   dgamma, dbeta  [channels] bf16, either may be NULL; overwritten, summed in
+ *                  float32 in a fixed order
+ * Otherwise as pcpp_group_norm_act.
+ */
+int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, const void* x,
+                                 const void* gamma, const void* beta,
+                                 const float* stats, const void* rng,
+                                 uint64_t draw, const void* dy, void* dx,
+                                 void* dgamma, void* dbeta, void* workspace,
+                                 size_t ws_bytes, void* stream);
+
+/*
+ * Attention with masks, a bias by distance and capped scores, bf16 storage
+ * with float32 accumulation, in training and in serving.  Per sequence b and
+ * head a, which reads key head a * kv_heads / heads:
+ *   z_ij = scale q_i . k_j;   s_ij = cap tanh(z_ij / cap)   (cap > 0, else z)
+ *   s_ij -= slopes[a] |p_i - j|                             (with slopes)
+ *   y_i = sum_j softmax_j(s_i.) v_j over the keys j that query i sees
+ * Query i stands at position p_i = q_pos[b] + i, key j at j.  Query i sees key
+ * j if all of these hold:
+ *   j < kv_len[b];
+ *   j <= p_i or j < prefix[b], if causal;
+ *   q_doc[b][i] = kv_doc[b][j] and q_doc[b][i] >= 0, with documents.
+ * A query that sees no key gets y = 0, its logarithm -infinity and no
+ * gradient; a key that no query sees gets gradients 0.  What a query does not
+ * see does not touch its result, infinities and NaN included.
+ */
+typedef struct {
+    int32_t batch;         /* sequences B, 1 .. 65535                        */
+    int32_t n_q, n_kv;     /* tokens, 1 .. 2^24                              */
+    int32_t heads;         /* of the queries, 1 .. 1024                      */
+    int32_t kv_heads;      /* of the keys and values, dividing heads         */
+    int32_t head_dim;      /* D, a multiple of 8, 8 .. 128                   */
+    int32_t causal;        /* 0 or 1                                         */
+    float scale;           /* finite                                         */
+    float cap;             /* finite, > 0; 0: none                           */
+    int32_t reserved;      /* must be 0                                      */
+    /* Elements from a token to the next and from a sequence to the next, both
+     * multiples of 8; 0: contiguous (heads * D, and tokens * the row).  A row
+     * is at least its heads * D; a gradient has the layout of its tensor. */
+    int64_t q_row, k_row, v_row, y_row;
+    int64_t q_batch, k_batch, v_batch, y_batch;
+} pcpp_masked_geom_t;
+
+/* Device arrays, 4-byte aligned, read by the kernels; each may be NULL. */
+typedef struct {
+    const int32_t* kv_len; /* [B], taken into 0 .. n_kv; NULL: n_kv          */
+    const int32_t* q_pos;  /* [B], any values; NULL: n_kv - n_q              */
+    const int32_t* prefix; /* [B]; needs causal; NULL: 0                     */
+    const int32_t* q_doc;  /* [B, n_q] document of each query, < 0: none     */
+    const int32_t* kv_doc; /* [B, n_kv]; both or neither                     */
+    const float* slopes;   /* [heads], constants of the model (no gradient)  */
+} pcpp_mask_t;
+
+/* Bytes of device workspace (0 if g is invalid), for any mask.  It needs no
+ * clearing; nothing in it survives a call. */
+size_t pcpp_masked_attention_workspace_size(const pcpp_masked_geom_t* g);
+
+/*
+ *   m     NULL (no masks, no bias) or as above
+ *   q     [B, n_q, heads, D], k, v [B, n_kv, kv_heads, D], y as q, in the
+ *         geometry's rows
+ *   lse   NULL, or [B, heads, n_q] float32: the natural logarithm of the sum
+ *         of exp(s_ij) over the keys seen, what the backward pass reads
+ * Few queries on a long cache are worked in pieces of the keys, joined in a
+ * second launch.  Keys at kv_len[b] and behind are not read.
+ * Errors: PCPP_EINVAL (geometry, NULL or misaligned pointers - 16 bytes, lse
+ * and the mask's arrays 4 - documents of one side only, prefix without causal,
+ * outputs overlapping anything), PCPP_ENOTSUP (head_dim), PCPP_EWORKSPACE.
+ * Asynchronous on `stream`.
+ */
+int pcpp_masked_attention(const pcpp_masked_geom_t* g, const pcpp_mask_t* m,
+                          const void* q, const void* k, const void* v, void* y,
+                          float* lse, void* workspace, size_t ws_bytes,
+                          void* stream);
+
+/*
+ * Its backward pass, from y and lse:
+ *   P_ij = exp(s_ij - lse_i);  dP_ij = dy_i . v_j;
+ *   dS_ij = P_ij (dP_ij - dy_i . y_i);  dz_ij = dS_ij (1 - tanh(z_ij / cap)^2)
+ *   dq_i = scale sum_j dz_ij k_j;  dk_j = scale sum_i dz_ij q_i;
+ *   dv_j = sum_i P_ij dy_i       (i over the queries of all heads that read j)
+ *   y, lse  the forward pass's;  dy  in y's layout
+ *   dq, dk, dv  in the layouts of q, k, v; dq, or dk and dv, may be NULL.
+ *         Every token's row is written, those behind kv_len too (with 0).
+ * No atomics: a result is the same at every call.  Otherwise as above.
+ */
+size_t pcpp_masked_attention_backward_workspace_size(const pcpp_masked_geom_t* g);
+int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g,
+                                   const pcpp_mask_t* m, const void* q,
+                                   const void* k, const void* v, const void* y,
+                                   const float* lse, const void* dy, void* dq,
+                                   void* dk, void* dv, void* workspace,
+                                   size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

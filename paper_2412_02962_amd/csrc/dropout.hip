@@ -1,0 +1,106 @@
+// Dropout with the residual's addition, and the way back of its gradient.
+//   pcpp_dropout  y = residual + (kept ? x / (1 - p) : 0)
+
+#include <stdint.h>
+
+#include "../../include/pcpp.h"
+#include "args.h"
+#include "common.h"
+#include "dropout.h"
+#include "rows8.h"
+
+#define PCPP_EXPORT extern "C" __attribute__((visibility("default")))
+
+namespace pcpp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;
+
+struct DropoutParams {
+    const void* x;
+    const void* residual;  // or null
+    void* y;
+    int64_t n;
+    Dropout drop;
+};
+
+// Elements at .. n - 1 of the last block of eight, the rest as 0.
+template <typename T>
+__device__ __forceinline__ void load_tail(const T* p, int64_t at, int64_t n, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = at + e < n ? (float)p[at + e] : 0.f;
+}
+
+template <typename X, typename Y>
+__global__ __launch_bounds__(kThreads) void dropout(DropoutParams p) {
+    const X* x = (const X*)p.x;
+    const Y* res = (const Y*)p.residual;
+    Y* y = (Y*)p.y;
+    const int64_t whole = p.n / 8, blocks = (p.n + 7) / 8;
+    const int64_t i0 = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
+    float v[kUnroll][8], r[kUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[u][e] = 0.f;
+        if (i < whole) {
+            load8(x + 8 * i, v[u]);
+            if (res != nullptr) load8(res + 8 * i, r[u]);
+        } else if (i < blocks) {
+            load_tail(x, 8 * i, p.n, v[u]);
+            if (res != nullptr) load_tail(res, 8 * i, p.n, r[u]);
+        }
+    }
+    const DropoutKey key = dropout_key(p.drop);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int64_t i = i0 + u * kThreads;
+        if (i >= blocks) break;
+        if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)i, v[u]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] += r[u][e];
+        if (i < whole) {
+            store8(y + 8 * i, v[u]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (8 * i + e < p.n) y[8 * i + e] = (Y)v[u][e];
+        }
+    }
+}
+
+}  // namespace
+
+}  // namespace pcpp
+
+using namespace pcpp;
+
+PCPP_EXPORT int pcpp_dropout(int64_t n, int32_t x_dtype, int32_t y_dtype, float p, const void* rng, uint64_t draw,
+                             const void* x, const void* residual, void* y, void* stream) {
+    if (n < 1 || n > ((int64_t)1 << 36) || !(p >= 0.f && p <= 1.f)) return PCPP_EINVAL;
+    for (const int32_t t : {x_dtype, y_dtype})
+        if (t != PCPP_DTYPE_F32 && t != PCPP_DTYPE_BF16) return PCPP_ENOTSUP;
+    if (!x || !y || (p > 0.f && !rng)) return PCPP_EINVAL;
+    if (!aligned_to(x, 16) || !aligned_to(residual, 16) || !aligned_to(y, 16) || !aligned_to(rng, 8)) return PCPP_EINVAL;
+    const int64_t xb = n * (x_dtype == PCPP_DTYPE_F32 ? 4 : 2), yb = n * (y_dtype == PCPP_DTYPE_F32 ? 4 : 2);
+    // y may replace the residual, or x of its type: every element is read and
+    // written by one lane
+    const Range out[] = {{y, yb}};
+    const Range in[] = {{x == y && x_dtype == y_dtype ? nullptr : x, xb}, {residual == y ? nullptr : residual, yb}, {rng, 16}};
+    if (outputs_overlap(out, 1, in, 3)) return PCPP_EINVAL;
+    const DropoutParams a = {x, residual, y, n, make_dropout(p, rng, draw)};
+    const int64_t per = 8 * kThreads * kUnroll;
+    const unsigned grid = (unsigned)((n + per - 1) / per);
+    const hipStream_t s = (hipStream_t)stream;
+    if (x_dtype == PCPP_DTYPE_F32) {
+        if (y_dtype == PCPP_DTYPE_F32) dropout<float, float><<<grid, kThreads, 0, s>>>(a);
+        else dropout<float, bf16><<<grid, kThreads, 0, s>>>(a);
+    } else {
+        if (y_dtype == PCPP_DTYPE_F32) dropout<bf16, float><<<grid, kThreads, 0, s>>>(a);
+        else dropout<bf16, bf16><<<grid, kThreads, 0, s>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}

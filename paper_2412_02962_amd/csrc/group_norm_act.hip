@@ -1,0 +1,596 @@
+// GroupNorm with its activation and dropout on channels-last rows, for
+// training (and inference in float32 or with GELU), and its backward pass.
+//   pcpp_group_norm_act           n = (x - mean) rstd;  z = n gamma + beta;
+//                                 y = dropped(act(z))
+//   pcpp_group_norm_act_backward  g = dropped(dy) act'(z);  w = g gamma;
+//                                 dx = rstd (w - mean(w) - n mean(w n));
+//                                 dgamma = sum g n;  dbeta = sum g
+//
+// Both directions are bound by the memory, in two launches each: sums over a
+// chunk of tokens and a slab of channels (whole groups, whole vectors of
+// eight) into a record per chunk and group; then the rows again, with the
+// records merged by every workgroup that needs them.  A thread keeps its eight
+// channels for all of its rows, so that their parameters stay in registers.
+// Nothing of the forward pass but mean and rstd is kept: z, the activation's
+// derivative and dropout's mask are computed again.
+
+#include <stdint.h>
+
+#include "../../include/pcpp.h"
+#include "args.h"
+#include "common.h"
+#include "dropout.h"
+#include "ff_act.h"
+#include "gemm.h"
+#include "rows8.h"
+
+#define PCPP_EXPORT extern "C" __attribute__((visibility("default")))
+
+namespace pcpp {
+
+namespace {
+
+constexpr int kMaxThreads = 512;
+constexpr int kMaxGroups = 256;
+constexpr int kMaxChunks = 64;
+
+// How a launch cuts [B, N, C]: slabs of S channels (whole groups), chunks of
+// tokens; a thread holds one vector of V in a row, RP rows side by side.
+struct Cut {
+    int32_t B, N, C, G;
+    int32_t cg;       // channels of a group
+    int32_t S, V, RP, gs;
+    int32_t chunks;   // of the launch that sums
+    int32_t threads;
+};
+
+struct NormActParams {
+    const void* x;
+    const void* dy;      // backward
+    const bf16* gamma;
+    const bf16* beta;
+    void* y;             // forward's y, backward's dx
+    float* stats;        // [B][G][2] mean, rstd: forward writes it (or null), backward reads it
+    float* records;      // forward [B][chunks][G][3] count, mean, M2; backward [B][chunks][G][2] sums of w, w n
+    float* columns;      // backward: [2][B * chunks][C] sums of g n and g, or null
+    bf16* dgamma;
+    bf16* dbeta;
+    Dropout drop;
+    Cut cut;
+    int32_t apply_blocks;  // workgroups of the apply launch that apply, per slab and image
+    float eps;
+};
+
+// Row lane, vector and channel of a thread; false for the threads left over.
+struct Place {
+    int r, v, c0;
+    bool in;
+};
+__device__ __forceinline__ Place place_of(const Cut& a, int slab) {
+    const int r = threadIdx.x / a.V, v = threadIdx.x - r * a.V;
+    return Place{r, v, slab * a.S + 8 * v, r < a.RP};
+}
+
+// The sum of v over T consecutive lanes (a power of two up to a wavefront), in
+// each of them.
+__device__ __forceinline__ float lanes_sum(float v, int T) {
+    for (int d = 1; d < T; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+// Lanes that share a group of the slab.
+__device__ __forceinline__ int group_lanes(int threads, int gs) {
+    int t = 1;
+    while (2 * t * gs <= threads && t < 64) t *= 2;
+    return t;
+}
+
+// ---- statistics ----
+
+// A thread's rows in runs of ROWS, each with its own mean and squared
+// deviations (two passes over registers), merged into the thread's by Chan et
+// al.'s update: no difference of large sums anywhere.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
+    __shared__ float lds_mean[kMaxThreads * 8], lds_m2[kMaxThreads * 8];
+    const Cut a = p.cut;
+    const int chunk = blockIdx.x, slab = blockIdx.y, b = blockIdx.z;
+    const int lo = (int)((int64_t)a.N * chunk / a.chunks), hi = (int)((int64_t)a.N * (chunk + 1) / a.chunks);
+    const Place at = place_of(a, slab);
+    const T* x = (const T*)p.x + (int64_t)b * a.N * a.C + at.c0;
+    float mean[8], m2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mean[e] = m2[e] = 0.f;
+    float n = 0.f;
+    if (at.in) {
+        for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
+            float v[ROWS][8];
+            int rows = 0;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+                if (t + i * a.RP < hi) {
+                    load8(x + (int64_t)(t + i * a.RP) * a.C, v[i]);
+                    rows = i + 1;
+                }
+            }
+            const float cnt = (float)rows, total = n + cnt;
+            const float share = cnt / total, both = n * share;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float s = 0.f, q = 0.f;
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) s += v[i][e];
+                const float m = s / cnt;
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    const float d = i < rows ? v[i][e] - m : 0.f;
+                    q = __builtin_fmaf(d, d, q);
+                }
+                const float d = m - mean[e];
+                mean[e] = __builtin_fmaf(d, share, mean[e]);
+                m2[e] += __builtin_fmaf(d * d, both, q);
+            }
+            n = total;
+        }
+        store8(lds_mean + at.r * a.S + 8 * at.v, mean);
+        store8(lds_m2 + at.r * a.S + 8 * at.v, m2);
+    }
+    __syncthreads();
+    // A group's entries: RP row lanes of its channels.
+    const int T_ = group_lanes(a.threads, a.gs);
+    const int g = threadIdx.x / T_, l = threadIdx.x % T_;
+    const bool mine = g < a.gs;
+    const int entries = mine ? a.RP * a.cg : 0;
+    auto rows_of = [&](int r) { return (float)max(0, (hi - lo - r + a.RP - 1) / a.RP); };
+    float sum = 0.f;
+    for (int i = l; i < entries; i += T_) {
+        const int r = i / a.cg, c = g * a.cg + i - r * a.cg;
+        sum = __builtin_fmaf(rows_of(r), lds_mean[r * a.S + c], sum);
+    }
+    const float count = (float)(hi - lo) * (float)a.cg;
+    const float gm = lanes_sum(sum, T_) / count;
+    float q = 0.f;
+    for (int i = l; i < entries; i += T_) {
+        const int r = i / a.cg, c = g * a.cg + i - r * a.cg;
+        const float d = lds_mean[r * a.S + c] - gm;
+        q += __builtin_fmaf(d * d, rows_of(r), lds_m2[r * a.S + c]);
+    }
+    q = lanes_sum(q, T_);
+    if (mine && l == 0) {
+        float* o = p.records + (((int64_t)b * a.chunks + chunk) * a.G + slab * a.gs + g) * 3;
+        o[0] = count;
+        o[1] = gm;
+        o[2] = q;
+    }
+}
+
+// ---- forward ----
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z, float* grad) {
+    if constexpr (ACT == PCPP_ACT_NONE) {
+        if (grad) *grad = 1.f;
+        return z;
+    } else {
+        return ff_act<ACT>(z, grad);
+    }
+}
+
+template <typename T, int ACT, int ROWS>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_apply(NormActParams p) {
+    __shared__ float g_mean[kMaxGroups], g_rstd[kMaxGroups];
+    const Cut a = p.cut;
+    const int slab = blockIdx.y, b = blockIdx.z;
+    {
+        const int T_ = group_lanes(a.threads, a.gs);
+        const int g = threadIdx.x / T_, l = threadIdx.x % T_;
+        const bool mine = g < a.gs;
+        const float* rec = p.records + ((int64_t)b * a.chunks * a.G + slab * a.gs + (mine ? g : 0)) * 3;
+        float sum = 0.f, q = 0.f;
+        const float count = (float)a.N * (float)a.cg;
+        for (int i = l; i < a.chunks; i += T_) sum = __builtin_fmaf(rec[(int64_t)i * a.G * 3], rec[(int64_t)i * a.G * 3 + 1], sum);
+        const float m = lanes_sum(sum, T_) / count;
+        for (int i = l; i < a.chunks; i += T_) {
+            const float* o = rec + (int64_t)i * a.G * 3;
+            const float d = o[1] - m;
+            q += __builtin_fmaf(d * d, o[0], o[2]);
+        }
+        q = lanes_sum(q, T_);
+        if (mine && l == 0) {
+            const float rstd = 1.f / sqrtf(q / count + p.eps);
+            g_mean[g] = m;
+            g_rstd[g] = rstd;
+            if (p.stats != nullptr && blockIdx.x == 0) {
+                float* o = p.stats + ((int64_t)b * a.G + slab * a.gs + g) * 2;
+                o[0] = m;
+                o[1] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    const Place at = place_of(a, slab);
+    if (!at.in) return;
+    float mean[8], rstd[8], gamma[8], beta[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int g = (8 * at.v + e) / a.cg;
+        mean[e] = g_mean[g];
+        rstd[e] = g_rstd[g];
+    }
+    load8(p.gamma + at.c0, gamma);
+    load8(p.beta + at.c0, beta);
+    const DropoutKey key = dropout_key(p.drop);
+    const int lo = (int)((int64_t)a.N * blockIdx.x / p.apply_blocks), hi = (int)((int64_t)a.N * (blockIdx.x + 1) / p.apply_blocks);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
+        float v[ROWS][8];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (t + i * a.RP < hi) load8((const T*)p.x + base + (int64_t)(t + i * a.RP) * a.C, v[i]);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (t + i * a.RP >= hi) break;
+            const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[i][e] = act_of<ACT>(__builtin_fmaf((v[i][e] - mean[e]) * rstd[e], gamma[e], beta[e]), nullptr);
+            if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, v[i]);
+            store8((T*)p.y + o, v[i]);
+        }
+    }
+}
+
+// ---- backward ----
+
+// g and n of eight channels of a row: v holds x, d holds dy.
+template <int ACT>
+__device__ __forceinline__ void grad8(const NormActParams& p, const DropoutKey& key, int64_t o, const float (&mean)[8],
+                                      const float (&rstd)[8], const float (&gamma)[8], const float (&beta)[8],
+                                      float (&v)[8], float (&d)[8]) {
+    if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = (v[e] - mean[e]) * rstd[e];
+        float da;
+        act_of<ACT>(__builtin_fmaf(v[e], gamma[e], beta[e]), &da);
+        d[e] *= da;
+    }
+}
+
+__device__ __forceinline__ void load_params(const NormActParams& p, const Place& at, int slab, int b, float (&mean)[8],
+                                            float (&rstd)[8], float (&gamma)[8], float (&beta)[8]) {
+    const Cut& a = p.cut;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float* s = p.stats + ((int64_t)b * a.G + slab * a.gs + (8 * at.v + e) / a.cg) * 2;
+        mean[e] = s[0];
+        rstd[e] = s[1];
+    }
+    load8(p.gamma + at.c0, gamma);
+    load8(p.beta + at.c0, beta);
+}
+
+template <typename T, int ACT, int ROWS>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_grad_sums(NormActParams p) {
+    __shared__ float lds_n[kMaxThreads * 8], lds_g[kMaxThreads * 8];
+    const Cut a = p.cut;
+    const int chunk = blockIdx.x, slab = blockIdx.y, b = blockIdx.z;
+    const int lo = (int)((int64_t)a.N * chunk / a.chunks), hi = (int)((int64_t)a.N * (chunk + 1) / a.chunks);
+    const Place at = place_of(a, slab);
+    if (at.in) {
+        float mean[8], rstd[8], gamma[8], beta[8], sn[8], sg[8];
+        load_params(p, at, slab, b, mean, rstd, gamma, beta);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sn[e] = sg[e] = 0.f;
+        const DropoutKey key = dropout_key(p.drop);
+        const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+        for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
+            float v[ROWS][8], d[ROWS][8];
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (t + i * a.RP < hi) {
+                    const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
+                    load8((const T*)p.x + o, v[i]);
+                    load8((const T*)p.dy + o, d[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (t + i * a.RP >= hi) break;
+                grad8<ACT>(p, key, base + (int64_t)(t + i * a.RP) * a.C, mean, rstd, gamma, beta, v[i], d[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sn[e] = __builtin_fmaf(d[i][e], v[i][e], sn[e]);
+                    sg[e] += d[i][e];
+                }
+            }
+        }
+        store8(lds_n + at.r * a.S + 8 * at.v, sn);
+        store8(lds_g + at.r * a.S + 8 * at.v, sg);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.S; c += a.threads) {
+        float tn = 0.f, tg = 0.f;
+        for (int r = 0; r < a.RP; ++r) {
+            tn += lds_n[r * a.S + c];
+            tg += lds_g[r * a.S + c];
+        }
+        if (p.columns != nullptr) {
+            float* o = p.columns + ((int64_t)b * a.chunks + chunk) * a.C + slab * a.S + c;
+            o[0] = tn;
+            o[(int64_t)a.B * a.chunks * a.C] = tg;
+        }
+        const float gamma = bf16_to_f32(p.gamma[slab * a.S + c]);
+        lds_n[c] = tn * gamma;  // row 0, which this thread alone has read
+        lds_g[c] = tg * gamma;
+    }
+    __syncthreads();
+    const int T_ = group_lanes(a.threads, a.gs);
+    const int g = threadIdx.x / T_, l = threadIdx.x % T_;
+    const bool mine = g < a.gs;
+    float s0 = 0.f, s1 = 0.f;
+    if (mine)
+        for (int c = l; c < a.cg; c += T_) {
+            s0 += lds_g[g * a.cg + c];
+            s1 += lds_n[g * a.cg + c];
+        }
+    s0 = lanes_sum(s0, T_);
+    s1 = lanes_sum(s1, T_);
+    if (mine && l == 0) {
+        float* o = p.records + (((int64_t)b * a.chunks + chunk) * a.G + slab * a.gs + g) * 2;
+        o[0] = s0;
+        o[1] = s1;
+    }
+}
+
+// dgamma and dbeta of 16 channels: the chunks' sums in a fixed order.
+__device__ __forceinline__ void column_totals(const NormActParams& p, int block, float* lds) {
+    const Cut& a = p.cut;
+    const int per = (a.C + 15) / 16, which = block / per;
+    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, lanes = a.threads >> 4;
+    const int c = 16 * (block - which * per) + l, rows = a.B * a.chunks;
+    const float* in = p.columns + (int64_t)which * rows * a.C;
+    float t = 0.f;
+    if (c < a.C)
+        for (int i = r; i < rows; i += lanes) t += in[(int64_t)i * a.C + c];
+    lds[17 * r + l] = t;
+    __syncthreads();
+    bf16* out = which ? p.dbeta : p.dgamma;
+    if (r == 0 && c < a.C && out != nullptr) {
+        float v = 0.f;
+        for (int i = 0; i < lanes; ++i) v += lds[17 * i + l];
+        out[c] = f32_to_bf16(v);
+    }
+}
+int column_blocks(const NormActParams& p) { return p.columns != nullptr ? 2 * ((p.cut.C + 15) / 16) : 0; }
+
+// blockIdx.x: apply_blocks x slabs x images, then the columns' totals.
+template <typename T, int ACT, int ROWS>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_grad_apply(NormActParams p) {
+    __shared__ float lds[17 * (kMaxThreads / 16)];
+    __shared__ float g_m0[kMaxGroups], g_m1[kMaxGroups];
+    const Cut a = p.cut;
+    const int slabs = a.C / a.S;
+    const int64_t applying = (int64_t)p.apply_blocks * slabs * a.B;
+    if (blockIdx.x >= applying) {
+        column_totals(p, (int)(blockIdx.x - applying), lds);
+        return;
+    }
+    const int part = (int)(blockIdx.x % p.apply_blocks), sb = (int)(blockIdx.x / p.apply_blocks);
+    const int slab = sb % slabs, b = sb / slabs;
+    {
+        const int T_ = group_lanes(a.threads, a.gs);
+        const int g = threadIdx.x / T_, l = threadIdx.x % T_;
+        const bool mine = g < a.gs;
+        const float* rec = p.records + ((int64_t)b * a.chunks * a.G + slab * a.gs + (mine ? g : 0)) * 2;
+        float s0 = 0.f, s1 = 0.f;
+        for (int i = l; i < a.chunks; i += T_) {
+            s0 += rec[(int64_t)i * a.G * 2];
+            s1 += rec[(int64_t)i * a.G * 2 + 1];
+        }
+        s0 = lanes_sum(s0, T_);
+        s1 = lanes_sum(s1, T_);
+        if (mine && l == 0) {
+            const float count = (float)a.N * (float)a.cg;
+            g_m0[g] = s0 / count;
+            g_m1[g] = s1 / count;
+        }
+    }
+    __syncthreads();
+    const Place at = place_of(a, slab);
+    if (!at.in) return;
+    float mean[8], rstd[8], gamma[8], beta[8], m0[8], m1[8];
+    load_params(p, at, slab, b, mean, rstd, gamma, beta);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int g = (8 * at.v + e) / a.cg;
+        m0[e] = g_m0[g];
+        m1[e] = g_m1[g];
+    }
+    const DropoutKey key = dropout_key(p.drop);
+    const int lo = (int)((int64_t)a.N * part / p.apply_blocks), hi = (int)((int64_t)a.N * (part + 1) / p.apply_blocks);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
+        float v[ROWS][8], d[ROWS][8];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (t + i * a.RP < hi) {
+                const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
+                load8((const T*)p.x + o, v[i]);
+                load8((const T*)p.dy + o, d[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (t + i * a.RP >= hi) break;
+            const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
+            grad8<ACT>(p, key, o, mean, rstd, gamma, beta, v[i], d[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[i][e] = rstd[e] * (__builtin_fmaf(d[i][e], gamma[e], -m0[e]) - v[i][e] * m1[e]);
+            store8((T*)p.y + o, d[i]);
+        }
+    }
+}
+
+int gcd_of(int a, int b) { return b == 0 ? a : gcd_of(b, a % b); }
+
+// Slabs as wide as still give the chip its workgroups.
+Cut cut_of(int B, int N, int C, int G) {
+    Cut best = {};
+    const int cg = C / G, least = 8 / gcd_of(8, cg);  // groups whose channels are whole vectors; divides G as 8 divides C
+    for (int gs = G; gs >= least; --gs) {
+        if (G % gs != 0 || gs % least != 0) continue;
+        Cut a = {B, N, C, G, cg, gs * cg, gs * cg / 8, 0, gs, 0, 256};
+        if (a.V > 256) a.threads = kMaxThreads;
+        a.RP = a.threads / a.V;
+        const int64_t fit = (N + 8 * a.RP - 1) / (8 * a.RP);
+        a.chunks = (int)(fit < kMaxChunks ? fit : kMaxChunks);
+        if (best.B != 0 && (a.V < 8 || 5 * a.V * a.RP < 4 * best.V * best.RP)) continue;
+        best = a;
+        if ((int64_t)B * (G / gs) * a.chunks >= 512) break;
+    }
+    return best;
+}
+
+// Rows of a thread of the apply launches: enough workgroups first.
+int apply_blocks_of(const Cut& a) {
+    const int64_t most = (a.N + 4 * a.RP - 1) / (4 * a.RP), slabs = (int64_t)a.B * (a.C / a.S);
+    int64_t n = (2048 + slabs - 1) / slabs;
+    n = n < most ? n : most;
+    return (int)(n > 0 ? n : 1);
+}
+
+int64_t stats_floats(const Cut& a) { return (int64_t)a.B * a.chunks * a.G * 3; }
+int64_t grad_floats(const Cut& a) { return (int64_t)a.B * a.chunks * (2 * (int64_t)a.C + 2 * a.G); }
+
+template <typename F>
+void with_act(int act, F f) {
+    using std::integral_constant;
+    if (act == PCPP_ACT_SILU) f(integral_constant<int, PCPP_ACT_SILU>());
+    else if (act == PCPP_ACT_GELU) f(integral_constant<int, PCPP_ACT_GELU>());
+    else f(integral_constant<int, PCPP_ACT_NONE>());
+}
+
+int check_geom(const pcpp_norm_act_geom_t* g) {
+    if (!g || g->reserved != 0) return PCPP_EINVAL;
+    if (g->batch < 1 || g->batch > 65535 || g->tokens < 1 || g->channels < 1 || g->groups < 1) return PCPP_EINVAL;
+    if (!(g->eps > 0.f) || !(g->drop >= 0.f && g->drop <= 1.f)) return PCPP_EINVAL;
+    if (g->dtype != PCPP_DTYPE_F32 && g->dtype != PCPP_DTYPE_BF16) return PCPP_ENOTSUP;
+    if (g->act != PCPP_ACT_GELU && g->act != PCPP_ACT_SILU && g->act != PCPP_ACT_NONE) return PCPP_ENOTSUP;
+    if (!gn_shapes_ok(g->channels, g->groups)) return PCPP_ENOTSUP;
+    if ((int64_t)g->batch * g->tokens > ((int64_t)1 << 36) / g->channels) return PCPP_EINVAL;
+    return PCPP_OK;
+}
+
+}  // namespace
+
+}  // namespace pcpp
+
+using namespace pcpp;
+
+PCPP_EXPORT size_t pcpp_group_norm_act_workspace_size(const pcpp_norm_act_geom_t* g) {
+    if (check_geom(g) != PCPP_OK) return 0;
+    const Cut a = cut_of(g->batch, g->tokens, g->channels, g->groups);
+    const int64_t f = stats_floats(a), b = grad_floats(a);
+    return (size_t)(f > b ? f : b) * sizeof(float);
+}
+
+PCPP_EXPORT int pcpp_group_norm_act(const pcpp_norm_act_geom_t* g, const void* x, const void* gamma, const void* beta,
+                                    const void* rng, uint64_t draw, void* y, float* stats, void* workspace,
+                                    size_t ws_bytes, void* stream) {
+    const int st = check_geom(g);
+    if (st != PCPP_OK) return st;
+    if (!x || !gamma || !beta || !y || (g->drop > 0.f && !rng)) return PCPP_EINVAL;
+    const void* ptrs[] = {x, gamma, beta, y};
+    for (const void* q : ptrs)
+        if (!aligned_to(q, 16)) return PCPP_EINVAL;
+    if (!aligned_to(stats, 4) || !aligned_to(rng, 8)) return PCPP_EINVAL;
+    if (!workspace || ws_bytes < pcpp_group_norm_act_workspace_size(g)) return PCPP_EWORKSPACE;
+    if (!aligned_to(workspace, 16)) return PCPP_EINVAL;
+    const int64_t n = (int64_t)g->batch * g->tokens * g->channels, size = g->dtype == PCPP_DTYPE_F32 ? 4 : 2;
+    const int64_t cb = 2 * (int64_t)g->channels, sb = 8 * (int64_t)g->batch * g->groups;
+    const Range out[] = {{y, n * size}, {stats, sb}, {workspace, (int64_t)pcpp_group_norm_act_workspace_size(g)}};
+    const Range in[] = {{x, n * size}, {gamma, cb}, {beta, cb}, {rng, 16}};
+    if (outputs_overlap(out, 3, in, 4)) return PCPP_EINVAL;
+    const Cut a = cut_of(g->batch, g->tokens, g->channels, g->groups);
+    NormActParams p = {};
+    p.x = x;
+    p.gamma = (const bf16*)gamma;
+    p.beta = (const bf16*)beta;
+    p.y = y;
+    p.stats = stats;
+    p.records = (float*)workspace;
+    p.drop = make_dropout(g->drop, rng, draw);
+    p.cut = a;
+    p.apply_blocks = apply_blocks_of(a);
+    p.eps = g->eps;
+    const hipStream_t s = (hipStream_t)stream;
+    const dim3 sums(a.chunks, a.C / a.S, a.B), apply(p.apply_blocks, a.C / a.S, a.B);
+    if (g->dtype == PCPP_DTYPE_F32)
+        norm_act_stats<float, 8><<<sums, a.threads, 0, s>>>(p);
+    else
+        norm_act_stats<bf16, 8><<<sums, a.threads, 0, s>>>(p);
+    if (hipGetLastError() != hipSuccess) return PCPP_EHIP;
+    with_act(g->act, [&](auto act) {
+        if (g->dtype == PCPP_DTYPE_F32)
+            norm_act_apply<float, act(), 4><<<apply, a.threads, 0, s>>>(p);
+        else
+            norm_act_apply<bf16, act(), 4><<<apply, a.threads, 0, s>>>(p);
+    });
+    return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}
+
+PCPP_EXPORT int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, const void* x, const void* gamma,
+                                             const void* beta, const float* stats, const void* rng, uint64_t draw,
+                                             const void* dy, void* dx, void* dgamma, void* dbeta, void* workspace,
+                                             size_t ws_bytes, void* stream) {
+    const int st = check_geom(g);
+    if (st != PCPP_OK) return st;
+    if (!x || !gamma || !beta || !stats || !dy || !dx || (g->drop > 0.f && !rng)) return PCPP_EINVAL;
+    const void* ptrs[] = {x, gamma, beta, dy, dx, dgamma, dbeta};
+    for (const void* q : ptrs)
+        if (!aligned_to(q, 16)) return PCPP_EINVAL;
+    if (!aligned_to(stats, 4) || !aligned_to(rng, 8)) return PCPP_EINVAL;
+    if (!workspace || ws_bytes < pcpp_group_norm_act_workspace_size(g)) return PCPP_EWORKSPACE;
+    if (!aligned_to(workspace, 16)) return PCPP_EINVAL;
+    const int64_t n = (int64_t)g->batch * g->tokens * g->channels, size = g->dtype == PCPP_DTYPE_F32 ? 4 : 2;
+    const int64_t cb = 2 * (int64_t)g->channels, sb = 8 * (int64_t)g->batch * g->groups;
+    // dx may replace dy: every element is read and written by one lane
+    const Range out[] = {{dx, n * size}, {dgamma, cb}, {dbeta, cb}, {workspace, (int64_t)pcpp_group_norm_act_workspace_size(g)}};
+    const Range in[] = {{x, n * size}, {gamma, cb}, {beta, cb}, {stats, sb}, {rng, 16}, {dy, n * size}};
+    if (outputs_overlap(out, 4, in, dx == dy ? 5 : 6)) return PCPP_EINVAL;
+    if (dx == dy && outputs_overlap(out + 1, 3, in + 5, 1)) return PCPP_EINVAL;
+    const Cut a = cut_of(g->batch, g->tokens, g->channels, g->groups);
+    NormActParams p = {};
+    p.x = x;
+    p.dy = dy;
+    p.gamma = (const bf16*)gamma;
+    p.beta = (const bf16*)beta;
+    p.y = dx;
+    p.stats = (float*)stats;
+    p.records = (float*)workspace;
+    p.columns = dgamma || dbeta ? (float*)workspace + (int64_t)a.B * a.chunks * 2 * a.G : nullptr;
+    p.dgamma = (bf16*)dgamma;
+    p.dbeta = (bf16*)dbeta;
+    p.drop = make_dropout(g->drop, rng, draw);
+    p.cut = a;
+    p.apply_blocks = apply_blocks_of(a);
+    const hipStream_t s = (hipStream_t)stream;
+    const dim3 sums(a.chunks, a.C / a.S, a.B);
+    const int64_t blocks = (int64_t)p.apply_blocks * (a.C / a.S) * a.B + column_blocks(p);
+    with_act(g->act, [&](auto act) {
+        if (g->dtype == PCPP_DTYPE_F32)
+            norm_act_grad_sums<float, act(), 4><<<sums, a.threads, 0, s>>>(p);
+        else
+            norm_act_grad_sums<bf16, act(), 4><<<sums, a.threads, 0, s>>>(p);
+    });
+    if (hipGetLastError() != hipSuccess) return PCPP_EHIP;
+    with_act(g->act, [&](auto act) {
+        if (g->dtype == PCPP_DTYPE_F32)
+            norm_act_grad_apply<float, act(), 4><<<(unsigned)blocks, a.threads, 0, s>>>(p);
+        else
+            norm_act_grad_apply<bf16, act(), 4><<<(unsigned)blocks, a.threads, 0, s>>>(p);
+    });
+    return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+}

@@ -1,0 +1,459 @@
+// Masked attention, forward: many queries (masked_forward), and few queries on
+// many keys (masked_few, masked_join).  See masked_attention.h for the
+// operands' layout.
+//
+// Scores are computed transposed, S^T = K Q^T, a query to a lane: its maximum,
+// its sum and its mask are a lane's own, and P^T is the operand of y^T = V^T P^T
+// as it stands.  The maximum is taken only when a lane's probabilities of 32
+// keys sum to 2^20 or more (or to no number): until then the one before serves.
+
+#include <type_traits>
+
+#include "masked_attention.h"
+
+namespace pcpp {
+
+using namespace masked;
+
+namespace {
+
+constexpr float P_LIMIT = 1048576.0f;
+constexpr int NW = 4;
+constexpr int NT = 64 * NW;
+constexpr int QB = 32 * NW;  // queries of a workgroup of masked_forward
+
+// A lane's query.
+struct Row {
+    int pos, limit, doc;  // limit: it sees no key from here on
+    float slope2;         // of the bias, log2 units
+};
+
+// Running maximum (log2 units), sum and result of the lanes' queries.
+template <int DB>
+struct State {
+    float m, l;
+    f32x16 o[DB];
+};
+template <int DB>
+__device__ __forceinline__ void clear(State<DB>& st) {
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[mb][r] = 0.f;
+}
+
+// 32 keys from key j0, rows row0 of the tiles in LDS.  partial: some query does
+// not see some key.  TWO: the probabilities as two bf16 (for few queries, where
+// the products cost nothing and a token's error counts).
+template <int DB, bool TWO>
+__device__ __forceinline__ void step(const Params& p, State<DB>& st, const bf16x8 (&q)[2 * DB], const Row& row,
+                                     const char* kt, const char* vt, const int* docs, int row0, int j0, bool partial,
+                                     bool careful, int lane) {
+    const int half = lane >> 5;
+    f32x16 s;
+#pragma unroll
+    for (int kk = 0; kk < 2 * DB; ++kk)
+        s = mfma32x32x16(row_operand<DB>(kt, row0, kk, lane), q[kk], kk == 0 ? f32x16{} : s);
+    float w[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = score(p, s[r]);
+    const int base = j0 + 4 * half;
+    if (row.slope2 != 0.f) {
+        const int d0 = row.pos - base;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = __builtin_fmaf(-row.slope2, (float)abs(d0 - (8 * (r >> 2) + (r & 3))), w[r]);
+    }
+    if (partial) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            i32x4 d = {};
+            if (p.kv_doc) d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool seen = base + 8 * g + e < row.limit && (!p.kv_doc || (d[e] == row.doc && d[e] >= 0));
+                w[4 * g + e] = seen ? w[4 * g + e] : -INFINITY;
+            }
+        }
+    }
+    float e[16], sum;
+    auto exps = [&](float mneg) __attribute__((always_inline)) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+            e[r] = fast_exp2(w[r] + mneg);
+            e[r + 1] = fast_exp2(w[r + 1] + mneg);
+            a += TWO ? e[r] : bf16_to_f32(f32_to_bf16(e[r]));
+            b += TWO ? e[r + 1] : bf16_to_f32(f32_to_bf16(e[r + 1]));
+        }
+        sum = a + b;
+    };
+    exps(-st.m);
+    if (__any(!(sum < P_LIMIT))) {
+        float mx = w[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, w[r]);
+        // (each query by its own sums: what others see is nothing to it)
+        const bool over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
+        const float m_new = over ? fmaxf(st.m, max_halves(mx)) : st.m;
+        const float alpha = m_new == st.m ? 1.f : fast_exp2(st.m - m_new);
+        st.m = m_new;
+        st.l *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st.o[mb][r] *= alpha;
+        exps(m_new == -INFINITY ? 0.f : -m_new);
+    }
+    st.l += sum;
+    auto add = [&](const float (&x)[16]) __attribute__((always_inline)) {
+        if (careful && partial)
+            add_rows_careful<DB>(st.o, x, vt, row0, lane);
+        else
+            add_rows<DB>(st.o, x, vt, row0, lane);
+    };
+    add(e);
+    if constexpr (TWO) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[r] -= bf16_to_f32(f32_to_bf16(e[r]));
+        add(e);
+    }
+}
+
+template <int DB>
+__device__ __forceinline__ void load_query(const Params& p, const bf16* row, bool in, bf16x8 (&q)[2 * DB], int lane) {
+#pragma unroll
+    for (int kk = 0; kk < 2 * DB; ++kk) {
+        const int c = 16 * kk + 8 * (lane >> 5);
+        q[kk] = in && c < p.D ? *(const bf16x8*)(row + c) : bf16x8{};
+    }
+}
+
+__device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int head, int i, bool in) {
+    Row r;
+    r.pos = sq.pos0 + i;
+    r.limit = limit_of(p, sq, i);
+    r.doc = in && p.q_doc ? p.q_doc[(int64_t)b * p.nq + i] : -1;
+    r.slope2 = p.slopes ? p.slopes[head] * LOG2E : 0.f;
+    return r;
+}
+
+template <int DB>
+__global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_forward(Params p) {
+    using T = Tile<DB>;
+    __shared__ __attribute__((aligned(16))) char kt[T::BYTES], vt[T::BYTES];
+    __shared__ __attribute__((aligned(16))) int docs[TILE];
+    __shared__ int redo;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nqb = (p.nq + QB - 1) / QB;
+    const int bh = blockIdx.x / nqb, qb = blockIdx.x - bh * nqb;
+    const int b = bh / p.H, head = bh - b * p.H, kh = head / p.G;
+    const Seq sq = seq_of(p, b);
+    const int i0 = qb * QB, last = min(i0 + QB, p.nq) - 1;
+    const int w0 = i0 + 32 * wave, wlast = min(w0 + 32, p.nq) - 1;  // the wavefront's queries (w0 > wlast: none)
+    const int i = w0 + (lane & 31);
+    const bool in = i < p.nq;
+    const Row row = row_of(p, sq, b, head, i, in);
+    bf16x8 q[2 * DB];
+    load_query<DB>(p, p.q + b * p.q_batch + (int64_t)min(i, p.nq - 1) * p.q_row + head * p.D, in, q, lane);
+
+    DocRange all = {}, mine = {};
+    if (p.kv_doc) {
+        mine = range_of_lanes(row.doc, in);
+        const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
+        all = r[0];
+        if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+    }
+    const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
+    const int end = tiles_of(limit_of(p, sq, last));
+    const int lim_lo = limit_of(p, sq, w0), lim_hi = w0 <= wlast ? limit_of(p, sq, wlast) : 0;
+    auto next = [&](int t) {
+        if (p.kv_doc)
+            while (t < end && !ranges_meet(ranges[t], all)) ++t;
+        return t;
+    };
+
+    // Staging: DB vectors of K and of V a thread.
+    u32x4 kr[DB], vr[DB];
+    int dr = -1;
+    const bf16* kb = p.k + b * p.k_batch + kh * p.D;
+    const bf16* vb = p.v + b * p.v_batch + kh * p.D;
+    auto load = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < DB; ++u) {
+            const int id = tid + NT * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
+            const int j = t * TILE + r;
+            const bool ok = j < sq.len && c < p.D;
+            kr[u] = ok ? *(const u32x4*)(kb + j * p.k_row + c) : u32x4{};
+            vr[u] = ok ? *(const u32x4*)(vb + j * p.v_row + c) : u32x4{};
+        }
+        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid] : -1;
+    };
+    auto store = [&]() {
+#pragma unroll
+        for (int u = 0; u < DB; ++u) {
+            const int id = tid + NT * u, r = id / T::VECS, c = id - r * T::VECS;
+            *(u32x4*)(kt + r * T::LD + 16 * c) = kr[u];
+            *(u32x4*)(vt + r * T::LD + 16 * c) = vr[u];
+        }
+        if (p.kv_doc && tid < TILE) docs[tid] = dr;
+    };
+
+    State<DB> st;
+    // Once; again with care where that left something that is no number.
+    for (int pass = 0; pass < 2; ++pass) {
+        clear(st);
+        int t = next(0);
+        if (t < end) load(t);
+        while (t < end) {
+            __syncthreads();
+            store();
+            __syncthreads();
+            const int tn = next(t + 1);
+            if (tn < end) load(tn);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const int j0 = t * TILE + 32 * h;
+                if (j0 >= lim_hi) continue;
+                const bool partial = j0 + 32 > lim_lo || (p.kv_doc && !same_document(ranges[t], mine));
+                step<DB, false>(p, st, q, row, kt, vt, docs, 32 * h, j0, partial, pass > 0, lane);
+            }
+            t = tn;
+        }
+        if (pass > 0) break;
+        __syncthreads();
+        if (tid == 0) redo = 0;
+        __syncthreads();
+        if (any_not_finite<DB>(st.o) && lane == 0) redo = 1;
+        __syncthreads();
+        if (!redo) break;
+    }
+
+    const float l = sum_halves(st.l);
+    if (!in) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16* out = p.y + b * p.y_batch + (int64_t)i * p.y_row + head * p.D + 4 * (lane >> 5);
+#pragma unroll
+    for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            if (32 * mb + 8 * g >= p.D) break;
+            bf16x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = f32_to_bf16(st.o[mb][4 * g + e] * inv);
+            *(bf16x4*)(out + 32 * mb + 8 * g) = v;
+        }
+    if (p.lse && lane < 32) p.lse[(int64_t)bh * p.nq + i] = l == 0.f ? -INFINITY : (st.m + log2f(l)) * LN2;
+}
+
+// ---- few queries ----
+//
+// Up to 32 rows (the queries of all heads that share a key head) to a
+// workgroup, which takes a piece of the keys; its wavefronts take tiles of 32
+// keys in turn, each through an LDS tile of its own without a barrier, and meet
+// at the end.
+
+constexpr int FEW_KEYS = 32;
+
+template <int DB>
+__global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_few(Params p) {
+    using T = Tile<DB>;
+    constexpr int HALF = FEW_KEYS * T::LD;
+    __shared__ __attribute__((aligned(16))) char lds[NW][2 * HALF];
+    __shared__ __attribute__((aligned(16))) int docs[NW][FEW_KEYS];
+    __shared__ float ml[NW][32][2];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int piece = blockIdx.x % p.pieces, rest = blockIdx.x / p.pieces;
+    const int rb = rest % p.row_blocks, bk = rest / p.row_blocks;
+    const int b = bk / p.KH, kh = bk - b * p.KH;
+    const Seq sq = seq_of(p, b);
+    const int rows = p.G * p.nq, rho = rb * MASKED_FEW_ROWS + col;
+    const bool in = rho < rows;
+    const int g = min(rho, rows - 1) / p.nq, i = min(rho, rows - 1) - g * p.nq, head = kh * p.G + g;
+    const Row row = row_of(p, sq, b, head, i, true);
+    bf16x8 q[2 * DB];
+    load_query<DB>(p, p.q + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, true, q, lane);
+    DocRange mine = {};
+    if (p.kv_doc) mine = range_of_lanes(row.doc, true);
+    const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
+    const int lim_lo = limit_of(p, sq, 0), lim_hi = limit_of(p, sq, p.nq - 1);
+    const int tiles = (lim_hi + FEW_KEYS - 1) / FEW_KEYS;
+    const int t0 = (int)((int64_t)tiles * piece / p.pieces), t1 = (int)((int64_t)tiles * (piece + 1) / p.pieces);
+    char *kt = lds[wave], *vt = lds[wave] + HALF;
+    auto next = [&](int t) {
+        if (p.kv_doc)
+            while (t < t1 && !ranges_meet(ranges[t / 2], mine)) t += NW;
+        return t;
+    };
+
+    constexpr int PER = FEW_KEYS * T::VECS / 64;  // vectors of K and of V a lane
+    u32x4 kr[PER], vr[PER];
+    int dr = -1;
+    const bf16* kb = p.k + b * p.k_batch + kh * p.D;
+    const bf16* vb = p.v + b * p.v_batch + kh * p.D;
+    auto load = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int id = lane + 64 * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
+            const int j = t * FEW_KEYS + r;
+            const bool ok = j < sq.len && c < p.D;
+            kr[u] = ok ? *(const u32x4*)(kb + j * p.k_row + c) : u32x4{};
+            vr[u] = ok ? *(const u32x4*)(vb + j * p.v_row + c) : u32x4{};
+        }
+        if (p.kv_doc) dr = lane < FEW_KEYS && t * FEW_KEYS + lane < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * FEW_KEYS + lane] : -1;
+    };
+    auto store = [&]() {
+        __builtin_amdgcn_wave_barrier();  // the tile before has been read (LDS works in order)
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int id = lane + 64 * u, r = id / T::VECS, c = id - r * T::VECS;
+            *(u32x4*)(kt + r * T::LD + 16 * c) = kr[u];
+            *(u32x4*)(vt + r * T::LD + 16 * c) = vr[u];
+        }
+        if (p.kv_doc && lane < FEW_KEYS) docs[wave][lane] = dr;
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    State<DB> st;
+    for (int pass = 0; pass < 2; ++pass) {
+        clear(st);
+        int t = next(t0 + wave);
+        if (t < t1) load(t);
+        while (t < t1) {
+            store();
+            const int tn = next(t + NW);
+            if (tn < t1) load(tn);
+            const int j0 = t * FEW_KEYS;
+            const bool partial = j0 + FEW_KEYS > lim_lo || (p.kv_doc && !same_document(ranges[t / 2], mine));
+            step<DB, true>(p, st, q, row, kt, vt, docs[wave], 0, j0, partial, pass > 0, lane);
+            t = tn;
+        }
+        if (pass > 0 || !any_not_finite<DB>(st.o)) break;
+    }
+
+    // The wavefronts' results on one maximum, and their sum.
+    const float l = sum_halves(st.l);
+    if (lane < 32) {
+        ml[wave][col][0] = st.m;
+        ml[wave][col][1] = l;
+    }
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[w][col][0]);
+    auto factor = [](float mw, float m) { return mw == -INFINITY ? 0.f : mw == m ? 1.f : fast_exp2(mw - m); };
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) total = __builtin_fmaf(ml[w][col][1], factor(ml[w][col][0], m), total);
+    const float f = factor(st.m, m);
+    float* o = (float*)lds[wave];  // [register][lane]; 64 KB a workgroup at most, as its tiles
+    static_assert(DB * 16 * 64 * 4 <= 2 * HALF, "results in the tiles' place");
+#pragma unroll
+    for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[(16 * mb + r) * 64 + lane] = f == 0.f ? 0.f : st.o[mb][r] * f;
+    __syncthreads();
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int u = 0; u < 4 * DB; ++u) {
+        const int reg = NW * u + wave;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += ((const float*)lds[w])[reg * 64 + lane];
+        if (p.pieces > 1) {
+            p.part_o[((int64_t)blockIdx.x * (16 * DB) + reg) * 64 + lane] = v;
+        } else {
+            const int c = 32 * (reg >> 4) + 8 * ((reg & 15) >> 2) + 4 * (lane >> 5) + (reg & 3);
+            if (in && c < p.D) p.y[b * p.y_batch + (int64_t)i * p.y_row + head * p.D + c] = f32_to_bf16(v * inv);
+        }
+    }
+    if (wave == 0 && lane < 32) {
+        if (p.pieces > 1) {
+            float* pml = p.part_ml + ((int64_t)blockIdx.x * 32 + col) * 2;
+            pml[0] = m;
+            pml[1] = total;
+        } else if (p.lse && in) {
+            p.lse[((int64_t)b * p.H + head) * p.nq + i] = total == 0.f ? -INFINITY : (m + log2f(total)) * LN2;
+        }
+    }
+}
+
+// The pieces of 32 rows joined: a workgroup takes four of the 16 DB registers'
+// worth of results.
+template <int DB>
+__global__ __launch_bounds__(NT) void masked_join(Params p) {
+    const int lane = threadIdx.x & 63, col = lane & 31;
+    const int part = blockIdx.x % (4 * DB), rest = blockIdx.x / (4 * DB);
+    const int reg = 4 * part + (threadIdx.x >> 6);
+    const int rb = rest % p.row_blocks, bk = rest / p.row_blocks;
+    const int b = bk / p.KH, kh = bk - b * p.KH;
+    const float* po = p.part_o + ((int64_t)rest * p.pieces * (16 * DB) + reg) * 64 + lane;
+    const float* pml = p.part_ml + ((int64_t)rest * p.pieces * 32 + col) * 2;
+    float m = -INFINITY;
+    for (int k = 0; k < p.pieces; ++k) m = fmaxf(m, pml[(int64_t)k * 64]);
+    float v = 0.f, total = 0.f;
+    for (int k = 0; k < p.pieces; ++k) {
+        const float mk = pml[(int64_t)k * 64];
+        if (mk == -INFINITY) continue;
+        const float f = mk == m ? 1.f : fast_exp2(mk - m);
+        total = __builtin_fmaf(pml[(int64_t)k * 64 + 1], f, total);
+        v = __builtin_fmaf(po[(int64_t)k * (16 * DB * 64)], f, v);
+    }
+    const int rows = p.G * p.nq, rho = rb * MASKED_FEW_ROWS + col;
+    if (rho >= rows) return;
+    const int g = rho / p.nq, i = rho - g * p.nq, head = kh * p.G + g;
+    const int c = 32 * (reg >> 4) + 8 * ((reg & 15) >> 2) + 4 * (lane >> 5) + (reg & 3);
+    if (c < p.D) p.y[b * p.y_batch + (int64_t)i * p.y_row + head * p.D + c] = f32_to_bf16(total == 0.f ? 0.f : v / total);
+    if (p.lse && reg == 0 && lane < 32)
+        p.lse[((int64_t)b * p.H + head) * p.nq + i] = total == 0.f ? -INFINITY : (m + log2f(total)) * LN2;
+}
+
+// Ranges of the documents of 64 tokens each, a wavefront to a tile; the
+// queries' tiles first, then the keys'.
+__global__ __launch_bounds__(NT) void masked_ranges(Params p) {
+    const int lane = threadIdx.x & 63;
+    const int nq = tiles_of(p.nq), nkv = tiles_of(p.nkv);
+    const int64_t t = (int64_t)blockIdx.x * NW + (threadIdx.x >> 6);
+    if (t >= (int64_t)p.B * (nq + nkv)) return;
+    const bool keys = t >= (int64_t)p.B * nq;
+    const int64_t u = keys ? t - (int64_t)p.B * nq : t;
+    const int per = keys ? nkv : nq, n = keys ? p.nkv : p.nq;
+    const int b = (int)(u / per), i = (int)(u - (int64_t)b * per) * TILE + lane;
+    const int32_t* doc = keys ? p.kv_doc : p.q_doc;
+    const DocRange r = range_of_lanes(i < n ? doc[(int64_t)b * n + i] : 0, i < n);
+    if (lane == 0) (keys ? p.kv_range : p.q_range)[u] = r;
+}
+
+}  // namespace
+
+hipError_t launch_masked_ranges(const Params& p, hipStream_t s) {
+    const int64_t t = (int64_t)p.B * (tiles_of(p.nq) + tiles_of(p.nkv));
+    masked_ranges<<<(unsigned)((t + NW - 1) / NW), NT, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_masked_forward(const Params& p, hipStream_t s) {
+    const int64_t blocks = (int64_t)p.B * p.H * ((p.nq + QB - 1) / QB);
+    return with_blocks(p.D, [&](auto db) {
+        masked_forward<db()><<<(unsigned)blocks, NT, 0, s>>>(p);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_masked_few(const Params& p, hipStream_t s) {
+    const int64_t groups = (int64_t)p.B * p.KH * p.row_blocks;
+    return with_blocks(p.D, [&](auto db) {
+        masked_few<db()><<<(unsigned)(groups * p.pieces), NT, 0, s>>>(p);
+        if (p.pieces > 1) {
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            masked_join<db()><<<(unsigned)(groups * 4 * db()), NT, 0, s>>>(p);
+        }
+        return hipGetLastError();
+    });
+}
+
+}  // namespace pcpp

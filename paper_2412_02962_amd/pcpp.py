@@ -140,6 +140,30 @@ class pcpp_ff_grads_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in FF_PTR_FIELDS]
 
 
+PCPP_ACT_NONE = 2
+
+
+class pcpp_norm_act_geom_t(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("channels", ctypes.c_int32), ("groups", ctypes.c_int32),
+        ("act", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("drop", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class pcpp_masked_geom_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q", "n_kv", "heads", "kv_heads", "head_dim", "causal")] + [
+        ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("q_row", "k_row", "v_row", "y_row", "q_batch", "k_batch", "v_batch", "y_batch")]
+
+
+MASK_PTR_FIELDS = ("kv_len", "q_pos", "prefix", "q_doc", "kv_doc", "slopes")
+
+
+class pcpp_mask_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in MASK_PTR_FIELDS]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built: run __graft_entry__.build() "
@@ -150,6 +174,8 @@ def _load():
     wp = ctypes.POINTER(pcpp_block_weights_t)
     i32p = ctypes.POINTER(ctypes.c_int32)
     fp, fwp = ctypes.POINTER(pcpp_ff_geom_t), ctypes.POINTER(pcpp_ff_weights_t)
+    np_, mp, mkp = (ctypes.POINTER(t) for t in (pcpp_norm_act_geom_t, pcpp_masked_geom_t, pcpp_mask_t))
+    u64 = ctypes.c_uint64
     sig = {
         "pcpp_version": (ctypes.c_int, []),
         "pcpp_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -200,6 +226,14 @@ def _load():
         "pcpp_gated_ff": (ctypes.c_int, [fp, fwp] + [vp] * 5 + [sz, vp]),
         "pcpp_gated_ff_backward_workspace_size": (sz, [fp]),
         "pcpp_gated_ff_backward": (ctypes.c_int, [fp, fwp] + [vp] * 6 + [ctypes.POINTER(pcpp_ff_grads_t), vp, sz, vp]),
+        "pcpp_dropout": (ctypes.c_int, [ctypes.c_int64, i32, i32, ctypes.c_float, vp, u64, vp, vp, vp, vp]),
+        "pcpp_group_norm_act_workspace_size": (sz, [np_]),
+        "pcpp_group_norm_act": (ctypes.c_int, [np_, vp, vp, vp, vp, u64, vp, vp, vp, sz, vp]),
+        "pcpp_group_norm_act_backward": (ctypes.c_int, [np_] + [vp] * 5 + [u64] + [vp] * 5 + [sz, vp]),
+        "pcpp_masked_attention_workspace_size": (sz, [mp]),
+        "pcpp_masked_attention": (ctypes.c_int, [mp, mkp] + [vp] * 6 + [sz, vp]),
+        "pcpp_masked_attention_backward_workspace_size": (sz, [mp]),
+        "pcpp_masked_attention_backward": (ctypes.c_int, [mp, mkp] + [vp] * 10 + [sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -224,6 +258,9 @@ EXPORTED = (
     "pcpp_checkpoint_save", "pcpp_checkpoint_load", "pcpp_rms_norm", "pcpp_rms_norm_backward_workspace_size",
     "pcpp_rms_norm_backward", "pcpp_gated_ff_workspace_size", "pcpp_gated_ff_plan", "pcpp_gated_ff",
     "pcpp_gated_ff_backward_workspace_size", "pcpp_gated_ff_backward",
+    "pcpp_dropout", "pcpp_group_norm_act_workspace_size", "pcpp_group_norm_act", "pcpp_group_norm_act_backward",
+    "pcpp_masked_attention_workspace_size", "pcpp_masked_attention", "pcpp_masked_attention_backward_workspace_size",
+    "pcpp_masked_attention_backward",
 )
 
 
@@ -591,3 +628,70 @@ def pcpp_gated_ff_backward(g, w, x, x_scales, pre_codes, pre_scales, dy, dx, gra
     _check("pcpp_gated_ff_backward", _lib.pcpp_gated_ff_backward(
         ctypes.byref(g), ctypes.byref(w), _ptr(x), _ptr(x_scales), _ptr(pre_codes), _ptr(pre_scales), _ptr(dy),
         _ptr(dx), None if grads is None else ctypes.byref(grads), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pcpp_dropout(n, x_dtype, y_dtype, p, rng, draw, x, residual, y, stream=None):
+    """rng: device int64 [2], the seed and the first stream."""
+    _check("pcpp_dropout", _lib.pcpp_dropout(n, x_dtype, y_dtype, p, _ptr(rng), draw, _ptr(x), _ptr(residual), _ptr(y),
+                                             _stream(stream)))
+
+
+def make_norm_act_geom(batch, tokens, channels, groups, act=PCPP_ACT_SILU, dtype=PCPP_DTYPE_BF16, eps=1e-5, drop=0.0,
+                       reserved=0) -> pcpp_norm_act_geom_t:
+    return pcpp_norm_act_geom_t(batch, tokens, channels, groups, act, dtype, eps, drop, reserved)
+
+
+def pcpp_group_norm_act_workspace_size(g) -> int:
+    return _lib.pcpp_group_norm_act_workspace_size(ctypes.byref(g))
+
+
+def pcpp_group_norm_act(g, x, gamma, beta, rng, draw, y, stats, workspace, ws_bytes, stream=None):
+    _check("pcpp_group_norm_act", _lib.pcpp_group_norm_act(
+        ctypes.byref(g), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(rng), draw, _ptr(y), _ptr(stats), _ptr(workspace),
+        ws_bytes, _stream(stream)))
+
+
+def pcpp_group_norm_act_backward(g, x, gamma, beta, stats, rng, draw, dy, dx, dgamma, dbeta, workspace, ws_bytes,
+                                 stream=None):
+    _check("pcpp_group_norm_act_backward", _lib.pcpp_group_norm_act_backward(
+        ctypes.byref(g), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(stats), _ptr(rng), draw, _ptr(dy), _ptr(dx),
+        _ptr(dgamma), _ptr(dbeta), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def make_masked_geom(batch, n_q, n_kv, heads, kv_heads, head_dim, causal=False, scale=None, cap=0.0, q_row=0, k_row=0,
+                     v_row=0, y_row=0, q_batch=0, k_batch=0, v_batch=0, y_batch=0, reserved=0) -> pcpp_masked_geom_t:
+    """scale None: 1 / sqrt(head_dim).  Rows and batches in elements, 0: contiguous."""
+    return pcpp_masked_geom_t(batch, n_q, n_kv, heads, kv_heads, head_dim, int(causal),
+                              head_dim ** -0.5 if scale is None else scale, cap, reserved, q_row, k_row, v_row, y_row,
+                              q_batch, k_batch, v_batch, y_batch)
+
+
+def make_mask(kv_len=None, q_pos=None, prefix=None, q_doc=None, kv_doc=None, slopes=None) -> pcpp_mask_t:
+    """Device tensors (int32; slopes float32) or None.  They have to outlive the calls."""
+    return pcpp_mask_t(*[_ptr(t) for t in (kv_len, q_pos, prefix, q_doc, kv_doc, slopes)])
+
+
+def _mask(m):
+    return None if m is None else ctypes.byref(m)
+
+
+def pcpp_masked_attention_workspace_size(g) -> int:
+    return _lib.pcpp_masked_attention_workspace_size(ctypes.byref(g))
+
+
+def pcpp_masked_attention(g, m, q, k, v, y, lse=None, workspace=None, ws_bytes=0, stream=None):
+    """m: a pcpp_mask_t or None."""
+    _check("pcpp_masked_attention", _lib.pcpp_masked_attention(
+        ctypes.byref(g), _mask(m), _ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse), _ptr(workspace), ws_bytes,
+        _stream(stream)))
+
+
+def pcpp_masked_attention_backward_workspace_size(g) -> int:
+    return _lib.pcpp_masked_attention_backward_workspace_size(ctypes.byref(g))
+
+
+def pcpp_masked_attention_backward(g, m, q, k, v, y, lse, dy, dq, dk, dv, workspace, ws_bytes, stream=None):
+    """m: a pcpp_mask_t or None."""
+    _check("pcpp_masked_attention_backward", _lib.pcpp_masked_attention_backward(
+        ctypes.byref(g), _mask(m), _ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse), _ptr(dy), _ptr(dq), _ptr(dk),
+        _ptr(dv), _ptr(workspace), ws_bytes, _stream(stream)))
