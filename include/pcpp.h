@@ -1007,7 +1007,8 @@ typedef struct {
     int32_t reserved;      /* must be 0                                      */
     /* Elements from a token to the next and from a sequence to the next, both
      * multiples of 8; 0: contiguous (heads * D, and tokens * the row).  A row
-     * is at least its heads * D; a gradient has the layout of its tensor. */
+     * is at least its heads * D and at most 2^24, the sequences' distances
+     * together at most 2^40; a gradient has the layout of its tensor. */
     int64_t q_row, k_row, v_row, y_row;
     int64_t q_batch, k_batch, v_batch, y_batch;
 } pcpp_masked_geom_t;

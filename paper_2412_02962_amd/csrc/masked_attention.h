@@ -13,6 +13,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace pcpp {
@@ -78,129 +80,268 @@ __device__ __forceinline__ bool same_document(const DocRange& a, const DocRange&
     return a.lo >= 0 && a.lo == a.hi && b.lo == a.lo && b.hi == a.lo;
 }
 
-// The score of q . k in log2 units before the bias; in `slope` its derivative
-// by z, 1 - tanh^2.  cap tanh(x) = cap - 2 cap / (e^2x + 1): right at both ends
-// without a test, off by 2^-23 of the cap in the middle.
-__device__ __forceinline__ float score(const Params& p, float dot, float* slope = nullptr) {
-    if (p.cap2 == 0.f) {
+// The score of q . k in log2 units before the bias, plus `add`; in `slope` a
+// quarter of its derivative by z, (1 - tanh^2) / 4 (without a cap: 1).
+// cap tanh(x) = cap - 2 cap / (e^2x + 1): right at both ends without a test,
+// off by 2^-23 of the cap in the middle.
+template <bool CAP>
+__device__ __forceinline__ float score(const Params& p, float dot, float add, float* slope = nullptr) {
+    if constexpr (!CAP) {
         if (slope) *slope = 1.f;
-        return dot * p.z_mul;
+        return __builtin_fmaf(dot, p.z_mul, add);
+    } else {
+        const float r = __builtin_amdgcn_rcpf(fast_exp2(dot * p.z_mul) + 1.f);
+        if (slope) *slope = __builtin_fmaf(-r, r, r);
+        return __builtin_fmaf(-2.f * p.cap2, r, p.cap2 + add);
     }
-    const float r = __builtin_amdgcn_rcpf(fast_exp2(dot * p.z_mul) + 1.f);
-    if (slope) *slope = 4.f * r * (1.f - r);
-    return __builtin_fmaf(-2.f * p.cap2, r, p.cap2);
 }
 
-// ---- tiles in LDS: rows of 32 DB channels and 16 bytes, which puts the rows
-// that a wavefront reads at once into different banks ----
+// ---- tiles in LDS: 64 rows of RB bytes, the channels behind a head's 0.  The
+// 16 bytes c of row r lie at c ^ swizzle(r): rows read at one channel by 32
+// lanes, and four rows of 32 bytes by the 16 lanes of a transposing read, then
+// lie in different banks.  The swizzle repeats every eight rows. ----
 
 template <int DB>
 struct Tile {
-    static constexpr int CH = 32 * DB;       // channels, those behind a head's 0
-    static constexpr int LD = CH * 2 + 16;   // bytes of a row
-    static constexpr int VECS = 4 * DB;      // vectors of eight of a row
-    static constexpr int BYTES = TILE * LD;
+    static constexpr int RB = DB <= 2 ? 128 : 256;  // bytes of a row
+    static constexpr int VECS = RB / 16;
+    static constexpr int BYTES = TILE * RB;
+    __device__ static __forceinline__ int swizzle(int r) { return RB == 128 ? ((r >> 1) & 3) << 1 : (r & 7) << 1; }
 };
 
-// Rows row0 + (lane % 32), channels 16 kk + 8 (lane / 32) ..: a product that
-// contracts channels.
-template <int DB>
-__device__ __forceinline__ bf16x8 row_operand(const char* tile, int row0, int kk, int lane) {
-    return *(const bf16x8*)(tile + (row0 + (lane & 31)) * Tile<DB>::LD + 32 * kk + 16 * (lane >> 5));
+// 16 bytes per lane from a wave-uniform base and a lane's offset straight into
+// LDS, lane l's at lds + 16 l.  In assembly, since the compiler's own tracking
+// of such writes would wait for all of them before any LDS read; the kernels
+// order them by landed() and barriers.
+__device__ __forceinline__ void load_lds(uint64_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    typedef __attribute__((address_space(3))) const void* lptr;
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr)p);
 }
 
-// Channel 32 mb + (lane % 32) of the 16 rows from row0, in the order of the
-// scores' registers: a product that contracts rows.  Two transposing reads of
-// four rows each for either half of the lanes.
-template <int DB>
-__device__ __forceinline__ bf16x8 column_operand(const char* tile, int row0, int mb, int lane) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int row = row0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
-    const int at = 32 * mb + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const char* a = tile + row * Tile<DB>::LD + 2 * at;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 8 * Tile<DB>::LD));
-    const short __attribute__((ext_vector_type(8))) w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(bf16x8, w);
-}
-
-// Eight registers as an operand.
-__device__ __forceinline__ bf16x8 packed(const float (&w)[16], int st) {
-    bf16x8 o;
+// Tiles of ROWS rows of one tensor: each of NW wavefronts brings its share of
+// the rows, 1 KB at a time.  Rows behind the tensor's last are copies of that
+// one (their weights are 0).
+template <int DB, int NW, int ROWS>
+struct Loader {
+    using T = Tile<DB>;
+    static constexpr int PIECES = ROWS * T::RB / 1024 / NW;
+    static constexpr int PIECE_ROWS = 1024 / T::RB;
+    static_assert(PIECES >= 1 && (T::RB == 128 || PIECES % 2 == 0), "shares");
+    uint32_t row_bytes;
+    uint32_t off[2];  // of the pieces of even and of odd number: their swizzles differ where a piece has four rows
+    int row, first;
+    bool in[2];
+    __device__ __forceinline__ Loader(int64_t row_elements, int D, int wave, int lane) {
+        row_bytes = (uint32_t)(2 * row_elements);
+        row = lane / T::VECS;
+        first = PIECES * wave;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = f32_to_bf16(w[8 * st + e]);
-    return o;
+        for (int i = 0; i < 2; ++i) {
+            const int c = (lane % T::VECS) ^ T::swizzle(row + i * PIECE_ROWS);
+            off[i] = (uint32_t)row * row_bytes + 16 * c;
+            in[i] = 8 * c < D;  // what the head does not have stays 0 in LDS
+        }
+    }
+    // Rows row0 .. of the tensor at `base`, which has `rows`, into the tile at `lds`.
+    __device__ __forceinline__ void issue(const bf16* base, int row0, int rows, uint32_t lds) const {
+        const uint64_t at = uniform64((uint64_t)(uintptr_t)base + (uint64_t)row0 * row_bytes);
+        if (row0 + ROWS <= rows) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int piece = first + i;
+                if (in[i & 1]) load_lds(at + (uint64_t)(piece * PIECE_ROWS) * row_bytes, off[i & 1], lds + 1024 * piece);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int piece = first + i, r = piece * PIECE_ROWS + row, last = rows - 1 - row0;
+                const uint32_t o = off[i & 1] + (uint32_t)(min(r, last) - row) * row_bytes;
+                if (in[i & 1]) load_lds(at, o, lds + 1024 * piece);
+            }
+        }
+    }
+};
+
+// A lane's addresses in a tile (of one slot; the slots' distance is a power of
+// two above the tile's bits).
+template <int DB>
+struct Reader {
+    using T = Tile<DB>;
+    uint32_t row_at, col_at;
+    __device__ __forceinline__ explicit Reader(int lane) {
+        const int r = lane & 31;
+        row_at = (uint32_t)(r * T::RB + 16 * (lane >> 5) + 16 * T::swizzle(r));
+        const int t = 4 * (lane >> 5) + ((lane & 15) >> 2), e = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        col_at = (uint32_t)(t * T::RB + 16 * ((e >> 3) ^ T::swizzle(t)) + 2 * (e & 7));
+    }
+    // The addresses of the reads that follow are worked out there, not kept in
+    // registers for the whole loop.
+    __device__ __forceinline__ Reader fresh() const {
+        Reader r = *this;
+        if constexpr (DB > 2) asm volatile("" : "+v"(r.row_at), "+v"(r.col_at));
+        return r;
+    }
+    // Rows row0 + (lane % 32), channels 16 kk + 8 (lane / 32) ..: a product
+    // that contracts channels.  row0 a multiple of 32.
+    __device__ __forceinline__ bf16x8 rows(const char* tile, int row0, int kk) const {
+        return *(const bf16x8*)(tile + row0 * T::RB + (row_at ^ (32 * kk)));
+    }
+    // Channel 32 mb + (lane % 32) of the 16 rows from row0, in the order of the
+    // scores' registers: a product that contracts rows.  Two transposing reads
+    // of four rows each for either half of the lanes.
+    __device__ __forceinline__ bf16x8 columns(const char* tile, int row0, int mb) const {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const char* a = tile + row0 * T::RB + (col_at ^ (64 * mb));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 8 * T::RB));
+        const short __attribute__((ext_vector_type(8))) w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8, w);
+    }
+};
+
+// 0 to the whole of a workgroup's tiles, where a head has fewer channels than
+// they do: what no load writes stays 0.
+__device__ __forceinline__ void clear_tiles(char* lds, int bytes, int threads) {
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * threads) *(u32x4*)(lds + i) = u32x4{};
+}
+
+// The tiles of a sequence that may hold documents of `all`, 64 looked over at a
+// time (a lane each: one by one, each look is a wait for memory); `mine` is the
+// wavefront's part of `all`.
+struct DocWindow {
+    const DocRange* ranges;
+    int end, base;
+    DocRange all, mine, r;
+    uint64_t meets;
+    bool on;
+    __device__ __forceinline__ void init(const DocRange* ranges_, int end_, const DocRange& all_, const DocRange& mine_, bool on_) {
+        ranges = ranges_, end = end_, base = -TILE, all = all_, mine = mine_, on = on_;
+        r = DocRange{0, -1};
+        meets = 0;
+    }
+    // The first tile from t on (end: none).
+    __device__ __forceinline__ int next(int t) {
+        if (!on) return t;
+        while (t < end) {
+            if (t >= base + TILE || t < base) {
+                base = t;
+                const int u = t + (int)(threadIdx.x & 63);
+                r = u < end ? ranges[u] : DocRange{0, -1};
+                meets = __ballot(ranges_meet(r, all));
+            }
+            const uint64_t m = meets >> (t - base);
+            if (m) return t + __builtin_ctzll(m);
+            t = base + TILE;
+        }
+        return end;
+    }
+    // Of a tile that next() has just returned: all of it and of the workgroup,
+    // or of the wavefront, one document; none of the wavefront's in it.
+    __device__ __forceinline__ DocRange range(int t) const {
+        return DocRange{__builtin_amdgcn_readlane(r.lo, t - base), __builtin_amdgcn_readlane(r.hi, t - base)};
+    }
+    __device__ __forceinline__ bool same_all(int t) const { return !on || (t < end && same_document(range(t), all)); }
+    __device__ __forceinline__ bool same(int t) const { return !on || (t < end && same_document(range(t), mine)); }
+    __device__ __forceinline__ bool apart(int t) const { return on && t < end && !ranges_meet(range(t), mine); }
+};
+
+// The workgroup's place in a list of n: neighbours in the list, which read the
+// same keys, run on one of the chip's eight parts with a cache of their own.
+constexpr int PARTS = 8;
+__device__ __forceinline__ int64_t place_in(int64_t n) {
+    const int64_t per = (n + PARTS - 1) / PARTS;
+    const int64_t id = (int64_t)(blockIdx.x % PARTS) * per + blockIdx.x / PARTS;
+    return blockIdx.x / PARTS < per && id < n ? id : -1;
+}
+inline unsigned blocks_for(int64_t n) { return (unsigned)((n + PARTS - 1) / PARTS * PARTS); }
+
+// Sixteen registers as two operands.
+__device__ __forceinline__ void pack(const float (&w)[16], bf16x8 (&o)[2]) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r >> 3][r & 7] = f32_to_bf16(w[r]);
 }
 
 // acc += sum over the 32 rows from row0 of (their weights) x (their channels).
 template <int DB>
-__device__ __forceinline__ void add_rows(f32x16 (&acc)[DB], const float (&w)[16], const char* tile, int row0, int lane) {
+__device__ __forceinline__ void add_rows(f32x16 (&acc)[DB], const bf16x8 (&w)[2], const Reader<DB>& rd, const char* tile,
+                                         int row0) {
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
-        const bf16x8 b = packed(w, st);
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int mb = 0; mb < DB; ++mb)
-            acc[mb] = mfma32x32x16(column_operand<DB>(tile, row0 + 16 * st, mb, lane), b, acc[mb]);
-    }
+        for (int mb = 0; mb < DB; ++mb) acc[mb] = mfma32x32x16(rd.columns(tile, row0 + 16 * st, mb), w[st], acc[mb]);
 }
 
-// The eight values of an operand, infinities and NaN as 0.
-__device__ __forceinline__ bf16x8 finite_only(bf16x8 v) {
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if ((w[e] & 0x00007f80u) == 0x00007f80u) w[e] &= 0xffff0000u;
-        if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
-    }
-    return __builtin_bit_cast(bf16x8, w);
-}
+// ---- infinities and NaN in rows that the mask hides from some lanes ----
+//
+// A product takes 0 x infinity from a row that a lane's weight of 0 hides.  So
+// a tile that some lane does not see all of is looked over when it has landed;
+// where it holds infinities or NaN (never, in a sound program), every lane
+// notes which of its sums they belong to, and they become 0 in LDS.
 
-// The same where some weights are 0 because the mask hides the row, and the row
-// may hold infinities or NaN: the product takes what is finite (bit for bit what
-// it takes without them), and what is not goes to the weights that are not 0,
-// value by value.
-template <int DB>
-__device__ __forceinline__ void add_rows_careful(f32x16 (&acc)[DB], const float (&w)[16], const char* tile, int row0,
-                                                 int lane) {
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-        const bf16x8 b = packed(w, st);
-#pragma unroll
-        for (int mb = 0; mb < DB; ++mb)
-            acc[mb] = mfma32x32x16(finite_only(column_operand<DB>(tile, row0 + 16 * st, mb, lane)), b, acc[mb]);
-    }
-#pragma unroll 1
-    for (int j = 0; j < 32; ++j) {
-        const int reg = 4 * (j >> 3) + (j & 3);
-        float x = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x = r == reg ? w[r] : x;
-        x = __shfl(x, (lane & 31) + 32 * ((j >> 2) & 1));
-#pragma unroll
-        for (int mb = 0; mb < DB; ++mb)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const bf16x4 c = *(const bf16x4*)(tile + (row0 + j) * Tile<DB>::LD + 2 * (32 * mb + 8 * g + 4 * (lane >> 5)));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = bf16_to_f32(c[e]), o = acc[mb][4 * g + e];
-                    acc[mb][4 * g + e] = x != 0.f && !(fabsf(v) < INFINITY) ? __builtin_fmaf(x, v, o) : o;
-                }
-            }
-    }
-}
-
-// Whether any lane of the wavefront holds a value that is no number.
-template <int DB>
-__device__ __forceinline__ bool any_not_finite(const f32x16 (&acc)[DB]) {
+// Sixteen bytes at a: whether there are any; and, `clean`, 0 in their place.
+__device__ __forceinline__ bool not_finite16(const char* a) {
+    const u32x4 w = *(const u32x4*)a;
     bool bad = false;
 #pragma unroll
-    for (int mb = 0; mb < DB; ++mb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) bad |= !(fabsf(acc[mb][r]) < INFINITY);
-    return __any(bad);
+    for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+    return bad;
 }
+__device__ __forceinline__ void make_finite16(char* a) {
+    u32x4 w = *(const u32x4*)a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+        if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
+    }
+    *(u32x4*)a = w;
+}
+
+// Which of a lane's sums take an infinity of either sign (NaN: both).
+template <int DB>
+struct Spoilt {
+    uint64_t plus, minus;
+    // The 32 rows from row0 of a tile; bit j of `seen`: the lane sees row j.
+    __device__ __forceinline__ void note(const char* tile, int row0, uint32_t seen, int lane) {
+#pragma unroll 1
+        for (int j = 0; j < 32; ++j) {
+            const bool sees = seen >> j & 1;
+#pragma unroll
+            for (int g = 0; g < 4 * DB; ++g) {
+                const int at = (row0 + j) * Tile<DB>::RB + 16 * (g ^ Tile<DB>::swizzle(j)) + 8 * (lane >> 5);
+                const u32x2 w = *(const u32x2*)(tile + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t h = w[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+                    const bool nan = (h & 0x7fffu) > 0x7f80u;
+                    plus |= (uint64_t)(sees && (nan || h == 0x7f80u)) << (4 * g + e);
+                    minus |= (uint64_t)(sees && (nan || h == 0xff80u)) << (4 * g + e);
+                }
+                __builtin_amdgcn_sched_barrier(0);  // few registers before speed here
+            }
+        }
+    }
+    __device__ __forceinline__ void put(f32x16 (&acc)[DB]) const {
+        if (!__any((plus | minus) != 0)) return;
+#pragma unroll
+        for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (plus >> (16 * mb + r) & 1) acc[mb][r] += INFINITY;
+                if (minus >> (16 * mb + r) & 1) acc[mb][r] -= INFINITY;
+            }
+    }
+};
 
 __device__ __forceinline__ float max_halves(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -234,15 +375,21 @@ hipError_t launch_masked_dkv(const masked::Params& p, hipStream_t s);
 
 constexpr int MASKED_FEW_ROWS = 32;  // rows (queries x heads of a key head) of a workgroup of launch_masked_few
 
-// f(head's channels in blocks of 32).
+// f(head's channels in blocks of 32, capped, biased).  Capped scores without a
+// bias take the biased form with slopes of 0: two operations of a dozen more.
 template <typename F>
-hipError_t with_blocks(int head_dim, F f) {
+hipError_t with_shape(const masked::Params& p, F f) {
     using std::integral_constant;
-    switch ((head_dim + 31) / 32) {
-        case 1: return f(integral_constant<int, 1>());
-        case 2: return f(integral_constant<int, 2>());
-        case 3: return f(integral_constant<int, 3>());
-        default: return f(integral_constant<int, 4>());
+    using std::bool_constant;
+    auto variant = [&](auto db) {
+        if (p.cap2 != 0.f) return f(db, bool_constant<true>(), bool_constant<true>());
+        return p.slopes ? f(db, bool_constant<false>(), bool_constant<true>()) : f(db, bool_constant<false>(), bool_constant<false>());
+    };
+    switch ((p.D + 31) / 32) {
+        case 1: return variant(integral_constant<int, 1>());
+        case 2: return variant(integral_constant<int, 2>());
+        case 3: return variant(integral_constant<int, 3>());
+        default: return variant(integral_constant<int, 4>());
     }
 }
 

@@ -20,7 +20,8 @@ using namespace masked;
 namespace {
 
 constexpr int kMaxTokens = 1 << 24;
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxBatch = (int64_t)1 << 40;  // elements
+constexpr int64_t kMaxRow = 1 << 24;             // 64 rows are less than 2^32 bytes
 
 // A tensor's rows in elements: [batch, tokens, width] at `row` and `batch`.
 struct Layout {
@@ -32,7 +33,7 @@ struct Layout {
 
 // The strides as given, or contiguous; false if they are not allowed.
 bool layout_of(int64_t row, int64_t batch, int B, int tokens, int width, Layout* o) {
-    if (row < 0 || batch < 0 || row > kMaxStride / tokens || batch > kMaxStride / B || row % 8 != 0 || batch % 8 != 0)
+    if (row < 0 || batch < 0 || row > kMaxRow || batch > kMaxBatch / B || row % 8 != 0 || batch % 8 != 0)
         return false;
     o->row = row == 0 ? width : row;
     if (o->row < width) return false;
@@ -221,7 +222,7 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
     const hipStream_t s = (hipStream_t)stream;
     if (p.kv_doc && launch_masked_ranges(p, s) != hipSuccess) return PCPP_EHIP;
     if (launch_masked_delta(p, s) != hipSuccess) return PCPP_EHIP;
+    if (launch_masked_dq(p, s) != hipSuccess) return PCPP_EHIP;  // dq, if wanted, and delta for what follows
     if (dk && launch_masked_dkv(p, s) != hipSuccess) return PCPP_EHIP;
-    if (dq && launch_masked_dq(p, s) != hipSuccess) return PCPP_EHIP;
     return PCPP_OK;
 }

@@ -4,6 +4,10 @@
 // scores again.  Two kernels that own what they write, and so no atomics, for
 // two more products than one that adds to dq from everywhere.  See
 // masked_attention.h for the operands' layout.
+//
+// delta_i = dy_i . y_i takes y as it was rounded; the sum over the keys of P (dP -
+// delta) is what it is off by, since that sum is 0.  masked_dq adds it up and
+// leaves the better delta to masked_dkv, which runs after it.
 
 #include <type_traits>
 
@@ -71,16 +75,18 @@ __device__ __forceinline__ void store_rows(bf16* row, const f32x16 (&acc)[DB], f
         }
 }
 
-template <int DB>
-__global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dq(Params p) {
+template <int DB, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     using T = Tile<DB>;
-    __shared__ __attribute__((aligned(16))) char kt[T::BYTES], vt[T::BYTES];
-    __shared__ __attribute__((aligned(16))) int docs[TILE];
-    __shared__ int redo;
+    constexpr int SLOT = 2 * T::BYTES;  // K, V
+    __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
+    __shared__ __attribute__((aligned(16))) int docs[2][TILE];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + BLOCK - 1) / BLOCK;
-    const int bh = blockIdx.x / nqb, qb = blockIdx.x - bh * nqb;
+    const int64_t id = place_in((int64_t)p.B * p.H * nqb);
+    if (id < 0) return;
+    const int bh = (int)(id / nqb), qb = nqb - 1 - (int)(id - (int64_t)bh * nqb);  // the longest first
     const int b = bh / p.H, head = bh - b * p.H, kh = head / p.G;
     const Seq sq = seq_of(p, b);
     const int i0 = qb * BLOCK, last = min(i0 + BLOCK, p.nq) - 1;
@@ -95,121 +101,146 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dq(Params p) {
     load_rows<DB>(p.q + b * p.q_batch + (int64_t)ic * p.q_row + head * p.D, in, p.D, q, lane);
     load_rows<DB>(p.dy + b * p.y_batch + (int64_t)ic * p.y_row + head * p.D, in, p.D, dy, lane);
 
-    DocRange all = {}, mine = {};
-    if (p.kv_doc) {
-        mine = range_of_lanes(doc, in);
-        const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
-        all = r[0];
-        if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
-    }
-    const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
     const int end = tiles_of(limit_of(p, sq, last));
     const int lim_lo = limit_of(p, sq, w0), lim_hi = w0 <= wlast ? limit_of(p, sq, wlast) : 0;
-    auto next = [&](int t) {
-        if (p.kv_doc)
-            while (t < end && !ranges_meet(ranges[t], all)) ++t;
-        return t;
-    };
-    u32x4 kr[DB], vr[DB];
-    int dr = -1;
+    const int least = limit_of(p, sq, i0);  // every query sees the keys before (documents apart)
+    DocWindow window;
+    {
+        DocRange all = {}, mine = {};
+        if (p.kv_doc) {
+            mine = range_of_lanes(doc, in);
+            const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
+            all = r[0];
+            if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+        }
+        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
+    }
+    const Loader<DB, NW, TILE> kload(p.k_row, p.D, wave, lane), vload(p.v_row, p.D, wave, lane);
+    const Reader<DB> reader(lane);
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
-    auto load = [&](int t) {
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
-            const int j = t * TILE + r;
-            const bool ok = j < sq.len && c < p.D;
-            kr[u] = ok ? *(const u32x4*)(kb + j * p.k_row + c) : u32x4{};
-            vr[u] = ok ? *(const u32x4*)(vb + j * p.v_row + c) : u32x4{};
-        }
+    const uint32_t lds0 = lds_address(lds);
+    int dr = -1;
+    auto issue = [&](int t, int slot) {
+        kload.issue(kb, t * TILE, sq.len, lds0 + slot * SLOT);
+        vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
         if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid] : -1;
     };
-    auto store = [&]() {
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = id - r * T::VECS;
-            *(u32x4*)(kt + r * T::LD + 16 * c) = kr[u];
-            *(u32x4*)(vt + r * T::LD + 16 * c) = vr[u];
-        }
-        if (p.kv_doc && tid < TILE) docs[tid] = dr;
-    };
+    if (p.D < 32 * DB) {
+        clear_tiles(lds, 2 * SLOT, NT);
+        __syncthreads();
+    }
 
     f32x16 acc[DB];
-    auto step = [&](int row0, int j0, bool partial, bool careful) __attribute__((always_inline)) {
+    float off = 0.f;  // sum of P (dP - delta)
+    auto step = [&](const char* kt, const int* dt, int row0, int j0, bool partial) __attribute__((always_inline)) {
+        const char* vt = kt + T::BYTES;
+        const Reader<DB> rd = reader.fresh();
         f32x16 s, dp;
 #pragma unroll
         for (int kk = 0; kk < 2 * DB; ++kk) {
-            s = mfma32x32x16(row_operand<DB>(kt, row0, kk, lane), q[kk], kk == 0 ? f32x16{} : s);
-            dp = mfma32x32x16(row_operand<DB>(vt, row0, kk, lane), dy[kk], kk == 0 ? f32x16{} : dp);
+            s = mfma32x32x16(rd.rows(kt, row0, kk), q[kk], kk == 0 ? f32x16{} : s);
+            dp = mfma32x32x16(rd.rows(vt, row0, kk), dy[kk], kk == 0 ? f32x16{} : dp);
         }
-        float w[16];
         const int base = j0 + 4 * half;
+        const float far = (float)(pos - base);
+        float w[16];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            i32x4 d = {};
-            if (partial && p.kv_doc) d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+        for (int r = 0; r < 16; ++r) {
+            float slope, x = score<CAP>(p, s[r], -lse2, &slope);
+            if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far - (float)(8 * (r >> 2) + (r & 3))), x);
+            w[r] = fast_exp2(x) * (dp[r] - delta);
+            if constexpr (CAP) dp[r] = slope;
+        }
+        if (partial) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * g + e;
-                float sl, x = score(p, s[r], &sl);
-                if (slope2 != 0.f) x = __builtin_fmaf(-slope2, (float)abs(pos - base - (8 * g + e)), x);
-                const float pr = fast_exp2(x - lse2);
-                const bool seen = !partial || (base + 8 * g + e < limit && (!p.kv_doc || (d[e] == doc && d[e] >= 0)));
-                w[r] = seen ? pr * (dp[r] - delta) * sl : 0.f;
+            for (int g = 0; g < 4; ++g) {
+                i32x4 d = {};
+                if (p.kv_doc) d = *(const i32x4*)(dt + row0 + 8 * g + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * g + e;
+                    const bool seen = 8 * g + e < limit - base && (!p.kv_doc || (d[e] == doc && d[e] >= 0));
+                    w[r] = seen ? w[r] : 0.f;
+                    if constexpr (CAP) dp[r] = seen ? dp[r] : 0.f;
+                }
             }
         }
-        if (careful && partial)
-            add_rows_careful<DB>(acc, w, kt, row0, lane);
-        else
-            add_rows<DB>(acc, w, kt, row0, lane);
+        bf16x8 o[2];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            off += w[r];
+            o[r >> 3][r & 7] = f32_to_bf16(CAP ? w[r] * dp[r] : w[r]);
+        }
+        add_rows<DB>(acc, o, rd, kt, row0);
     };
 
-    for (int pass = 0; pass < 2; ++pass) {
-        clear<DB>(acc);
-        int t = next(0);
-        if (t < end) load(t);
-        while (t < end) {
-            __syncthreads();
-            store();
-            __syncthreads();
-            const int tn = next(t + 1);
-            if (tn < end) load(tn);
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int j0 = t * TILE + 32 * h;
-                if (j0 >= lim_hi) continue;
-                step(32 * h, j0, j0 + 32 > lim_lo || (p.kv_doc && !same_document(ranges[t], mine)), pass > 0);
+    clear<DB>(acc);
+    int slot = 0, t = window.next(0);
+    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
+    Spoilt<DB> spoilt = {};
+    if (t < end) issue(t, slot);
+    while (t < end) {
+        landed();
+        if (p.kv_doc && tid < TILE) docs[slot][tid] = dr;
+        __syncthreads();  // the tile is there, and nobody reads the one before any more
+        const int tn = window.next(t + 1);
+        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
+        if (tn < end) issue(tn, slot ^ 1);
+        char* kt = lds + slot * SLOT;
+        if ((t + 1) * TILE > least || !same_all) {
+            bool bad = false;
+#pragma unroll
+            for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(kt + o + 16 * tid);
+            if (__syncthreads_or(bad)) {
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t seen = 0;
+                    for (int r = 0; r < 32; ++r) {
+                        const int jr = t * TILE + 32 * h + r, d = p.kv_doc ? docs[slot][32 * h + r] : 0;
+                        seen |= (uint32_t)(jr < limit && (!p.kv_doc || (d == doc && d >= 0))) << r;
+                    }
+                    spoilt.note(kt, 32 * h, seen, lane);
+                }
+                // (the scores are NaN or infinite with or without what is taken out)
+                __syncthreads();
+                for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(kt + o + 16 * tid);
+                __syncthreads();
             }
-            t = tn;
         }
-        if (pass > 0) break;
-        __syncthreads();
-        if (tid == 0) redo = 0;
-        __syncthreads();
-        if (any_not_finite<DB>(acc) && lane == 0) redo = 1;
-        __syncthreads();
-        if (!redo) break;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int j0 = t * TILE + 32 * h;
+            if (j0 >= lim_hi || apart) continue;
+            step(kt, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same);
+        }
+        t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
+        slot ^= 1;
     }
-    if (in) store_rows<DB>(p.dq + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, acc, p.scale, p.D, lane);
+    spoilt.put(acc);
+    off = sum_halves(off);
+    if (!in) return;
+    if (lane < 32) p.delta[(int64_t)bh * p.nq + i] = delta + off;
+    if (p.dq) store_rows<DB>(p.dq + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, acc, CAP ? 4.f * p.scale : p.scale, p.D, lane);
 }
 
-// What a tile's queries bring besides q and dy.
+// What a tile's queries bring besides q and dy; delta negative.
 struct QueryTile {
     float lse2[TILE], delta[TILE];
-    int limit[TILE], doc[TILE];
+    int doc[TILE];
 };
 
-template <int DB>
-__global__ __launch_bounds__(NT, 1) void masked_dkv(Params p) {
+template <int DB, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_dkv(Params p) {
     using T = Tile<DB>;
-    __shared__ __attribute__((aligned(16))) char qt[T::BYTES], gt[T::BYTES];
-    __shared__ __attribute__((aligned(16))) QueryTile rows;
-    __shared__ int redo;
+    constexpr int SLOT = 2 * T::BYTES;  // Q, dy
+    __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
+    __shared__ __attribute__((aligned(16))) QueryTile brought[2];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nkb = (p.nkv + BLOCK - 1) / BLOCK;
-    const int bk = blockIdx.x / nkb, kb = blockIdx.x - bk * nkb;
+    const int64_t id = place_in((int64_t)p.B * p.KH * nkb);
+    if (id < 0) return;
+    const int bk = (int)(id / nkb), kb = (int)(id - (int64_t)bk * nkb);
     const int b = bk / p.KH, kh = bk - b * p.KH;
     const Seq sq = seq_of(p, b);
     const int k0 = kb * BLOCK, klast = min(k0 + BLOCK, p.nkv) - 1;
@@ -217,142 +248,156 @@ __global__ __launch_bounds__(NT, 1) void masked_dkv(Params p) {
     const int j = w0 + (lane & 31);
     const bool in = j < p.nkv, live = j < sq.len;
     const int doc = live && p.kv_doc ? p.kv_doc[(int64_t)b * p.nkv + j] : -1;
+    // The queries that see key j by length, past and prefix: from .. nq - 1.
+    const int from = !live ? p.nq : !p.causal || j < sq.prefix ? 0 : min(max(j - sq.pos0, 0), p.nq);
     bf16x8 k[2 * DB], v[2 * DB];
     load_rows<DB>(p.k + b * p.k_batch + (int64_t)min(j, p.nkv - 1) * p.k_row + kh * p.D, live, p.D, k, lane);
     load_rows<DB>(p.v + b * p.v_batch + (int64_t)min(j, p.nkv - 1) * p.v_row + kh * p.D, live, p.D, v, lane);
 
-    DocRange all = {}, mine = {};
-    if (p.kv_doc) {
-        mine = range_of_lanes(doc, live);
-        const DocRange* r = p.kv_range + (int64_t)b * tiles_of(p.nkv) + k0 / TILE;
-        all = r[0];
-        if (klast / TILE > k0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
-    }
-    const DocRange* ranges = p.q_range + (int64_t)b * tiles_of(p.nq);
-    // The queries' limits grow: from the first that sees the block's first key.
     const int ntq = tiles_of(p.nq);
-    int first = 0;
+    int first = 0;  // tile of the first query that sees the block's first key
     if (p.causal && k0 >= sq.prefix) first = min(max(k0 - sq.pos0, 0), p.nq) / TILE;
     if (k0 >= sq.len) first = ntq;
-    const int tiles = ntq - min(first, ntq);  // of each head
-    const int steps = tiles * p.G;
-    auto next = [&](int t) {
-        if (p.kv_doc)
-            while (t < steps && !ranges_meet(ranges[first + t % tiles], all)) ++t;
-        return t;
-    };
-    u32x4 qr[DB], gr[DB];
+    DocWindow window;
+    {
+        DocRange all = {}, mine = {};
+        if (p.kv_doc) {
+            mine = range_of_lanes(doc, live);
+            const DocRange* r = p.kv_range + (int64_t)b * tiles_of(p.nkv) + k0 / TILE;
+            all = r[0];
+            if (klast / TILE > k0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+        }
+        window.init(p.q_range + (int64_t)b * ntq, ntq, all, mine, p.kv_doc != nullptr);
+    }
+    const Loader<DB, NW, TILE> qload(p.q_row, p.D, wave, lane), gload(p.y_row, p.D, wave, lane);
+    const Reader<DB> reader(lane);
+    const uint32_t lds0 = lds_address(lds);
     float lr = 0.f, er = 0.f;
-    int mr = 0, dr = -1;
-    auto load = [&](int t) {
-        const int g = t / tiles, i0 = (first + t - g * tiles) * TILE, head = kh * p.G + g;
-        const bf16* qb = p.q + b * p.q_batch + head * p.D;
-        const bf16* gb = p.dy + b * p.y_batch + head * p.D;
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
-            const int i = i0 + r;
-            const bool ok = i < p.nq && c < p.D;
-            qr[u] = ok ? *(const u32x4*)(qb + i * p.q_row + c) : u32x4{};
-            gr[u] = ok ? *(const u32x4*)(gb + i * p.y_row + c) : u32x4{};
-        }
+    int dr = -1;
+    auto issue = [&](int g, int t, int slot) {
+        const int head = kh * p.G + g;
+        qload.issue(p.q + b * p.q_batch + head * p.D, t * TILE, p.nq, lds0 + slot * SLOT);
+        gload.issue(p.dy + b * p.y_batch + head * p.D, t * TILE, p.nq, lds0 + slot * SLOT + T::BYTES);
         if (tid < TILE) {
-            const int i = i0 + tid;
-            const bool ok = i < p.nq;
+            const int i = min(t * TILE + tid, p.nq - 1);
             const int64_t at = ((int64_t)b * p.H + head) * p.nq + i;
-            lr = ok ? p.lse[at] * LOG2E : 0.f;
-            er = ok ? p.delta[at] : 0.f;
-            mr = ok ? limit_of(p, sq, i) : 0;
-            dr = ok && p.q_doc ? p.q_doc[(int64_t)b * p.nq + i] : -1;
+            lr = p.lse[at] * -LOG2E;
+            er = -p.delta[at];
+            if (p.q_doc) dr = p.q_doc[(int64_t)b * p.nq + i];
         }
     };
-    auto store = [&]() {
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = id - r * T::VECS;
-            *(u32x4*)(qt + r * T::LD + 16 * c) = qr[u];
-            *(u32x4*)(gt + r * T::LD + 16 * c) = gr[u];
-        }
-        if (tid < TILE) {
-            rows.lse2[tid] = lr;
-            rows.delta[tid] = er;
-            rows.limit[tid] = mr;
-            rows.doc[tid] = dr;
-        }
-    };
+    if (p.D < 32 * DB) {
+        clear_tiles(lds, 2 * SLOT, NT);
+        __syncthreads();
+    }
 
     f32x16 dk[DB], dv[DB];
-    auto step = [&](int row0, int i0, float slope2, bool partial, bool careful) __attribute__((always_inline)) {
+    auto step = [&](const char* qt, const QueryTile& rows, int row0, int i0, float slope2, bool partial) __attribute__((always_inline)) {
+        const char* gt = qt + T::BYTES;
+        const Reader<DB> rd = reader.fresh();
         f32x16 s, dp;
 #pragma unroll
-        for (int kk = 0; kk < 2 * DB; ++kk) {
-            s = mfma32x32x16(row_operand<DB>(qt, row0, kk, lane), k[kk], kk == 0 ? f32x16{} : s);
-            dp = mfma32x32x16(row_operand<DB>(gt, row0, kk, lane), v[kk], kk == 0 ? f32x16{} : dp);
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 d = *(const f32x4*)(rows.delta + row0 + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * g + e] = d[e];
         }
+#pragma unroll
+        for (int kk = 0; kk < 2 * DB; ++kk) {
+            s = mfma32x32x16(rd.rows(qt, row0, kk), k[kk], kk == 0 ? f32x16{} : s);
+            dp = mfma32x32x16(rd.rows(gt, row0, kk), v[kk], dp);
+        }
+        const int base = i0 + 4 * half;
+        const float far = (float)(sq.pos0 + base - j);
         float w[16], z[16];
-        const int d0 = sq.pos0 + i0 + 4 * half - j;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int at = row0 + 8 * g + 4 * half;
-            const f32x4 lse2 = *(const f32x4*)(rows.lse2 + at), delta = *(const f32x4*)(rows.delta + at);
-            i32x4 lim = {}, d = {};
-            if (partial) {
-                lim = *(const i32x4*)(rows.limit + at);
-                d = *(const i32x4*)(rows.doc + at);
-            }
+            const f32x4 lse2 = *(const f32x4*)(rows.lse2 + row0 + 8 * g + 4 * half);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * g + e;
-                float sl, x = score(p, s[r], &sl);
-                if (slope2 != 0.f) x = __builtin_fmaf(-slope2, (float)abs(d0 + 8 * g + e), x);
-                const bool seen = !partial || (j < lim[e] && (!p.kv_doc || (d[e] == doc && d[e] >= 0)));
-                const float pr = fast_exp2(x - lse2[e]);
-                w[r] = seen ? pr : 0.f;
-                z[r] = seen ? pr * (dp[r] - delta[e]) * sl : 0.f;
+                float slope, x = score<CAP>(p, s[r], lse2[e], &slope);
+                if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(far + (float)(8 * g + e)), x);
+                w[r] = fast_exp2(x);
+                z[r] = w[r] * dp[r];
+                if constexpr (CAP) z[r] *= slope;
             }
         }
-        if (careful && partial) {
-            add_rows_careful<DB>(dv, w, gt, row0, lane);
-            add_rows_careful<DB>(dk, z, qt, row0, lane);
-        } else {
-            add_rows<DB>(dv, w, gt, row0, lane);
-            add_rows<DB>(dk, z, qt, row0, lane);
+        if (partial) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                i32x4 d = {};
+                if (p.kv_doc) d = *(const i32x4*)(rows.doc + row0 + 8 * g + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * g + e;
+                    const bool seen = 8 * g + e >= from - base && 8 * g + e < p.nq - base && (!p.kv_doc || (d[e] == doc && d[e] >= 0));
+                    w[r] = seen ? w[r] : 0.f;
+                    z[r] = seen ? z[r] : 0.f;
+                }
+            }
         }
+        bf16x8 o[2];
+        pack(w, o);
+        add_rows<DB>(dv, o, rd, gt, row0);
+        pack(z, o);
+        add_rows<DB>(dk, o, rd, qt, row0);
     };
 
-    for (int pass = 0; pass < 2; ++pass) {
-        clear<DB>(dk);
-        clear<DB>(dv);
-        int t = next(0);
-        if (t < steps) load(t);
-        while (t < steps) {
-            __syncthreads();
-            store();
-            __syncthreads();
-            const int tn = next(t + 1);
-            if (tn < steps) load(tn);
-            const int g = t / tiles, tile = first + t - g * tiles;
-            const float slope2 = p.slopes ? p.slopes[kh * p.G + g] * LOG2E : 0.f;
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int i0 = tile * TILE + 32 * h;
-                if (i0 >= p.nq || w0 >= limit_of(p, sq, min(i0 + 31, p.nq - 1))) continue;
-                const bool partial = i0 + 32 > p.nq || w0 + 32 > limit_of(p, sq, i0) ||
-                                     (p.kv_doc && !same_document(ranges[tile], mine));
-                step(32 * h, i0, slope2, partial, pass > 0);
-            }
-            t = tn;
+    clear<DB>(dk);
+    clear<DB>(dv);
+    int slot = 0, g = 0, t = window.next(first);
+    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
+    Spoilt<DB> spoilt_k = {}, spoilt_v = {};
+    if (t >= ntq) g = p.G;  // no query sees the block
+    if (g < p.G) issue(g, t, slot);
+    while (g < p.G) {
+        landed();
+        if (tid < TILE) {
+            brought[slot].lse2[tid] = lr;
+            brought[slot].delta[tid] = er;
+            brought[slot].doc[tid] = dr;
         }
-        if (pass > 0) break;
-        __syncthreads();
-        if (tid == 0) redo = 0;
-        __syncthreads();
-        if ((any_not_finite<DB>(dk) || any_not_finite<DB>(dv)) && lane == 0) redo = 1;
-        __syncthreads();
-        if (!redo) break;
+        __syncthreads();  // the tile is there, and nobody reads the one before any more
+        int gn = g, tn = window.next(t + 1);
+        if (tn >= ntq) ++gn, tn = window.next(first);
+        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
+        if (gn < p.G) issue(gn, tn, slot ^ 1);
+        const float slope2 = BIAS && p.slopes ? p.slopes[kh * p.G + g] * LOG2E : 0.f;
+        char* qt = lds + slot * SLOT;
+        if ((t + 1) * TILE > p.nq || k0 + BLOCK > limit_of(p, sq, t * TILE) || !same_all) {
+            bool bad = false;
+#pragma unroll
+            for (int o = 0; o < SLOT; o += 16 * NT) bad |= not_finite16(qt + o + 16 * tid);
+            if (__syncthreads_or(bad)) {
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t seen = 0;
+                    for (int r = 0; r < 32; ++r) {
+                        const int i = t * TILE + 32 * h + r, d = brought[slot].doc[32 * h + r];
+                        seen |= (uint32_t)(i >= from && i < p.nq && (!p.kv_doc || (d == doc && d >= 0))) << r;
+                    }
+                    spoilt_k.note(qt, 32 * h, seen, lane);
+                    spoilt_v.note(qt + T::BYTES, 32 * h, seen, lane);
+                }
+                // (the scores, or dy . v, are NaN or infinite with or without what is taken out)
+                __syncthreads();
+                for (int o = 0; o < SLOT; o += 16 * NT) make_finite16(qt + o + 16 * tid);
+                __syncthreads();
+            }
+        }
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int i0 = t * TILE + 32 * h;
+            if (apart || i0 >= p.nq || w0 >= limit_of(p, sq, min(i0 + 31, p.nq - 1))) continue;
+            step(qt, brought[slot], 32 * h, i0, slope2, i0 + 32 > p.nq || w0 + 32 > limit_of(p, sq, i0) || !same);
+        }
+        g = gn, t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
+        slot ^= 1;
     }
+    spoilt_k.put(dk);
+    spoilt_v.put(dv);
     if (!in) return;
-    store_rows<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, dk, p.scale, p.D, lane);
+    store_rows<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, dk, CAP ? 4.f * p.scale : p.scale, p.D, lane);
     store_rows<DB>(p.dv + b * p.v_batch + (int64_t)j * p.v_row + kh * p.D, dv, 1.f, p.D, lane);
 }
 
@@ -366,16 +411,16 @@ hipError_t launch_masked_delta(const Params& p, hipStream_t s) {
 
 hipError_t launch_masked_dq(const Params& p, hipStream_t s) {
     const int64_t blocks = (int64_t)p.B * p.H * ((p.nq + BLOCK - 1) / BLOCK);
-    return with_blocks(p.D, [&](auto db) {
-        masked_dq<db()><<<(unsigned)blocks, NT, 0, s>>>(p);
+    return with_shape(p, [&](auto db, auto cap, auto bias) {
+        masked_dq<db(), cap(), bias()><<<blocks_for(blocks), NT, 0, s>>>(p);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_masked_dkv(const Params& p, hipStream_t s) {
     const int64_t blocks = (int64_t)p.B * p.KH * ((p.nkv + BLOCK - 1) / BLOCK);
-    return with_blocks(p.D, [&](auto db) {
-        masked_dkv<db()><<<(unsigned)blocks, NT, 0, s>>>(p);
+    return with_shape(p, [&](auto db, auto cap, auto bias) {
+        masked_dkv<db(), cap(), bias()><<<blocks_for(blocks), NT, 0, s>>>(p);
         return hipGetLastError();
     });
 }

@@ -44,53 +44,75 @@ __device__ __forceinline__ void clear(State<DB>& st) {
         for (int r = 0; r < 16; ++r) st.o[mb][r] = 0.f;
 }
 
+// What is the same in every step of a wavefront.
+template <int DB>
+struct Context {
+    const Params& p;
+    const bf16x8 (&q)[2 * DB];
+    const Row& row;
+    const Reader<DB>& rd;
+    int lane;
+};
+
 // 32 keys from key j0, rows row0 of the tiles in LDS.  partial: some query does
 // not see some key.  TWO: the probabilities as two bf16 (for few queries, where
 // the products cost nothing and a token's error counts).
-template <int DB, bool TWO>
-__device__ __forceinline__ void step(const Params& p, State<DB>& st, const bf16x8 (&q)[2 * DB], const Row& row,
-                                     const char* kt, const char* vt, const int* docs, int row0, int j0, bool partial,
-                                     bool careful, int lane) {
-    const int half = lane >> 5;
+template <int DB, bool CAP, bool BIAS, bool TWO>
+__device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs,
+                                     int row0, int j0, bool partial) {
+    const Params& p = c.p;
+    const Row& row = c.row;
+    const Reader<DB> rd = c.rd.fresh();
+    const int half = c.lane >> 5;
     f32x16 s;
 #pragma unroll
-    for (int kk = 0; kk < 2 * DB; ++kk)
-        s = mfma32x32x16(row_operand<DB>(kt, row0, kk, lane), q[kk], kk == 0 ? f32x16{} : s);
-    float w[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w[r] = score(p, s[r]);
+    for (int kk = 0; kk < 2 * DB; ++kk) s = mfma32x32x16(rd.rows(kt, row0, kk), c.q[kk], kk == 0 ? f32x16{} : s);
     const int base = j0 + 4 * half;
-    if (row.slope2 != 0.f) {
-        const int d0 = row.pos - base;
+    const float far = (float)(row.pos - base);
+    // Scores less the maximum, in log2 units; -infinity where not seen (also
+    // while the maximum is still -infinity and all others are infinite).
+    float w[16], sum;
+    auto scores = [&](float add) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] = __builtin_fmaf(-row.slope2, (float)abs(d0 - (8 * (r >> 2) + (r & 3))), w[r]);
-    }
-    if (partial) {
+        for (int r = 0; r < 16; ++r) {
+            w[r] = score<CAP>(p, s[r], add);
+            if constexpr (BIAS) w[r] = __builtin_fmaf(-row.slope2, fabsf(far - (float)(8 * (r >> 2) + (r & 3))), w[r]);
+        }
+        if (partial) {
+            const int limit = row.limit - base;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            i32x4 d = {};
-            if (p.kv_doc) d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+            for (int g = 0; g < 4; ++g) {
+                i32x4 d = {};
+                if (p.kv_doc) d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool seen = base + 8 * g + e < row.limit && (!p.kv_doc || (d[e] == row.doc && d[e] >= 0));
-                w[4 * g + e] = seen ? w[4 * g + e] : -INFINITY;
+                for (int e = 0; e < 4; ++e) {
+                    const bool seen = 8 * g + e < limit && (!p.kv_doc || (d[e] == row.doc && d[e] >= 0));
+                    w[4 * g + e] = seen ? w[4 * g + e] : -INFINITY;
+                }
             }
         }
-    }
-    float e[16], sum;
-    auto exps = [&](float mneg) __attribute__((always_inline)) {
-        float a = 0.f, b = 0.f;
+    };
+    bf16x8 pr[2];
+    auto exps = [&]() __attribute__((always_inline)) {
+        float a = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-            e[r] = fast_exp2(w[r] + mneg);
-            e[r + 1] = fast_exp2(w[r + 1] + mneg);
-            a += TWO ? e[r] : bf16_to_f32(f32_to_bf16(e[r]));
-            b += TWO ? e[r + 1] : bf16_to_f32(f32_to_bf16(e[r + 1]));
+            w[r] = fast_exp2(w[r]);
+            w[r + 1] = fast_exp2(w[r + 1]);
+            const bf16x2 pk = {f32_to_bf16(w[r]), f32_to_bf16(w[r + 1])};
+            pr[r >> 3][r & 7] = pk[0];
+            pr[r >> 3][(r & 7) + 1] = pk[1];
+            if constexpr (TWO)
+                a += w[r] + w[r + 1];
+            else
+                a = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, a, false);
         }
-        sum = a + b;
+        sum = a;
     };
-    exps(-st.m);
+    scores(-st.m);
+    exps();
     if (__any(!(sum < P_LIMIT))) {
+        scores(0.f);
         float mx = w[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, w[r]);
@@ -104,21 +126,25 @@ __device__ __forceinline__ void step(const Params& p, State<DB>& st, const bf16x
         for (int mb = 0; mb < DB; ++mb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) st.o[mb][r] *= alpha;
-        exps(m_new == -INFINITY ? 0.f : -m_new);
+        scores(-st.m);
+        exps();
     }
     st.l += sum;
-    auto add = [&](const float (&x)[16]) __attribute__((always_inline)) {
-        if (careful && partial)
-            add_rows_careful<DB>(st.o, x, vt, row0, lane);
-        else
-            add_rows<DB>(st.o, x, vt, row0, lane);
-    };
-    add(e);
+    add_rows<DB>(st.o, pr, rd, vt, row0);
     if constexpr (TWO) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) e[r] -= bf16_to_f32(f32_to_bf16(e[r]));
-        add(e);
+        for (int r = 0; r < 16; ++r) w[r] -= bf16_to_f32(pr[r >> 3][r & 7]);
+        pack(w, pr);
+        add_rows<DB>(st.o, pr, rd, vt, row0);
     }
+}
+
+// Which of the 32 keys from j0 the lane's query sees.
+__device__ __forceinline__ uint32_t keys_seen(const Params& p, const Row& row, const int* docs, int j0) {
+    uint32_t seen = 0;
+    for (int j = 0; j < 32; ++j)
+        seen |= (uint32_t)(j0 + j < row.limit && (!p.kv_doc || (docs[j] == row.doc && row.doc >= 0))) << j;
+    return seen;
 }
 
 template <int DB>
@@ -139,16 +165,18 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
     return r;
 }
 
-template <int DB>
-__global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_forward(Params p) {
+template <int DB, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
     using T = Tile<DB>;
-    __shared__ __attribute__((aligned(16))) char kt[T::BYTES], vt[T::BYTES];
-    __shared__ __attribute__((aligned(16))) int docs[TILE];
-    __shared__ int redo;
+    constexpr int SLOT = 2 * T::BYTES;  // K, V
+    __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
+    __shared__ __attribute__((aligned(16))) int docs[2][TILE];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + QB - 1) / QB;
-    const int bh = blockIdx.x / nqb, qb = blockIdx.x - bh * nqb;
+    const int64_t id = place_in((int64_t)p.B * p.H * nqb);
+    if (id < 0) return;
+    const int bh = (int)(id / nqb), qb = nqb - 1 - (int)(id - (int64_t)bh * nqb);  // the longest first
     const int b = bh / p.H, head = bh - b * p.H, kh = head / p.G;
     const Seq sq = seq_of(p, b);
     const int i0 = qb * QB, last = min(i0 + QB, p.nq) - 1;
@@ -159,77 +187,73 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_forward(Params p) {
     bf16x8 q[2 * DB];
     load_query<DB>(p, p.q + b * p.q_batch + (int64_t)min(i, p.nq - 1) * p.q_row + head * p.D, in, q, lane);
 
-    DocRange all = {}, mine = {};
-    if (p.kv_doc) {
-        mine = range_of_lanes(row.doc, in);
-        const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
-        all = r[0];
-        if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
-    }
-    const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
     const int end = tiles_of(limit_of(p, sq, last));
     const int lim_lo = limit_of(p, sq, w0), lim_hi = w0 <= wlast ? limit_of(p, sq, wlast) : 0;
-    auto next = [&](int t) {
-        if (p.kv_doc)
-            while (t < end && !ranges_meet(ranges[t], all)) ++t;
-        return t;
-    };
+    const int least = limit_of(p, sq, i0);  // every query sees the keys before (documents apart)
+    DocWindow window;
+    {
+        DocRange all = {}, mine = {};
+        if (p.kv_doc) {
+            mine = range_of_lanes(row.doc, in);
+            const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
+            all = r[0];
+            if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+        }
+        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
+    }
 
-    // Staging: DB vectors of K and of V a thread.
-    u32x4 kr[DB], vr[DB];
-    int dr = -1;
+    const Loader<DB, NW, TILE> kload(p.k_row, p.D, wave, lane), vload(p.v_row, p.D, wave, lane);
+    const Reader<DB> rd(lane);
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
-    auto load = [&](int t) {
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
-            const int j = t * TILE + r;
-            const bool ok = j < sq.len && c < p.D;
-            kr[u] = ok ? *(const u32x4*)(kb + j * p.k_row + c) : u32x4{};
-            vr[u] = ok ? *(const u32x4*)(vb + j * p.v_row + c) : u32x4{};
-        }
+    const uint32_t lds0 = lds_address(lds);
+    int dr = -1;
+    auto issue = [&](int t, int slot) {
+        kload.issue(kb, t * TILE, sq.len, lds0 + slot * SLOT);
+        vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
         if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid] : -1;
     };
-    auto store = [&]() {
-#pragma unroll
-        for (int u = 0; u < DB; ++u) {
-            const int id = tid + NT * u, r = id / T::VECS, c = id - r * T::VECS;
-            *(u32x4*)(kt + r * T::LD + 16 * c) = kr[u];
-            *(u32x4*)(vt + r * T::LD + 16 * c) = vr[u];
-        }
-        if (p.kv_doc && tid < TILE) docs[tid] = dr;
-    };
+    if (p.D < 32 * DB) {
+        clear_tiles(lds, 2 * SLOT, NT);
+        __syncthreads();
+    }
 
     State<DB> st;
-    // Once; again with care where that left something that is no number.
-    for (int pass = 0; pass < 2; ++pass) {
-        clear(st);
-        int t = next(0);
-        if (t < end) load(t);
-        while (t < end) {
-            __syncthreads();
-            store();
-            __syncthreads();
-            const int tn = next(t + 1);
-            if (tn < end) load(tn);
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int j0 = t * TILE + 32 * h;
-                if (j0 >= lim_hi) continue;
-                const bool partial = j0 + 32 > lim_lo || (p.kv_doc && !same_document(ranges[t], mine));
-                step<DB, false>(p, st, q, row, kt, vt, docs, 32 * h, j0, partial, pass > 0, lane);
+    clear(st);
+    const Context<DB> c = {p, q, row, rd, lane};
+    int slot = 0, t = window.next(0);
+    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
+    Spoilt<DB> spoilt = {};
+    if (t < end) issue(t, slot);
+    while (t < end) {
+        landed();
+        if (p.kv_doc && tid < TILE) docs[slot][tid] = dr;
+        __syncthreads();  // the tile is there, and nobody reads the one before any more
+        const int tn = window.next(t + 1);
+        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
+        if (tn < end) issue(tn, slot ^ 1);
+        char *kt = lds + slot * SLOT, *vt = kt + T::BYTES;
+        if ((t + 1) * TILE > least || !same_all) {
+            bool bad = false;
+#pragma unroll
+            for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(vt + o + 16 * tid);
+            if (__syncthreads_or(bad)) {
+                for (int h = 0; h < 2; ++h) spoilt.note(vt, 32 * h, keys_seen(p, row, docs[slot] + 32 * h, t * TILE + 32 * h), lane);
+                __syncthreads();
+                for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(vt + o + 16 * tid);
+                __syncthreads();
             }
-            t = tn;
         }
-        if (pass > 0) break;
-        __syncthreads();
-        if (tid == 0) redo = 0;
-        __syncthreads();
-        if (any_not_finite<DB>(st.o) && lane == 0) redo = 1;
-        __syncthreads();
-        if (!redo) break;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int j0 = t * TILE + 32 * h;
+            if (j0 >= lim_hi || apart) continue;
+            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same);
+        }
+        t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
+        slot ^= 1;
     }
+    spoilt.put(st.o);
 
     const float l = sum_halves(st.l);
     if (!in) return;
@@ -257,12 +281,12 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_forward(Params p) {
 
 constexpr int FEW_KEYS = 32;
 
-template <int DB>
-__global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_few(Params p) {
+template <int DB, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     using T = Tile<DB>;
-    constexpr int HALF = FEW_KEYS * T::LD;
-    __shared__ __attribute__((aligned(16))) char lds[NW][2 * HALF];
-    __shared__ __attribute__((aligned(16))) int docs[NW][FEW_KEYS];
+    constexpr int HALF = FEW_KEYS * T::RB, SLOT = 2 * HALF;
+    __shared__ __attribute__((aligned(16))) char lds_all[NW * 2 * SLOT];
+    __shared__ __attribute__((aligned(16))) int docs[NW][2][FEW_KEYS];
     __shared__ float ml[NW][32][2];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -282,57 +306,77 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_few(Params p) {
     const int lim_lo = limit_of(p, sq, 0), lim_hi = limit_of(p, sq, p.nq - 1);
     const int tiles = (lim_hi + FEW_KEYS - 1) / FEW_KEYS;
     const int t0 = (int)((int64_t)tiles * piece / p.pieces), t1 = (int)((int64_t)tiles * (piece + 1) / p.pieces);
-    char *kt = lds[wave], *vt = lds[wave] + HALF;
-    auto next = [&](int t) {
-        if (p.kv_doc)
-            while (t < t1 && !ranges_meet(ranges[t / 2], mine)) t += NW;
-        return t;
-    };
-
-    constexpr int PER = FEW_KEYS * T::VECS / 64;  // vectors of K and of V a lane
-    u32x4 kr[PER], vr[PER];
-    int dr = -1;
+    char* lds = lds_all + wave * 2 * SLOT;
+    const uint32_t lds0 = lds_address(lds);
+    const Loader<DB, 1, FEW_KEYS> kload(p.k_row, p.D, 0, lane), vload(p.v_row, p.D, 0, lane);
+    const Reader<DB> rd(lane);
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
-    auto load = [&](int t) {
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int id = lane + 64 * u, r = id / T::VECS, c = 8 * (id - r * T::VECS);
-            const int j = t * FEW_KEYS + r;
-            const bool ok = j < sq.len && c < p.D;
-            kr[u] = ok ? *(const u32x4*)(kb + j * p.k_row + c) : u32x4{};
-            vr[u] = ok ? *(const u32x4*)(vb + j * p.v_row + c) : u32x4{};
+    // Every NW-th tile from t on that may hold a document of the rows, 64
+    // looked over at a time.
+    int base = -64 * NW;
+    uint64_t meets = 0, whole = 0;
+    auto next = [&](int t) {
+        if (!p.kv_doc) return t;
+        while (t < t1) {
+            if (t >= base + 64 * NW || t < base) {
+                base = t;
+                const int u = t + NW * lane;
+                const DocRange r = u < t1 ? ranges[u / 2] : DocRange{0, -1};
+                meets = __ballot(ranges_meet(r, mine));
+                whole = __ballot(same_document(r, mine));
+            }
+            const uint64_t m = meets >> ((t - base) / NW);
+            if (m) return t + NW * (int)__builtin_ctzll(m);
+            t = base + 64 * NW;
         }
+        return t;
+    };
+    auto same = [&](int t) { return !p.kv_doc || (t < t1 && (whole >> ((t - base) / NW) & 1)); };
+    int dr = -1;
+    auto issue = [&](int t, int slot) {
+        kload.issue(kb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT);
+        vload.issue(vb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT + HALF);
         if (p.kv_doc) dr = lane < FEW_KEYS && t * FEW_KEYS + lane < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * FEW_KEYS + lane] : -1;
     };
-    auto store = [&]() {
-        __builtin_amdgcn_wave_barrier();  // the tile before has been read (LDS works in order)
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int id = lane + 64 * u, r = id / T::VECS, c = id - r * T::VECS;
-            *(u32x4*)(kt + r * T::LD + 16 * c) = kr[u];
-            *(u32x4*)(vt + r * T::LD + 16 * c) = vr[u];
-        }
-        if (p.kv_doc && lane < FEW_KEYS) docs[wave][lane] = dr;
-        __builtin_amdgcn_wave_barrier();
-    };
+    if (p.D < 32 * DB) {
+        clear_tiles(lds_all, NW * 2 * SLOT, NT);
+        __syncthreads();
+    }
 
     State<DB> st;
-    for (int pass = 0; pass < 2; ++pass) {
-        clear(st);
-        int t = next(t0 + wave);
-        if (t < t1) load(t);
-        while (t < t1) {
-            store();
-            const int tn = next(t + NW);
-            if (tn < t1) load(tn);
-            const int j0 = t * FEW_KEYS;
-            const bool partial = j0 + FEW_KEYS > lim_lo || (p.kv_doc && !same_document(ranges[t / 2], mine));
-            step<DB, true>(p, st, q, row, kt, vt, docs[wave], 0, j0, partial, pass > 0, lane);
-            t = tn;
+    clear(st);
+    const Context<DB> c = {p, q, row, rd, lane};
+    int slot = 0, t = next(t0 + wave);
+    bool whole_t = same(t);
+    Spoilt<DB> spoilt = {};
+    if (t < t1) issue(t, slot);
+    while (t < t1) {
+        landed();
+        if (p.kv_doc && lane < FEW_KEYS) docs[wave][slot][lane] = dr;
+        const int tn = next(t + NW);
+        const bool whole_n = same(tn);
+        // (the other slot has been read: the products of the tile before have
+        // waited for that, or this does)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (tn < t1) issue(tn, slot ^ 1);
+        const int j0 = t * FEW_KEYS;
+        char *kt = lds + slot * SLOT, *vt = kt + HALF;
+        const bool partial = j0 + FEW_KEYS > lim_lo || !whole_t;
+        if (partial) {
+            bool bad = false;
+            for (int o = 0; o < HALF; o += 1024) bad |= not_finite16(vt + o + 16 * lane);
+            if (__any(bad)) {
+                spoilt.note(vt, 0, keys_seen(p, row, docs[wave][slot], j0), lane);
+                for (int o = 0; o < HALF; o += 1024) make_finite16(vt + o + 16 * lane);
+            }
         }
-        if (pass > 0 || !any_not_finite<DB>(st.o)) break;
+        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial);
+        t = tn, whole_t = whole_n;
+        slot ^= 1;
     }
+
+    spoilt.put(st.o);
 
     // The wavefronts' results on one maximum, and their sum.
     const float l = sum_halves(st.l);
@@ -349,8 +393,8 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_few(Params p) {
 #pragma unroll
     for (int w = 0; w < NW; ++w) total = __builtin_fmaf(ml[w][col][1], factor(ml[w][col][0], m), total);
     const float f = factor(st.m, m);
-    float* o = (float*)lds[wave];  // [register][lane]; 64 KB a workgroup at most, as its tiles
-    static_assert(DB * 16 * 64 * 4 <= 2 * HALF, "results in the tiles' place");
+    float* o = (float*)lds;  // [register][lane]
+    static_assert(DB * 16 * 64 * 4 <= 2 * SLOT, "results in the tiles' place");
 #pragma unroll
     for (int mb = 0; mb < DB; ++mb)
 #pragma unroll
@@ -362,7 +406,7 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_few(Params p) {
         const int reg = NW * u + wave;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) v += ((const float*)lds[w])[reg * 64 + lane];
+        for (int w = 0; w < NW; ++w) v += ((const float*)(lds_all + w * 2 * SLOT))[reg * 64 + lane];
         if (p.pieces > 1) {
             p.part_o[((int64_t)blockIdx.x * (16 * DB) + reg) * 64 + lane] = v;
         } else {
@@ -437,16 +481,16 @@ hipError_t launch_masked_ranges(const Params& p, hipStream_t s) {
 
 hipError_t launch_masked_forward(const Params& p, hipStream_t s) {
     const int64_t blocks = (int64_t)p.B * p.H * ((p.nq + QB - 1) / QB);
-    return with_blocks(p.D, [&](auto db) {
-        masked_forward<db()><<<(unsigned)blocks, NT, 0, s>>>(p);
+    return with_shape(p, [&](auto db, auto cap, auto bias) {
+        masked_forward<db(), cap(), bias()><<<blocks_for(blocks), NT, 0, s>>>(p);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_masked_few(const Params& p, hipStream_t s) {
     const int64_t groups = (int64_t)p.B * p.KH * p.row_blocks;
-    return with_blocks(p.D, [&](auto db) {
-        masked_few<db()><<<(unsigned)(groups * p.pieces), NT, 0, s>>>(p);
+    return with_shape(p, [&](auto db, auto cap, auto bias) {
+        masked_few<db(), cap(), bias()><<<(unsigned)(groups * p.pieces), NT, 0, s>>>(p);
         if (p.pieces > 1) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
