@@ -27,11 +27,12 @@ constexpr float LN2 = 0.69314718055994531f;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Documents of 64 tokens: the least and the largest number (lo < 0: some are
-// none; hi < 0: all are).
+// Documents of 64 tokens: the least number, its top bit set where some tokens
+// have none, and the largest (-1: all have none).
 struct DocRange {
     int32_t lo, hi;
 };
+constexpr uint32_t SOME_NONE = 0x80000000u;
 
 struct Params {
     const bf16 *q, *k, *v, *dy;
@@ -49,7 +50,8 @@ struct Params {
     const int32_t *kv_len, *q_pos, *prefix, *q_doc, *kv_doc;
     const float* slopes;
     DocRange *q_range, *kv_range;  // [B][tiles], with documents
-    // few queries: pieces of the keys, their results
+    // few queries: pieces of the keys, their results; keys' gradients: pieces of
+    // the queries, [pieces][B * KH][nkv][dk, dv][32 DB] float32 in part_o
     int32_t pieces, row_blocks;
     float* part_o;
     float* part_ml;
@@ -73,11 +75,20 @@ __device__ __forceinline__ int limit_of(const Params& p, const Seq& s, int i) {
     return p.causal ? min(s.len, max(s.pos0 + i + 1, s.prefix)) : s.len;
 }
 
+// Documents of keys are compared as max(number, -1), a query's (of a key's
+// workgroup, the key's) as itself or, if it has none, as a number that no key has.
+constexpr int NO_DOC = -2;
+__device__ __forceinline__ int own_document(int d) { return d >= 0 ? d : NO_DOC; }
+
+__device__ __forceinline__ int least_document(const DocRange& a) { return (int)((uint32_t)a.lo & ~SOME_NONE); }
 __device__ __forceinline__ bool ranges_meet(const DocRange& a, const DocRange& b) {
-    return a.hi >= max(b.lo, 0) && b.hi >= max(a.lo, 0);
+    return a.hi >= least_document(b) && b.hi >= least_document(a);
 }
 __device__ __forceinline__ bool same_document(const DocRange& a, const DocRange& b) {
     return a.lo >= 0 && a.lo == a.hi && b.lo == a.lo && b.hi == a.lo;
+}
+__device__ __forceinline__ DocRange joined(const DocRange& a, const DocRange& b) {
+    return DocRange{(int)((uint32_t)min(least_document(a), least_document(b)) | (((uint32_t)a.lo | (uint32_t)b.lo) & SOME_NONE)), max(a.hi, b.hi)};
 }
 
 // The score of q . k in log2 units before the bias, plus `add`; in `slope` a
@@ -227,7 +238,7 @@ struct DocWindow {
     bool on;
     __device__ __forceinline__ void init(const DocRange* ranges_, int end_, const DocRange& all_, const DocRange& mine_, bool on_) {
         ranges = ranges_, end = end_, base = -TILE, all = all_, mine = mine_, on = on_;
-        r = DocRange{0, -1};
+        r = DocRange{0x7fffffff, -1};
         meets = 0;
     }
     // The first tile from t on (end: none).
@@ -237,7 +248,7 @@ struct DocWindow {
             if (t >= base + TILE || t < base) {
                 base = t;
                 const int u = t + (int)(threadIdx.x & 63);
-                r = u < end ? ranges[u] : DocRange{0, -1};
+                r = u < end ? ranges[u] : DocRange{0x7fffffff, -1};
                 meets = __ballot(ranges_meet(r, all));
             }
             const uint64_t m = meets >> (t - base);
@@ -352,15 +363,17 @@ __device__ __forceinline__ float sum_halves(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The least and largest document of a wavefront's lanes, those out of play given as `in` false.
+// The documents of a wavefront's lanes, those that are `in`.
 __device__ __forceinline__ DocRange range_of_lanes(int doc, bool in) {
-    int lo = in ? doc : 0x7fffffff, hi = in ? doc : -1;
+    int lo = in && doc >= 0 ? doc : 0x7fffffff, hi = in ? max(doc, -1) : -1;
+    const bool none = __any(in && doc < 0);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         lo = min(lo, __shfl_xor(lo, d));
         hi = max(hi, __shfl_xor(hi, d));
     }
-    return DocRange{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi)};
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    return DocRange{(int)((uint32_t)lo | (none ? SOME_NONE : 0u)), __builtin_amdgcn_readfirstlane(hi)};
 }
 
 }  // namespace masked

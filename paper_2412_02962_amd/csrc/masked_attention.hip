@@ -106,7 +106,20 @@ int64_t forward_bytes(const pcpp_masked_geom_t* g) {
     return range_bytes(g) + few_blocks(g, few_plan(g)) * (few_floats(g) + 2 * MASKED_FEW_ROWS) * 4;
 }
 int64_t delta_bytes(const pcpp_masked_geom_t* g) { return round16((int64_t)g->batch * g->heads * g->n_q * 4); }
-int64_t backward_bytes(const pcpp_masked_geom_t* g) { return range_bytes(g) + delta_bytes(g); }
+// Pieces of the queries (of all heads) for the keys' gradients: with fewer
+// blocks of keys than two to a compute unit, as many as fill them.
+int kv_pieces(const pcpp_masked_geom_t* g) {
+    const int64_t blocks = (int64_t)g->batch * g->kv_heads * ((g->n_kv + 127) / 128);
+    const int64_t tiles = (int64_t)g->heads / g->kv_heads * ((g->n_q + 63) / 64);
+    int64_t n = (512 + blocks - 1) / blocks;
+    if (n > tiles / 8) n = tiles / 8;
+    return (int)(n < 1 ? 1 : n);
+}
+int64_t kv_bytes(const pcpp_masked_geom_t* g) {
+    const int n = kv_pieces(g);
+    return n == 1 ? 0 : (int64_t)n * g->batch * g->kv_heads * g->n_kv * 2 * ((g->head_dim + 31) / 32 * 32) * 4;
+}
+int64_t backward_bytes(const pcpp_masked_geom_t* g) { return range_bytes(g) + delta_bytes(g) + kv_bytes(g); }
 
 Params params_of(const pcpp_masked_geom_t* g, const pcpp_mask_t* m, const Shape& s, void* workspace) {
     Params p = {};
@@ -219,6 +232,8 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
     p.lse = (float*)lse;
     p.dq = (bf16*)dq, p.dk = (bf16*)dk, p.dv = (bf16*)dv;
     p.delta = (float*)((char*)workspace + range_bytes(g));
+    p.part_o = (float*)((char*)workspace + range_bytes(g) + delta_bytes(g));
+    p.pieces = kv_pieces(g);
     const hipStream_t s = (hipStream_t)stream;
     if (p.kv_doc && launch_masked_ranges(p, s) != hipSuccess) return PCPP_EHIP;
     if (launch_masked_delta(p, s) != hipSuccess) return PCPP_EHIP;

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     const int i = w0 + (lane & 31), ic = min(i, p.nq - 1);
     const bool in = i < p.nq;
     const int pos = sq.pos0 + i, limit = limit_of(p, sq, i);
-    const int doc = in && p.q_doc ? p.q_doc[(int64_t)b * p.nq + i] : -1;
+    const int doc = in && p.q_doc ? own_document(p.q_doc[(int64_t)b * p.nq + i]) : NO_DOC;
     const float slope2 = p.slopes ? p.slopes[head] * LOG2E : 0.f;
     const float lse2 = p.lse[(int64_t)bh * p.nq + ic] * LOG2E, delta = p.delta[(int64_t)bh * p.nq + ic];
     bf16x8 q[2 * DB], dy[2 * DB];
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
             mine = range_of_lanes(doc, in);
             const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
             all = r[0];
-            if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+            if (last / TILE > i0 / TILE) all = joined(all, r[1]);
         }
         window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
     }
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     auto issue = [&](int t, int slot) {
         kload.issue(kb, t * TILE, sq.len, lds0 + slot * SLOT);
         vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
-        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid] : -1;
+        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid], -1) : -1;
     };
     if (p.D < 32 * DB) {
         clear_tiles(lds, 2 * SLOT, NT);
@@ -153,16 +153,19 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
             if constexpr (CAP) dp[r] = slope;
         }
         if (partial) {
+            // (the derivative too: it is NaN where the key is)
+            auto keep = [&](int r, bool seen) __attribute__((always_inline)) {
+                w[r] = seen ? w[r] : 0.f;
+                if constexpr (CAP) dp[r] = seen ? dp[r] : 0.f;
+            };
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                i32x4 d = {};
-                if (p.kv_doc) d = *(const i32x4*)(dt + row0 + 8 * g + 4 * half);
+            for (int r = 0; r < 16; ++r) keep(r, 8 * (r >> 2) + (r & 3) < limit - base);
+            if (p.kv_doc) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * g + e;
-                    const bool seen = 8 * g + e < limit - base && (!p.kv_doc || (d[e] == doc && d[e] >= 0));
-                    w[r] = seen ? w[r] : 0.f;
-                    if constexpr (CAP) dp[r] = seen ? dp[r] : 0.f;
+                for (int g = 0; g < 4; ++g) {
+                    const i32x4 d = *(const i32x4*)(dt + row0 + 8 * g + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) keep(4 * g + e, d[e] == doc);
                 }
             }
         }
@@ -178,7 +181,6 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     clear<DB>(acc);
     int slot = 0, t = window.next(0);
     bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
-    Spoilt<DB> spoilt = {};
     if (t < end) issue(t, slot);
     while (t < end) {
         landed();
@@ -193,16 +195,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
 #pragma unroll
             for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(kt + o + 16 * tid);
             if (__syncthreads_or(bad)) {
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t seen = 0;
-                    for (int r = 0; r < 32; ++r) {
-                        const int jr = t * TILE + 32 * h + r, d = p.kv_doc ? docs[slot][32 * h + r] : 0;
-                        seen |= (uint32_t)(jr < limit && (!p.kv_doc || (d == doc && d >= 0))) << r;
-                    }
-                    spoilt.note(kt, 32 * h, seen, lane);
-                }
-                // (the scores are NaN or infinite with or without what is taken out)
-                __syncthreads();
+                // (a query that sees such a key has no number in its lse, and so none in dz)
                 for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(kt + o + 16 * tid);
                 __syncthreads();
             }
@@ -216,7 +209,6 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
         slot ^= 1;
     }
-    spoilt.put(acc);
     off = sum_halves(off);
     if (!in) return;
     if (lane < 32) p.delta[(int64_t)bh * p.nq + i] = delta + off;
@@ -224,40 +216,67 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
 }
 
 // What a tile's queries bring besides q and dy; delta negative.
+template <int ROWS>
 struct QueryTile {
-    float lse2[TILE], delta[TILE];
-    int doc[TILE];
+    float lse2[ROWS], delta[ROWS];
+    int doc[ROWS];
 };
 
+// A block of keys against a piece of the queries (of all heads that read them,
+// one head after the other).  Up to 64 channels: K and V in registers, tiles of
+// 64 queries; above, where the two sums alone take half the registers that two
+// wavefronts of a SIMD have, V in LDS and tiles of 32 queries.
 template <int DB, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_dkv(Params p) {
+__global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
     using T = Tile<DB>;
-    constexpr int SLOT = 2 * T::BYTES;  // Q, dy
-    __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
-    __shared__ __attribute__((aligned(16))) QueryTile brought[2];
+    constexpr int ROWS = DB <= 2 ? 64 : 32, TB = ROWS * T::RB;
+    constexpr int SLOT = 2 * TB;  // Q, dy
+    constexpr bool V_LDS = DB > 2;
+    constexpr int LDS = 2 * SLOT + (V_LDS ? BLOCK * T::RB : 0);
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    __shared__ __attribute__((aligned(16))) QueryTile<ROWS> brought[2];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nkb = (p.nkv + BLOCK - 1) / BLOCK;
-    const int64_t id = place_in((int64_t)p.B * p.KH * nkb);
+    const int64_t id = place_in((int64_t)p.B * p.KH * nkb * p.pieces);
     if (id < 0) return;
-    const int bk = (int)(id / nkb), kb = (int)(id - (int64_t)bk * nkb);
+    const int item = (int)(id / nkb), kb = (int)(id - (int64_t)item * nkb);
+    const int bk = item / p.pieces, piece = item - bk * p.pieces;
     const int b = bk / p.KH, kh = bk - b * p.KH;
     const Seq sq = seq_of(p, b);
     const int k0 = kb * BLOCK, klast = min(k0 + BLOCK, p.nkv) - 1;
     const int w0 = k0 + 32 * wave;
     const int j = w0 + (lane & 31);
     const bool in = j < p.nkv, live = j < sq.len;
-    const int doc = live && p.kv_doc ? p.kv_doc[(int64_t)b * p.nkv + j] : -1;
+    const int doc = live && p.kv_doc ? own_document(p.kv_doc[(int64_t)b * p.nkv + j]) : NO_DOC;
     // The queries that see key j by length, past and prefix: from .. nq - 1.
     const int from = !live ? p.nq : !p.causal || j < sq.prefix ? 0 : min(max(j - sq.pos0, 0), p.nq);
-    bf16x8 k[2 * DB], v[2 * DB];
+    if (V_LDS || p.D < 32 * DB) {
+        clear_tiles(lds, LDS, NT);
+        __syncthreads();
+    }
+    bf16x8 k[2 * DB], v[V_LDS ? 1 : 2 * DB];
     load_rows<DB>(p.k + b * p.k_batch + (int64_t)min(j, p.nkv - 1) * p.k_row + kh * p.D, live, p.D, k, lane);
-    load_rows<DB>(p.v + b * p.v_batch + (int64_t)min(j, p.nkv - 1) * p.v_row + kh * p.D, live, p.D, v, lane);
+    const bf16* vrow = p.v + b * p.v_batch + (int64_t)min(j, p.nkv - 1) * p.v_row + kh * p.D;
+    const Reader<DB> reader(lane);
+    char* vt = lds + 2 * SLOT;  // all of the block's keys
+    if constexpr (V_LDS) {
+        bf16x8 x[2 * DB];
+        load_rows<DB>(vrow, live, p.D, x, lane);
+#pragma unroll
+        for (int kk = 0; kk < 2 * DB; ++kk) *(bf16x8*)(vt + 32 * wave * T::RB + (reader.row_at ^ (32 * kk))) = x[kk];
+    } else {
+        load_rows<DB>(vrow, live, p.D, v, lane);
+    }
 
-    const int ntq = tiles_of(p.nq);
+    // Tiles of ROWS queries: this piece's, in order of heads and queries.
+    const int nt = (p.nq + ROWS - 1) / ROWS;
     int first = 0;  // tile of the first query that sees the block's first key
-    if (p.causal && k0 >= sq.prefix) first = min(max(k0 - sq.pos0, 0), p.nq) / TILE;
-    if (k0 >= sq.len) first = ntq;
+    if (p.causal && k0 >= sq.prefix) first = min(max(k0 - sq.pos0, 0), p.nq) / ROWS;
+    if (k0 >= sq.len) first = nt;
+    const int tiles = nt - min(first, nt);
+    const int64_t all_tiles = (int64_t)tiles * p.G;
+    const int64_t u0 = all_tiles * piece / p.pieces, u1 = all_tiles * (piece + 1) / p.pieces;
     DocWindow window;
     {
         DocRange all = {}, mine = {};
@@ -265,35 +284,36 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_dkv(Params p) {
             mine = range_of_lanes(doc, live);
             const DocRange* r = p.kv_range + (int64_t)b * tiles_of(p.nkv) + k0 / TILE;
             all = r[0];
-            if (klast / TILE > k0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+            if (klast / TILE > k0 / TILE) all = joined(all, r[1]);
         }
-        window.init(p.q_range + (int64_t)b * ntq, ntq, all, mine, p.kv_doc != nullptr);
+        window.init(p.q_range + (int64_t)b * tiles_of(p.nq), tiles_of(p.nq), all, mine, p.kv_doc != nullptr);
     }
-    const Loader<DB, NW, TILE> qload(p.q_row, p.D, wave, lane), gload(p.y_row, p.D, wave, lane);
-    const Reader<DB> reader(lane);
+    // The first tile from t on that may have the block's documents.
+    auto next = [&](int t) {
+        const int w = window.next(t * ROWS / TILE);
+        return w == t * ROWS / TILE ? t : w * (TILE / ROWS);
+    };
+
+    const Loader<DB, NW, ROWS> qload(p.q_row, p.D, wave, lane), gload(p.y_row, p.D, wave, lane);
     const uint32_t lds0 = lds_address(lds);
     float lr = 0.f, er = 0.f;
     int dr = -1;
     auto issue = [&](int g, int t, int slot) {
         const int head = kh * p.G + g;
-        qload.issue(p.q + b * p.q_batch + head * p.D, t * TILE, p.nq, lds0 + slot * SLOT);
-        gload.issue(p.dy + b * p.y_batch + head * p.D, t * TILE, p.nq, lds0 + slot * SLOT + T::BYTES);
-        if (tid < TILE) {
-            const int i = min(t * TILE + tid, p.nq - 1);
+        qload.issue(p.q + b * p.q_batch + head * p.D, t * ROWS, p.nq, lds0 + slot * SLOT);
+        gload.issue(p.dy + b * p.y_batch + head * p.D, t * ROWS, p.nq, lds0 + slot * SLOT + TB);
+        if (tid < ROWS) {
+            const int i = min(t * ROWS + tid, p.nq - 1);
             const int64_t at = ((int64_t)b * p.H + head) * p.nq + i;
             lr = p.lse[at] * -LOG2E;
             er = -p.delta[at];
-            if (p.q_doc) dr = p.q_doc[(int64_t)b * p.nq + i];
+            if (p.q_doc) dr = max(p.q_doc[(int64_t)b * p.nq + i], -1);
         }
     };
-    if (p.D < 32 * DB) {
-        clear_tiles(lds, 2 * SLOT, NT);
-        __syncthreads();
-    }
 
     f32x16 dk[DB], dv[DB];
-    auto step = [&](const char* qt, const QueryTile& rows, int row0, int i0, float slope2, bool partial) __attribute__((always_inline)) {
-        const char* gt = qt + T::BYTES;
+    auto step = [&](const char* qt, const QueryTile<ROWS>& rows, int row0, int i0, float slope2, bool partial) __attribute__((always_inline)) {
+        const char* gt = qt + TB;
         const Reader<DB> rd = reader.fresh();
         f32x16 s, dp;
 #pragma unroll
@@ -305,7 +325,12 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_dkv(Params p) {
 #pragma unroll
         for (int kk = 0; kk < 2 * DB; ++kk) {
             s = mfma32x32x16(rd.rows(qt, row0, kk), k[kk], kk == 0 ? f32x16{} : s);
-            dp = mfma32x32x16(rd.rows(gt, row0, kk), v[kk], dp);
+            if constexpr (V_LDS)
+                dp = mfma32x32x16(rd.rows(gt, row0, kk), rd.rows(vt, 32 * wave, kk), dp);
+            else
+                dp = mfma32x32x16(rd.rows(gt, row0, kk), v[kk], dp);
+            if constexpr (DB > 3)
+                if (kk & 1) __builtin_amdgcn_sched_barrier(0);  // no more operands ahead than registers for them
         }
         const int base = i0 + 4 * half;
         const float far = (float)(sq.pos0 + base - j);
@@ -324,81 +349,149 @@ __global__ __launch_bounds__(NT, DB > 2 ? 1 : 2) void masked_dkv(Params p) {
             }
         }
         if (partial) {
+            auto keep = [&](int r, bool seen) __attribute__((always_inline)) {
+                w[r] = seen ? w[r] : 0.f;
+                z[r] = seen ? z[r] : 0.f;
+            };
+            const uint32_t lo = from - base, n = max(p.nq - from, 0);  // rows lo .. lo + n - 1, in one comparison
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                i32x4 d = {};
-                if (p.kv_doc) d = *(const i32x4*)(rows.doc + row0 + 8 * g + 4 * half);
+            for (int r = 0; r < 16; ++r) keep(r, (uint32_t)(8 * (r >> 2) + (r & 3)) - lo < n);
+            if (p.kv_doc) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * g + e;
-                    const bool seen = 8 * g + e >= from - base && 8 * g + e < p.nq - base && (!p.kv_doc || (d[e] == doc && d[e] >= 0));
-                    w[r] = seen ? w[r] : 0.f;
-                    z[r] = seen ? z[r] : 0.f;
+                for (int g = 0; g < 4; ++g) {
+                    const i32x4 d = *(const i32x4*)(rows.doc + row0 + 8 * g + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) keep(4 * g + e, d[e] == doc);
                 }
             }
         }
         bf16x8 o[2];
+        if constexpr (DB > 3) __builtin_amdgcn_sched_barrier(0);
         pack(w, o);
         add_rows<DB>(dv, o, rd, gt, row0);
+        if constexpr (DB > 3) __builtin_amdgcn_sched_barrier(0);
         pack(z, o);
         add_rows<DB>(dk, o, rd, qt, row0);
     };
 
     clear<DB>(dk);
     clear<DB>(dv);
-    int slot = 0, g = 0, t = window.next(first);
-    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
-    Spoilt<DB> spoilt_k = {}, spoilt_v = {};
-    if (t >= ntq) g = p.G;  // no query sees the block
-    if (g < p.G) issue(g, t, slot);
-    while (g < p.G) {
+    Spoilt<DB> spoilt = {};
+    int slot = 0, g = 0, t = 0;
+    bool more = u0 < u1, same = true, apart = false, same_all = true;
+    // From tile t of head g on: the first that counts, and whether this piece has it.
+    auto settle = [&](int& hg, int& ht) {
+        while (hg < p.G) {
+            ht = next(ht);
+            if (ht < nt) return (int64_t)hg * tiles + ht - first < u1;
+            ++hg;
+            ht = first;
+        }
+        return false;
+    };
+    auto look = [&](int ht, bool& a, bool& c, bool& d) {
+        const int w = ht * ROWS / TILE;
+        a = window.same(w), c = window.apart(w), d = window.same_all(w);
+    };
+    if (more) {
+        g = (int)(u0 / tiles);
+        t = first + (int)(u0 - (int64_t)g * tiles);
+        more = settle(g, t);
+    }
+    if (more) {
+        look(t, same, apart, same_all);
+        issue(g, t, slot);
+    }
+    while (more) {
         landed();
-        if (tid < TILE) {
+        if (tid < ROWS) {
             brought[slot].lse2[tid] = lr;
             brought[slot].delta[tid] = er;
             brought[slot].doc[tid] = dr;
         }
         __syncthreads();  // the tile is there, and nobody reads the one before any more
-        int gn = g, tn = window.next(t + 1);
-        if (tn >= ntq) ++gn, tn = window.next(first);
-        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
-        if (gn < p.G) issue(gn, tn, slot ^ 1);
+        int gn = g, tn = t + 1;
+        const bool more_n = settle(gn, tn);
+        bool same_n = true, apart_n = false, same_all_n = true;
+        if (more_n) {
+            look(tn, same_n, apart_n, same_all_n);
+            issue(gn, tn, slot ^ 1);
+        }
         const float slope2 = BIAS && p.slopes ? p.slopes[kh * p.G + g] * LOG2E : 0.f;
         char* qt = lds + slot * SLOT;
-        if ((t + 1) * TILE > p.nq || k0 + BLOCK > limit_of(p, sq, t * TILE) || !same_all) {
+        const int i0 = t * ROWS;
+        if (i0 + ROWS > p.nq || k0 + BLOCK > limit_of(p, sq, i0) || !same_all) {
             bool bad = false;
 #pragma unroll
             for (int o = 0; o < SLOT; o += 16 * NT) bad |= not_finite16(qt + o + 16 * tid);
             if (__syncthreads_or(bad)) {
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < ROWS; h += 32) {
                     uint32_t seen = 0;
                     for (int r = 0; r < 32; ++r) {
-                        const int i = t * TILE + 32 * h + r, d = brought[slot].doc[32 * h + r];
-                        seen |= (uint32_t)(i >= from && i < p.nq && (!p.kv_doc || (d == doc && d >= 0))) << r;
+                        const int i = i0 + h + r, d = brought[slot].doc[h + r];
+                        seen |= (uint32_t)((i >= from) & (i < p.nq) & (!p.kv_doc || d == doc)) << r;
                     }
-                    spoilt_k.note(qt, 32 * h, seen, lane);
-                    spoilt_v.note(qt + T::BYTES, 32 * h, seen, lane);
+                    spoilt.note(qt + TB, h, seen, lane);
                 }
-                // (the scores, or dy . v, are NaN or infinite with or without what is taken out)
+                // (a query that is no number has none in its lse, and so none in P and dz)
                 __syncthreads();
                 for (int o = 0; o < SLOT; o += 16 * NT) make_finite16(qt + o + 16 * tid);
                 __syncthreads();
             }
         }
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-            const int i0 = t * TILE + 32 * h;
-            if (apart || i0 >= p.nq || w0 >= limit_of(p, sq, min(i0 + 31, p.nq - 1))) continue;
-            step(qt, brought[slot], 32 * h, i0, slope2, i0 + 32 > p.nq || w0 + 32 > limit_of(p, sq, i0) || !same);
+        for (int h = 0; h < ROWS; h += 32) {
+            const int ih = i0 + h;
+            if (apart || ih >= p.nq || w0 >= limit_of(p, sq, min(ih + 31, p.nq - 1))) continue;
+            step(qt, brought[slot], h, ih, slope2, ih + 32 > p.nq || w0 + 32 > limit_of(p, sq, ih) || !same);
         }
-        g = gn, t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
+        g = gn, t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
         slot ^= 1;
     }
-    spoilt_k.put(dk);
-    spoilt_v.put(dv);
+    spoilt.put(dv);
     if (!in) return;
-    store_rows<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, dk, CAP ? 4.f * p.scale : p.scale, p.D, lane);
+    const float f = CAP ? 4.f * p.scale : p.scale;
+    if (p.pieces > 1) {
+        constexpr int CH = 32 * DB;
+        float* o = p.part_o + (((int64_t)piece * p.B * p.KH + bk) * p.nkv + j) * (2 * CH) + 4 * half;
+#pragma unroll
+        for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                f32x4 a, c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = dk[mb][4 * q4 + e] * f, c[e] = dv[mb][4 * q4 + e];
+                *(f32x4*)(o + 32 * mb + 8 * q4) = a;
+                *(f32x4*)(o + CH + 32 * mb + 8 * q4) = c;
+            }
+        return;
+    }
+    store_rows<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, dk, f, p.D, lane);
     store_rows<DB>(p.dv + b * p.v_batch + (int64_t)j * p.v_row + kh * p.D, dv, 1.f, p.D, lane);
+}
+
+// The pieces' sums, in their order: eight channels of dk or dv of a key a thread.
+__global__ __launch_bounds__(NT) void masked_join_kv(Params p, int CH) {
+    const int per = 2 * CH / 8;
+    const int64_t id = (int64_t)blockIdx.x * NT + threadIdx.x, rows = (int64_t)p.B * p.KH * p.nkv;
+    const int64_t row = id / per;
+    if (row >= rows) return;
+    const int c = 8 * (int)(id - row * per);
+    const float* in = p.part_o + row * (2 * CH) + c;
+    f32x4 a = {}, b4 = {};
+    for (int k = 0; k < p.pieces; ++k) {
+        a += *(const f32x4*)(in + k * rows * (2 * CH));
+        b4 += *(const f32x4*)(in + k * rows * (2 * CH) + 4);
+    }
+    const int64_t bk = row / p.nkv;
+    const int j = (int)(row - bk * p.nkv), b = (int)(bk / p.KH), kh = (int)(bk - (int64_t)b * p.KH);
+    const int ch = c < CH ? c : c - CH;
+    if (ch >= p.D) return;
+    bf16* o = c < CH ? p.dk + b * p.k_batch + (int64_t)j * p.k_row : p.dv + b * p.v_batch + (int64_t)j * p.v_row;
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = f32_to_bf16(a[e]), v[4 + e] = f32_to_bf16(b4[e]);
+    *(bf16x8*)(o + kh * p.D + ch) = v;
 }
 
 }  // namespace
@@ -418,11 +511,16 @@ hipError_t launch_masked_dq(const Params& p, hipStream_t s) {
 }
 
 hipError_t launch_masked_dkv(const Params& p, hipStream_t s) {
-    const int64_t blocks = (int64_t)p.B * p.KH * ((p.nkv + BLOCK - 1) / BLOCK);
-    return with_shape(p, [&](auto db, auto cap, auto bias) {
+    const int64_t blocks = (int64_t)p.B * p.KH * ((p.nkv + BLOCK - 1) / BLOCK) * p.pieces;
+    const hipError_t e = with_shape(p, [&](auto db, auto cap, auto bias) {
         masked_dkv<db(), cap(), bias()><<<blocks_for(blocks), NT, 0, s>>>(p);
         return hipGetLastError();
     });
+    if (e != hipSuccess || p.pieces == 1) return e;
+    const int ch = (p.D + 31) / 32 * 32;
+    const int64_t threads = (int64_t)p.B * p.KH * p.nkv * (2 * ch / 8);
+    masked_join_kv<<<(unsigned)((threads + NT - 1) / NT), NT, 0, s>>>(p, ch);
+    return hipGetLastError();
 }
 
 }  // namespace pcpp

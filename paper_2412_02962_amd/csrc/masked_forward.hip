@@ -24,7 +24,8 @@ constexpr int QB = 32 * NW;  // queries of a workgroup of masked_forward
 
 // A lane's query.
 struct Row {
-    int pos, limit, doc;  // limit: it sees no key from here on
+    int pos, limit;       // limit: it sees no key from here on
+    int doc;              // NO_DOC: none
     float slope2;         // of the bias, log2 units
 };
 
@@ -81,13 +82,13 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
         if (partial) {
             const int limit = row.limit - base;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                i32x4 d = {};
-                if (p.kv_doc) d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+            for (int r = 0; r < 16; ++r) w[r] = 8 * (r >> 2) + (r & 3) < limit ? w[r] : -INFINITY;
+            if (p.kv_doc) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool seen = 8 * g + e < limit && (!p.kv_doc || (d[e] == row.doc && d[e] >= 0));
-                    w[4 * g + e] = seen ? w[4 * g + e] : -INFINITY;
+                for (int g = 0; g < 4; ++g) {
+                    const i32x4 d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[4 * g + e] = d[e] == row.doc ? w[4 * g + e] : -INFINITY;
                 }
             }
         }
@@ -143,7 +144,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
 __device__ __forceinline__ uint32_t keys_seen(const Params& p, const Row& row, const int* docs, int j0) {
     uint32_t seen = 0;
     for (int j = 0; j < 32; ++j)
-        seen |= (uint32_t)(j0 + j < row.limit && (!p.kv_doc || (docs[j] == row.doc && row.doc >= 0))) << j;
+        seen |= (uint32_t)((j0 + j < row.limit) & (!p.kv_doc || docs[j] == row.doc)) << j;
     return seen;
 }
 
@@ -160,7 +161,7 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
     Row r;
     r.pos = sq.pos0 + i;
     r.limit = limit_of(p, sq, i);
-    r.doc = in && p.q_doc ? p.q_doc[(int64_t)b * p.nq + i] : -1;
+    r.doc = in && p.q_doc ? own_document(p.q_doc[(int64_t)b * p.nq + i]) : NO_DOC;
     r.slope2 = p.slopes ? p.slopes[head] * LOG2E : 0.f;
     return r;
 }
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
             mine = range_of_lanes(row.doc, in);
             const DocRange* r = p.q_range + (int64_t)b * tiles_of(p.nq) + i0 / TILE;
             all = r[0];
-            if (last / TILE > i0 / TILE) all = DocRange{min(all.lo, r[1].lo), max(all.hi, r[1].hi)};
+            if (last / TILE > i0 / TILE) all = joined(all, r[1]);
         }
         window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
     }
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
     auto issue = [&](int t, int slot) {
         kload.issue(kb, t * TILE, sq.len, lds0 + slot * SLOT);
         vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
-        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid] : -1;
+        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid], -1) : -1;
     };
     if (p.D < 32 * DB) {
         clear_tiles(lds, 2 * SLOT, NT);
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
             if (t >= base + 64 * NW || t < base) {
                 base = t;
                 const int u = t + NW * lane;
-                const DocRange r = u < t1 ? ranges[u / 2] : DocRange{0, -1};
+                const DocRange r = u < t1 ? ranges[u / 2] : DocRange{0x7fffffff, -1};
                 meets = __ballot(ranges_meet(r, mine));
                 whole = __ballot(same_document(r, mine));
             }
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     auto issue = [&](int t, int slot) {
         kload.issue(kb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT);
         vload.issue(vb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT + HALF);
-        if (p.kv_doc) dr = lane < FEW_KEYS && t * FEW_KEYS + lane < sq.len ? p.kv_doc[(int64_t)b * p.nkv + t * FEW_KEYS + lane] : -1;
+        if (p.kv_doc) dr = lane < FEW_KEYS && t * FEW_KEYS + lane < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * FEW_KEYS + lane], -1) : -1;
     };
     if (p.D < 32 * DB) {
         clear_tiles(lds_all, NW * 2 * SLOT, NT);
