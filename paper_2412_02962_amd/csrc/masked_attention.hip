@@ -119,7 +119,7 @@ int64_t kv_bytes(const pcpp_masked_geom_t* g) {
     const int n = kv_pieces(g);
     return n == 1 ? 0 : (int64_t)n * g->batch * g->kv_heads * g->n_kv * 2 * ((g->head_dim + 31) / 32 * 32) * 4;
 }
-int64_t backward_bytes(const pcpp_masked_geom_t* g) { return range_bytes(g) + delta_bytes(g) + kv_bytes(g); }
+int64_t backward_bytes(const pcpp_masked_geom_t* g) { return range_bytes(g) + 2 * delta_bytes(g) + kv_bytes(g); }
 
 Params params_of(const pcpp_masked_geom_t* g, const pcpp_mask_t* m, const Shape& s, void* workspace) {
     Params p = {};
@@ -232,7 +232,8 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
     p.lse = (float*)lse;
     p.dq = (bf16*)dq, p.dk = (bf16*)dk, p.dv = (bf16*)dv;
     p.delta = (float*)((char*)workspace + range_bytes(g));
-    p.part_o = (float*)((char*)workspace + range_bytes(g) + delta_bytes(g));
+    p.lse2 = (float*)((char*)p.delta + delta_bytes(g));
+    p.part_o = (float*)((char*)p.lse2 + delta_bytes(g));
     p.pieces = kv_pieces(g);
     const hipStream_t s = (hipStream_t)stream;
     if (p.kv_doc && launch_masked_ranges(p, s) != hipSuccess) return PCPP_EHIP;

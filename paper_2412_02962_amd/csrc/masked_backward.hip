@@ -75,6 +75,30 @@ __device__ __forceinline__ void store_rows(bf16* row, const f32x16 (&acc)[DB], f
         }
 }
 
+// A row of gradients, or a piece's float32 part of it, in one pass over the
+// registers.
+template <int DB>
+__device__ __forceinline__ void store_sums(bf16* row, float* part, const f32x16 (&acc)[DB], float f, int D, int lane) {
+#pragma unroll
+    for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c = 32 * mb + 8 * g;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[mb][4 * g + e] * f;
+            if (part != nullptr) {
+                *(f32x4*)(part + c + 4 * (lane >> 5)) = v;
+            } else if (c < D) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(v[e]);
+                *(bf16x4*)(row + c + 4 * (lane >> 5)) = o;
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (all products at once would be registers for all)
+        }
+}
+
 template <int DB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     using T = Tile<DB>;
@@ -84,10 +108,10 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + BLOCK - 1) / BLOCK;
-    const int64_t id = place_in((int64_t)p.B * p.H * nqb);
-    if (id < 0) return;
-    const int bh = (int)(id / nqb), qb = nqb - 1 - (int)(id - (int64_t)bh * nqb);  // the longest first
-    const int b = bh / p.H, head = bh - b * p.H, kh = head / p.G;
+    const Place place = place_in((int64_t)p.B * p.H, nqb, p.causal);
+    if (place.item < 0) return;
+    const int bh = place.item, qb = nqb - 1 - place.block;
+    const int b = scalar(bh / p.H), head = bh - b * p.H, kh = scalar(head / p.G);
     const Seq sq = seq_of(p, b);
     const int i0 = qb * BLOCK, last = min(i0 + BLOCK, p.nq) - 1;
     const int w0 = i0 + 32 * wave, wlast = min(w0 + 32, p.nq) - 1;
@@ -180,15 +204,22 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
 
     clear<DB>(acc);
     int slot = 0, t = window.next(0);
-    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
-    if (t < end) issue(t, slot);
+    bool same = true, apart = false, same_all = true;
+    auto look = [&](int of, bool& a, bool& b_, bool& c_) { a = window.same(of), b_ = window.apart(of), c_ = window.same_all(of); };
+    if (t < end) {
+        look(t, same, apart, same_all);
+        issue(t, slot);
+    }
     while (t < end) {
         landed();
         if (p.kv_doc && tid < TILE) docs[slot][tid] = dr;
         __syncthreads();  // the tile is there, and nobody reads the one before any more
         const int tn = window.next(t + 1);
-        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
-        if (tn < end) issue(tn, slot ^ 1);
+        bool same_n = true, apart_n = false, same_all_n = true;
+        if (tn < end) {
+            look(tn, same_n, apart_n, same_all_n);
+            issue(tn, slot ^ 1);
+        }
         char* kt = lds + slot * SLOT;
         if ((t + 1) * TILE > least || !same_all) {
             bool bad = false;
@@ -211,11 +242,14 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     }
     off = sum_halves(off);
     if (!in) return;
-    if (lane < 32) p.delta[(int64_t)bh * p.nq + i] = delta + off;
+    if (lane < 32) {
+        p.delta[(int64_t)bh * p.nq + i] = -(delta + off);
+        p.lse2[(int64_t)bh * p.nq + i] = -lse2;
+    }
     if (p.dq) store_rows<DB>(p.dq + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, acc, CAP ? 4.f * p.scale : p.scale, p.D, lane);
 }
 
-// What a tile's queries bring besides q and dy; delta negative.
+// What a tile's queries bring besides q and dy, as masked_dq left it.
 template <int ROWS>
 struct QueryTile {
     float lse2[ROWS], delta[ROWS];
@@ -227,7 +261,7 @@ struct QueryTile {
 // 64 queries; above, where the two sums alone take half the registers that two
 // wavefronts of a SIMD have, V in LDS and tiles of 32 queries.
 template <int DB, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
+__global__ __launch_bounds__(NT, DB == 1 ? 3 : 2) void masked_dkv(Params p) {
     using T = Tile<DB>;
     constexpr int ROWS = DB <= 2 ? 64 : 32, TB = ROWS * T::RB;
     constexpr int SLOT = 2 * TB;  // Q, dy
@@ -235,14 +269,15 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
     constexpr int LDS = 2 * SLOT + (V_LDS ? BLOCK * T::RB : 0);
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ __attribute__((aligned(16))) QueryTile<ROWS> brought[2];
+    __shared__ Spoilt spoilt[NT];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nkb = (p.nkv + BLOCK - 1) / BLOCK;
-    const int64_t id = place_in((int64_t)p.B * p.KH * nkb * p.pieces);
-    if (id < 0) return;
-    const int item = (int)(id / nkb), kb = (int)(id - (int64_t)item * nkb);
-    const int bk = item / p.pieces, piece = item - bk * p.pieces;
-    const int b = bk / p.KH, kh = bk - b * p.KH;
+    const Place place = place_in((int64_t)p.B * p.KH * p.pieces, nkb, p.causal);
+    if (place.item < 0) return;
+    const int item = place.item, kb = place.block;  // (the first keys are seen by the most)
+    const int bk = scalar(item / p.pieces), piece = item - bk * p.pieces;
+    const int b = scalar(bk / p.KH), kh = bk - b * p.KH;
     const Seq sq = seq_of(p, b);
     const int k0 = kb * BLOCK, klast = min(k0 + BLOCK, p.nkv) - 1;
     const int w0 = k0 + 32 * wave;
@@ -250,7 +285,7 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
     const bool in = j < p.nkv, live = j < sq.len;
     const int doc = live && p.kv_doc ? own_document(p.kv_doc[(int64_t)b * p.nkv + j]) : NO_DOC;
     // The queries that see key j by length, past and prefix: from .. nq - 1.
-    const int from = !live ? p.nq : !p.causal || j < sq.prefix ? 0 : min(max(j - sq.pos0, 0), p.nq);
+    const int from = !live || (p.kv_doc && doc == NO_DOC) ? p.nq : !p.causal || j < sq.prefix ? 0 : min(max(j - sq.pos0, 0), p.nq);
     if (V_LDS || p.D < 32 * DB) {
         clear_tiles(lds, LDS, NT);
         __syncthreads();
@@ -276,7 +311,7 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
     if (k0 >= sq.len) first = nt;
     const int tiles = nt - min(first, nt);
     const int64_t all_tiles = (int64_t)tiles * p.G;
-    const int64_t u0 = all_tiles * piece / p.pieces, u1 = all_tiles * (piece + 1) / p.pieces;
+    const int u0 = scalar((int)(all_tiles * piece / p.pieces)), u1 = scalar((int)(all_tiles * (piece + 1) / p.pieces));
     DocWindow window;
     {
         DocRange all = {}, mine = {};
@@ -296,18 +331,17 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
 
     const Loader<DB, NW, ROWS> qload(p.q_row, p.D, wave, lane), gload(p.y_row, p.D, wave, lane);
     const uint32_t lds0 = lds_address(lds);
-    float lr = 0.f, er = 0.f;
-    int dr = -1;
+    const uint32_t brought0 = lds_address(brought);
     auto issue = [&](int g, int t, int slot) {
         const int head = kh * p.G + g;
         qload.issue(p.q + b * p.q_batch + head * p.D, t * ROWS, p.nq, lds0 + slot * SLOT);
         gload.issue(p.dy + b * p.y_batch + head * p.D, t * ROWS, p.nq, lds0 + slot * SLOT + TB);
         if (tid < ROWS) {
-            const int i = min(t * ROWS + tid, p.nq - 1);
-            const int64_t at = ((int64_t)b * p.H + head) * p.nq + i;
-            lr = p.lse[at] * -LOG2E;
-            er = -p.delta[at];
-            if (p.q_doc) dr = max(p.q_doc[(int64_t)b * p.nq + i], -1);
+            const uint32_t at = 4 * min(tid, p.nq - 1 - t * ROWS), to = brought0 + slot * sizeof(QueryTile<ROWS>);
+            const int64_t row = ((int64_t)b * p.H + head) * p.nq + t * ROWS;
+            load_lds4(uniform64((uint64_t)(uintptr_t)(p.lse2 + row)), at, to);
+            load_lds4(uniform64((uint64_t)(uintptr_t)(p.delta + row)), at, to + 4 * ROWS);
+            if (p.q_doc) load_lds4(uniform64((uint64_t)(uintptr_t)(p.q_doc + (int64_t)b * p.nq + t * ROWS)), at, to + 8 * ROWS);
         }
     };
 
@@ -374,16 +408,16 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
         add_rows<DB>(dk, o, rd, qt, row0);
     };
 
+    spoilt[tid] = Spoilt{0, 0};
     clear<DB>(dk);
     clear<DB>(dv);
-    Spoilt<DB> spoilt = {};
     int slot = 0, g = 0, t = 0;
     bool more = u0 < u1, same = true, apart = false, same_all = true;
     // From tile t of head g on: the first that counts, and whether this piece has it.
     auto settle = [&](int& hg, int& ht) {
         while (hg < p.G) {
             ht = next(ht);
-            if (ht < nt) return (int64_t)hg * tiles + ht - first < u1;
+            if (ht < nt) return hg * tiles + ht - first < u1;
             ++hg;
             ht = first;
         }
@@ -394,8 +428,8 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
         a = window.same(w), c = window.apart(w), d = window.same_all(w);
     };
     if (more) {
-        g = (int)(u0 / tiles);
-        t = first + (int)(u0 - (int64_t)g * tiles);
+        g = scalar(u0 / tiles);
+        t = first + u0 - g * tiles;
         more = settle(g, t);
     }
     if (more) {
@@ -404,11 +438,6 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
     }
     while (more) {
         landed();
-        if (tid < ROWS) {
-            brought[slot].lse2[tid] = lr;
-            brought[slot].delta[tid] = er;
-            brought[slot].doc[tid] = dr;
-        }
         __syncthreads();  // the tile is there, and nobody reads the one before any more
         int gn = g, tn = t + 1;
         const bool more_n = settle(gn, tn);
@@ -422,7 +451,7 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
         const int i0 = t * ROWS;
         if (i0 + ROWS > p.nq || k0 + BLOCK > limit_of(p, sq, i0) || !same_all) {
             bool bad = false;
-#pragma unroll
+#pragma unroll 1
             for (int o = 0; o < SLOT; o += 16 * NT) bad |= not_finite16(qt + o + 16 * tid);
             if (__syncthreads_or(bad)) {
                 for (int h = 0; h < ROWS; h += 32) {
@@ -431,7 +460,7 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
                         const int i = i0 + h + r, d = brought[slot].doc[h + r];
                         seen |= (uint32_t)((i >= from) & (i < p.nq) & (!p.kv_doc || d == doc)) << r;
                     }
-                    spoilt.note(qt + TB, h, seen, lane);
+                    note_spoilt<DB>(spoilt + tid, qt + TB, h, seen, lane);
                 }
                 // (a query that is no number has none in its lse, and so none in P and dz)
                 __syncthreads();
@@ -448,26 +477,12 @@ __global__ __launch_bounds__(NT, DB > 3 ? 1 : 2) void masked_dkv(Params p) {
         g = gn, t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
         slot ^= 1;
     }
-    spoilt.put(dv);
+    put_spoilt<DB>(spoilt + tid, dv);
     if (!in) return;
-    const float f = CAP ? 4.f * p.scale : p.scale;
-    if (p.pieces > 1) {
-        constexpr int CH = 32 * DB;
-        float* o = p.part_o + (((int64_t)piece * p.B * p.KH + bk) * p.nkv + j) * (2 * CH) + 4 * half;
-#pragma unroll
-        for (int mb = 0; mb < DB; ++mb)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                f32x4 a, c;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = dk[mb][4 * q4 + e] * f, c[e] = dv[mb][4 * q4 + e];
-                *(f32x4*)(o + 32 * mb + 8 * q4) = a;
-                *(f32x4*)(o + CH + 32 * mb + 8 * q4) = c;
-            }
-        return;
-    }
-    store_rows<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, dk, f, p.D, lane);
-    store_rows<DB>(p.dv + b * p.v_batch + (int64_t)j * p.v_row + kh * p.D, dv, 1.f, p.D, lane);
+    constexpr int CH = 32 * DB;
+    float* part = p.pieces > 1 ? p.part_o + (((int64_t)piece * p.B * p.KH + bk) * p.nkv + j) * (2 * CH) : nullptr;
+    store_sums<DB>(p.dk + b * p.k_batch + (int64_t)j * p.k_row + kh * p.D, part, dk, CAP ? 4.f * p.scale : p.scale, p.D, lane);
+    store_sums<DB>(p.dv + b * p.v_batch + (int64_t)j * p.v_row + kh * p.D, part ? part + CH : nullptr, dv, 1.f, p.D, lane);
 }
 
 // The pieces' sums, in their order: eight channels of dk or dv of a key a thread.

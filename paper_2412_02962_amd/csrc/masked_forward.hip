@@ -60,20 +60,30 @@ struct Context {
 // the products cost nothing and a token's error counts).
 template <int DB, bool CAP, bool BIAS, bool TWO>
 __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs,
-                                     int row0, int j0, bool partial) {
+                                     int row0, int j0, bool partial, bool first) {
     const Params& p = c.p;
     const Row& row = c.row;
     const Reader<DB> rd = c.rd.fresh();
     const int half = c.lane >> 5;
-    f32x16 s;
-#pragma unroll
-    for (int kk = 0; kk < 2 * DB; ++kk) s = mfma32x32x16(rd.rows(kt, row0, kk), c.q[kk], kk == 0 ? f32x16{} : s);
     const int base = j0 + 4 * half;
     const float far = (float)(row.pos - base);
-    // Scores less the maximum, in log2 units; -infinity where not seen (also
-    // while the maximum is still -infinity and all others are infinite).
-    float w[16], sum;
-    auto scores = [&](float add) __attribute__((always_inline)) {
+    // Mostly once round.  Where the probabilities by the maximum so far are too
+    // large, a second time for the scores' maximum and a third by that one (the
+    // scores are computed again: registers for them would be held all along).
+    // The first step of all begins with the maximum.
+    bool search = first, tried = false;
+    float w[16];
+    bf16x8 pr[2];
+    float sum;
+    uint32_t over = search ? ~0u : 0u;  // the lanes that need another maximum
+#pragma unroll 1
+    for (;;) {
+        f32x16 s;
+#pragma unroll
+        for (int kk = 0; kk < 2 * DB; ++kk) s = mfma32x32x16(rd.rows(kt, row0, kk), c.q[kk], kk == 0 ? f32x16{} : s);
+        // Scores less the maximum, in log2 units; -infinity where not seen (also
+        // while the maximum is still -infinity and all others are infinite).
+        const float add = search ? 0.f : -st.m;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             w[r] = score<CAP>(p, s[r], add);
@@ -92,10 +102,25 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
                 }
             }
         }
-    };
-    bf16x8 pr[2];
-    auto exps = [&]() __attribute__((always_inline)) {
-        float a = 0.f;
+        if (search) {
+            float mx = w[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, w[r]);
+            // (each query by its own sums: what others see is nothing to it)
+            const float m_new = over ? fmaxf(st.m, max_halves(mx)) : st.m;
+            const float alpha = m_new == st.m ? 1.f : fast_exp2(st.m - m_new);
+            st.m = m_new;
+            st.l *= alpha;
+#pragma unroll
+            for (int mb = 0; mb < DB; ++mb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st.o[mb][r] *= alpha;
+            search = false;
+            over = 0;
+            tried = true;
+            continue;
+        }
+        sum = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             w[r] = fast_exp2(w[r]);
@@ -104,31 +129,13 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
             pr[r >> 3][r & 7] = pk[0];
             pr[r >> 3][(r & 7) + 1] = pk[1];
             if constexpr (TWO)
-                a += w[r] + w[r + 1];
+                sum += w[r] + w[r + 1];
             else
-                a = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, a, false);
+                sum = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, sum, false);
         }
-        sum = a;
-    };
-    scores(-st.m);
-    exps();
-    if (__any(!(sum < P_LIMIT))) {
-        scores(0.f);
-        float mx = w[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, w[r]);
-        // (each query by its own sums: what others see is nothing to it)
-        const bool over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
-        const float m_new = over ? fmaxf(st.m, max_halves(mx)) : st.m;
-        const float alpha = m_new == st.m ? 1.f : fast_exp2(st.m - m_new);
-        st.m = m_new;
-        st.l *= alpha;
-#pragma unroll
-        for (int mb = 0; mb < DB; ++mb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) st.o[mb][r] *= alpha;
-        scores(-st.m);
-        exps();
+        if (tried || !__any(!(sum < P_LIMIT))) break;
+        over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
+        search = true;
     }
     st.l += sum;
     add_rows<DB>(st.o, pr, rd, vt, row0);
@@ -167,18 +174,19 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
 }
 
 template <int DB, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
+__global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) {
     using T = Tile<DB>;
     constexpr int SLOT = 2 * T::BYTES;  // K, V
     __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
     __shared__ __attribute__((aligned(16))) int docs[2][TILE];
+    __shared__ Spoilt spoilt[NT];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + QB - 1) / QB;
-    const int64_t id = place_in((int64_t)p.B * p.H * nqb);
-    if (id < 0) return;
-    const int bh = (int)(id / nqb), qb = nqb - 1 - (int)(id - (int64_t)bh * nqb);  // the longest first
-    const int b = bh / p.H, head = bh - b * p.H, kh = head / p.G;
+    const Place place = place_in((int64_t)p.B * p.H, nqb, p.causal);
+    if (place.item < 0) return;
+    const int bh = place.item, qb = nqb - 1 - place.block;
+    const int b = scalar(bh / p.H), head = bh - b * p.H, kh = scalar(head / p.G);
     const Seq sq = seq_of(p, b);
     const int i0 = qb * QB, last = min(i0 + QB, p.nq) - 1;
     const int w0 = i0 + 32 * wave, wlast = min(w0 + 32, p.nq) - 1;  // the wavefront's queries (w0 > wlast: none)
@@ -219,27 +227,39 @@ __global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
         __syncthreads();
     }
 
+    spoilt[tid] = Spoilt{0, 0};
     State<DB> st;
     clear(st);
+    bool first = true;
     const Context<DB> c = {p, q, row, rd, lane};
-    int slot = 0, t = window.next(0);
-    bool same = window.same(t), apart = window.apart(t), same_all = window.same_all(t);
-    Spoilt<DB> spoilt = {};
-    if (t < end) issue(t, slot);
-    while (t < end) {
+    TileOrder order = {-1, end, false};
+    if (BIAS && end > 0 && sq.pos0 + last >= 0) order.start = min((sq.pos0 + last) / TILE, end - 1);
+    int slot = 0, t;
+    bool more = order.first(window, t), same = true, apart = false, same_all = true;
+    auto look = [&](int of, bool& a, bool& b_, bool& c_) { a = window.same(of), b_ = window.apart(of), c_ = window.same_all(of); };
+    if (more) {
+        look(t, same, apart, same_all);
+        issue(t, slot);
+    }
+    while (more) {
         landed();
         if (p.kv_doc && tid < TILE) docs[slot][tid] = dr;
         __syncthreads();  // the tile is there, and nobody reads the one before any more
-        const int tn = window.next(t + 1);
-        const bool same_n = window.same(tn), apart_n = window.apart(tn), same_all_n = window.same_all(tn);
-        if (tn < end) issue(tn, slot ^ 1);
+        int tn = t;
+        bool same_n = true, apart_n = false, same_all_n = true;
+        const bool more_n = order.advance(window, tn);
+        if (more_n) {
+            look(tn, same_n, apart_n, same_all_n);
+            issue(tn, slot ^ 1);
+        }
         char *kt = lds + slot * SLOT, *vt = kt + T::BYTES;
         if ((t + 1) * TILE > least || !same_all) {
             bool bad = false;
 #pragma unroll
             for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(vt + o + 16 * tid);
             if (__syncthreads_or(bad)) {
-                for (int h = 0; h < 2; ++h) spoilt.note(vt, 32 * h, keys_seen(p, row, docs[slot] + 32 * h, t * TILE + 32 * h), lane);
+                for (int h = 0; h < 2; ++h)
+                    note_spoilt<DB>(spoilt + tid, vt, 32 * h, keys_seen(p, row, docs[slot] + 32 * h, t * TILE + 32 * h), lane);
                 __syncthreads();
                 for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(vt + o + 16 * tid);
                 __syncthreads();
@@ -249,12 +269,13 @@ __global__ __launch_bounds__(NT, 2) void masked_forward(Params p) {
         for (int h = 0; h < 2; ++h) {
             const int j0 = t * TILE + 32 * h;
             if (j0 >= lim_hi || apart) continue;
-            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same);
+            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same, first);
+            first = false;
         }
-        t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
+        t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
         slot ^= 1;
     }
-    spoilt.put(st.o);
+    put_spoilt<DB>(spoilt + tid, st.o);
 
     const float l = sum_halves(st.l);
     if (!in) return;
@@ -289,6 +310,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     __shared__ __attribute__((aligned(16))) char lds_all[NW * 2 * SLOT];
     __shared__ __attribute__((aligned(16))) int docs[NW][2][FEW_KEYS];
     __shared__ float ml[NW][32][2];
+    __shared__ Spoilt spoilt[NT];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int piece = blockIdx.x % p.pieces, rest = blockIdx.x / p.pieces;
@@ -313,27 +335,29 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     const Reader<DB> rd(lane);
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
-    // Every NW-th tile from t on that may hold a document of the rows, 64
-    // looked over at a time.
-    int base = -64 * NW;
+    // Every NW-th tile from t down that may hold a document of the rows, 64
+    // looked over at a time.  (The queries stand at the end, as a rule, and with
+    // a bias by distance the largest scores there too: from there the maximum
+    // does not move.)
+    int base = 1 << 30;
     uint64_t meets = 0, whole = 0;
     auto next = [&](int t) {
         if (!p.kv_doc) return t;
-        while (t < t1) {
-            if (t >= base + 64 * NW || t < base) {
+        while (t >= t0) {
+            if (base == 1 << 30 || t <= base - 64 * NW) {
                 base = t;
-                const int u = t + NW * lane;
-                const DocRange r = u < t1 ? ranges[u / 2] : DocRange{0x7fffffff, -1};
+                const int u = t - NW * lane;
+                const DocRange r = u >= t0 ? ranges[u / 2] : DocRange{0x7fffffff, -1};
                 meets = __ballot(ranges_meet(r, mine));
                 whole = __ballot(same_document(r, mine));
             }
-            const uint64_t m = meets >> ((t - base) / NW);
-            if (m) return t + NW * (int)__builtin_ctzll(m);
-            t = base + 64 * NW;
+            const uint64_t m = meets >> ((base - t) / NW);
+            if (m) return t - NW * (int)__builtin_ctzll(m);
+            t = base - 64 * NW;
         }
         return t;
     };
-    auto same = [&](int t) { return !p.kv_doc || (t < t1 && (whole >> ((t - base) / NW) & 1)); };
+    auto same = [&](int t) { return !p.kv_doc || (t >= t0 && (whole >> ((base - t) / NW) & 1)); };
     int dr = -1;
     auto issue = [&](int t, int slot) {
         kload.issue(kb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT);
@@ -345,22 +369,23 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
         __syncthreads();
     }
 
+    spoilt[tid] = Spoilt{0, 0};
     State<DB> st;
     clear(st);
+    bool first = true;
     const Context<DB> c = {p, q, row, rd, lane};
-    int slot = 0, t = next(t0 + wave);
+    int slot = 0, t = next(t1 - 1 - wave);
     bool whole_t = same(t);
-    Spoilt<DB> spoilt = {};
-    if (t < t1) issue(t, slot);
-    while (t < t1) {
+    if (t >= t0) issue(t, slot);
+    while (t >= t0) {
         landed();
         if (p.kv_doc && lane < FEW_KEYS) docs[wave][slot][lane] = dr;
-        const int tn = next(t + NW);
+        const int tn = next(t - NW);
         const bool whole_n = same(tn);
         // (the other slot has been read: the products of the tile before have
         // waited for that, or this does)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (tn < t1) issue(tn, slot ^ 1);
+        if (tn >= t0) issue(tn, slot ^ 1);
         const int j0 = t * FEW_KEYS;
         char *kt = lds + slot * SLOT, *vt = kt + HALF;
         const bool partial = j0 + FEW_KEYS > lim_lo || !whole_t;
@@ -368,16 +393,17 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
             bool bad = false;
             for (int o = 0; o < HALF; o += 1024) bad |= not_finite16(vt + o + 16 * lane);
             if (__any(bad)) {
-                spoilt.note(vt, 0, keys_seen(p, row, docs[wave][slot], j0), lane);
+                note_spoilt<DB>(spoilt + tid, vt, 0, keys_seen(p, row, docs[wave][slot], j0), lane);
                 for (int o = 0; o < HALF; o += 1024) make_finite16(vt + o + 16 * lane);
             }
         }
-        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial);
+        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first);
+        first = false;
         t = tn, whole_t = whole_n;
         slot ^= 1;
     }
 
-    spoilt.put(st.o);
+    put_spoilt<DB>(spoilt + tid, st.o);
 
     // The wavefronts' results on one maximum, and their sum.
     const float l = sum_halves(st.l);
