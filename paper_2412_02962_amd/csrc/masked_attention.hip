@@ -111,7 +111,7 @@ int64_t delta_bytes(const pcpp_masked_geom_t* g) { return round16((int64_t)g->ba
 int kv_pieces(const pcpp_masked_geom_t* g) {
     const int64_t blocks = (int64_t)g->batch * g->kv_heads * ((g->n_kv + 127) / 128);
     const int64_t tiles = (int64_t)g->heads / g->kv_heads * ((g->n_q + 63) / 64);
-    int64_t n = (512 + blocks - 1) / blocks;
+    int64_t n = ((g->causal ? 1024 : 512) + blocks - 1) / blocks;
     if (n > tiles / 8) n = tiles / 8;
     return (int)(n < 1 ? 1 : n);
 }
