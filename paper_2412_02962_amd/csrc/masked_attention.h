@@ -58,6 +58,9 @@ struct Params {
     float* part_ml;
 };
 
+// Blocks of 32 channels that a head of D is worked in (a tile's rows have 64
+// channels at least).
+__host__ __device__ inline int blocks_of(int D) { return D <= 64 ? 2 : (D + 31) / 32; }
 __host__ __device__ inline int tiles_of(int n) { return (n + TILE - 1) / TILE; }
 
 // Sequence b's keys, first position and prefix.
@@ -108,17 +111,21 @@ __device__ __forceinline__ float score(const Params& p, float dot, float add, fl
     }
 }
 
-// ---- tiles in LDS: 64 rows of RB bytes, the channels behind a head's 0.  The
-// 16 bytes c of row r lie at c ^ swizzle(r): rows read at one channel by 32
-// lanes, and four rows of 32 bytes by the 16 lanes of a transposing read, then
-// lie in different banks.  The swizzle repeats every eight rows. ----
+// ---- tiles in LDS: rows of RB bytes, the channels behind a head's 0.  The 16
+// bytes c of row r lie at c ^ swizzle(r).  LDS serves 256 bytes at a time: 16
+// rows at one channel (row reads), or four rows of 64 bytes (transposing reads
+// by 32 lanes); either lies in different banks.  The swizzle repeats every 16
+// rows, and eight rows on it differs in bit 1. ----
 
 template <int DB>
 struct Tile {
     static constexpr int RB = DB <= 2 ? 128 : 256;  // bytes of a row
     static constexpr int VECS = RB / 16;
     static constexpr int BYTES = TILE * RB;
-    __device__ static __forceinline__ int swizzle(int r) { return RB == 128 ? ((r >> 1) & 3) << 1 : (r & 7) << 1; }
+    __device__ static __forceinline__ int swizzle(int r) {
+        if constexpr (RB == 256) return (r & 3) << 2 | (r >> 2 & 3);
+        return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    }
 };
 
 // 16 bytes per lane from a wave-uniform base and a lane's offset straight into
@@ -152,19 +159,22 @@ struct Loader {
     using T = Tile<DB>;
     static constexpr int PIECES = ROWS * T::RB / 1024 / NW;
     static constexpr int PIECE_ROWS = 1024 / T::RB;
-    static_assert(PIECES >= 1 && (T::RB == 128 || PIECES % 2 == 0), "shares");
+    static_assert(PIECES >= 1, "shares");
+    static constexpr int PERIOD = 16 / PIECE_ROWS;  // pieces until the swizzle repeats
+    static constexpr int KINDS = PIECES < PERIOD ? PIECES : PERIOD;
+    static_assert(PIECES % KINDS == 0 && (PIECES >= PERIOD ? PIECES % PERIOD == 0 : PERIOD % PIECES == 0), "pieces i and i + KINDS are of a kind");
     uint32_t row_bytes;
-    uint32_t off[2];  // of the pieces of even and of odd number: their swizzles differ where a piece has four rows
+    uint32_t off[KINDS];
     int row, first;
-    int in;  // bit i: the lane's channels in pieces of parity i are the head's (the others stay 0 in LDS)
+    int in;  // bit i: the lane's channels in pieces of kind i are the head's (the others stay 0 in LDS)
     __device__ __forceinline__ Loader(int64_t row_elements, int D, int wave, int lane) {
         row_bytes = (uint32_t)(2 * row_elements);
         row = lane / T::VECS;
         first = PIECES * wave;
         in = 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int c = (lane % T::VECS) ^ T::swizzle(row + i * PIECE_ROWS);
+        for (int i = 0; i < KINDS; ++i) {
+            const int c = (lane % T::VECS) ^ T::swizzle(row + (first + i) * PIECE_ROWS);
             off[i] = (uint32_t)row * row_bytes + 16 * c;
             in |= (8 * c < D) << i;
         }
@@ -176,14 +186,14 @@ struct Loader {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int piece = first + i;
-                if (in >> (i & 1) & 1) load_lds(at + (uint64_t)(piece * PIECE_ROWS) * row_bytes, off[i & 1], lds + 1024 * piece);
+                if (in >> (i % KINDS) & 1) load_lds(at + (uint64_t)(piece * PIECE_ROWS) * row_bytes, off[i % KINDS], lds + 1024 * piece);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int piece = first + i, r = piece * PIECE_ROWS + row, last = rows - 1 - row0;
-                const uint32_t o = off[i & 1] + (uint32_t)(min(r, last) - row) * row_bytes;
-                if (in >> (i & 1) & 1) load_lds(at, o, lds + 1024 * piece);
+                const uint32_t o = off[i % KINDS] + (uint32_t)(min(r, last) - row) * row_bytes;
+                if (in >> (i % KINDS) & 1) load_lds(at, o, lds + 1024 * piece);
             }
         }
     }
@@ -197,7 +207,7 @@ struct Reader {
     uint32_t row_at, col_at;
     __device__ __forceinline__ explicit Reader(int lane) {
         const int r = lane & 31;
-        row_at = (uint32_t)(r * T::RB + 16 * (lane >> 5) + 16 * T::swizzle(r));
+        row_at = (uint32_t)(r * T::RB + 16 * ((lane >> 5) ^ T::swizzle(r)));
         const int t = 4 * (lane >> 5) + ((lane & 15) >> 2), e = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
         col_at = (uint32_t)(t * T::RB + 16 * ((e >> 3) ^ T::swizzle(t)) + 2 * (e & 7));
     }
@@ -219,9 +229,9 @@ struct Reader {
     __device__ __forceinline__ bf16x8 columns(const char* tile, int row0, int mb) const {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const char* a = tile + row0 * T::RB + (col_at ^ (64 * mb));
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 8 * T::RB));
+        const char* a = tile + row0 * T::RB;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + (col_at ^ (64 * mb))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 8 * T::RB + (col_at ^ (64 * mb + 32))));
         const short __attribute__((ext_vector_type(8))) w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(bf16x8, w);
     }
@@ -488,8 +498,7 @@ hipError_t with_shape(const masked::Params& p, F f) {
         if (p.cap2 != 0.f) return f(db, bool_constant<true>(), bool_constant<true>());
         return p.slopes ? f(db, bool_constant<false>(), bool_constant<true>()) : f(db, bool_constant<false>(), bool_constant<false>());
     };
-    switch ((p.D + 31) / 32) {
-        case 1: return variant(integral_constant<int, 1>());
+    switch (masked::blocks_of(p.D)) {
         case 2: return variant(integral_constant<int, 2>());
         case 3: return variant(integral_constant<int, 3>());
         default: return variant(integral_constant<int, 4>());

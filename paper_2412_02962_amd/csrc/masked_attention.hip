@@ -100,7 +100,7 @@ FewPlan few_plan(const pcpp_masked_geom_t* g) {
 int64_t few_blocks(const pcpp_masked_geom_t* g, const FewPlan& f) {
     return f.use && f.pieces > 1 ? (int64_t)g->batch * g->kv_heads * f.row_blocks * f.pieces : 0;
 }
-int64_t few_floats(const pcpp_masked_geom_t* g) { return (int64_t)MASKED_FEW_ROWS * ((g->head_dim + 31) / 32 * 32); }
+int64_t few_floats(const pcpp_masked_geom_t* g) { return (int64_t)MASKED_FEW_ROWS * (32 * blocks_of(g->head_dim)); }
 
 int64_t forward_bytes(const pcpp_masked_geom_t* g) {
     return range_bytes(g) + few_blocks(g, few_plan(g)) * (few_floats(g) + 2 * MASKED_FEW_ROWS) * 4;
@@ -117,7 +117,7 @@ int kv_pieces(const pcpp_masked_geom_t* g) {
 }
 int64_t kv_bytes(const pcpp_masked_geom_t* g) {
     const int n = kv_pieces(g);
-    return n == 1 ? 0 : (int64_t)n * g->batch * g->kv_heads * g->n_kv * 2 * ((g->head_dim + 31) / 32 * 32) * 4;
+    return n == 1 ? 0 : (int64_t)n * g->batch * g->kv_heads * g->n_kv * 2 * (32 * blocks_of(g->head_dim)) * 4;
 }
 int64_t backward_bytes(const pcpp_masked_geom_t* g) { return range_bytes(g) + 2 * delta_bytes(g) + kv_bytes(g); }
 

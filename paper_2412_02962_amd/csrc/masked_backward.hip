@@ -182,12 +182,16 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
                 w[r] = seen ? w[r] : 0.f;
                 if constexpr (CAP) dp[r] = seen ? dp[r] : 0.f;
             };
+            int lim = limit - base;
+            asm volatile("" : "+v"(lim));  // (a branch, not selections in every step)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) keep(r, 8 * (r >> 2) + (r & 3) < limit - base);
+            for (int r = 0; r < 16; ++r) keep(r, 8 * (r >> 2) + (r & 3) < lim);
             if (p.kv_doc) {
+                int at = row0 + 4 * half;
+                asm volatile("" : "+v"(at));
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const i32x4 d = *(const i32x4*)(dt + row0 + 8 * g + 4 * half);
+                    const i32x4 d = *(const i32x4*)(dt + at + 8 * g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) keep(4 * g + e, d[e] == doc);
                 }
@@ -261,7 +265,7 @@ struct QueryTile {
 // 64 queries; above, where the two sums alone take half the registers that two
 // wavefronts of a SIMD have, V in LDS and tiles of 32 queries.
 template <int DB, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, DB == 1 ? 3 : 2) void masked_dkv(Params p) {
+__global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     using T = Tile<DB>;
     constexpr int ROWS = DB <= 2 ? 64 : 32, TB = ROWS * T::RB;
     constexpr int SLOT = 2 * TB;  // Q, dy
@@ -387,13 +391,17 @@ __global__ __launch_bounds__(NT, DB == 1 ? 3 : 2) void masked_dkv(Params p) {
                 w[r] = seen ? w[r] : 0.f;
                 z[r] = seen ? z[r] : 0.f;
             };
-            const uint32_t lo = from - base, n = max(p.nq - from, 0);  // rows lo .. lo + n - 1, in one comparison
+            uint32_t lo = from - base;
+            const uint32_t n = max(p.nq - from, 0);  // rows lo .. lo + n - 1, in one comparison
+            asm volatile("" : "+v"(lo));             // (a branch, not selections in every step)
 #pragma unroll
             for (int r = 0; r < 16; ++r) keep(r, (uint32_t)(8 * (r >> 2) + (r & 3)) - lo < n);
             if (p.kv_doc) {
+                int at = row0 + 4 * half;
+                asm volatile("" : "+v"(at));
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const i32x4 d = *(const i32x4*)(rows.doc + row0 + 8 * g + 4 * half);
+                    const i32x4 d = *(const i32x4*)(rows.doc + at + 8 * g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) keep(4 * g + e, d[e] == doc);
                 }
@@ -532,7 +540,7 @@ hipError_t launch_masked_dkv(const Params& p, hipStream_t s) {
         return hipGetLastError();
     });
     if (e != hipSuccess || p.pieces == 1) return e;
-    const int ch = (p.D + 31) / 32 * 32;
+    const int ch = 32 * blocks_of(p.D);
     const int64_t threads = (int64_t)p.B * p.KH * p.nkv * (2 * ch / 8);
     masked_join_kv<<<(unsigned)((threads + NT - 1) / NT), NT, 0, s>>>(p, ch);
     return hipGetLastError();

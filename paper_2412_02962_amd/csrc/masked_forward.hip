@@ -90,13 +90,16 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
             if constexpr (BIAS) w[r] = __builtin_fmaf(-row.slope2, fabsf(far - (float)(8 * (r >> 2) + (r & 3))), w[r]);
         }
         if (partial) {
-            const int limit = row.limit - base;
+            int limit = row.limit - base;
+            asm volatile("" : "+v"(limit));  // (a branch, not selections in every step)
 #pragma unroll
             for (int r = 0; r < 16; ++r) w[r] = 8 * (r >> 2) + (r & 3) < limit ? w[r] : -INFINITY;
             if (p.kv_doc) {
+                int at = row0 + 4 * half;
+                asm volatile("" : "+v"(at));
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const i32x4 d = *(const i32x4*)(docs + row0 + 8 * g + 4 * half);
+                    const i32x4 d = *(const i32x4*)(docs + at + 8 * g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[4 * g + e] = d[e] == row.doc ? w[4 * g + e] : -INFINITY;
                 }
