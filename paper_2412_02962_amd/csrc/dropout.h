@@ -58,14 +58,27 @@ __device__ __forceinline__ u32x4 philox(const DropoutKey& k, uint64_t block) {
     return u32x4{c0, c1, c2, c3};
 }
 
-// The eight elements of block `block`: scaled, or 0 (whatever they were).
-__device__ __forceinline__ void drop8(const Dropout& d, const DropoutKey& k, uint64_t block, float (&v)[8]) {
+// The eight elements of block `block`: as they are, or 0 (whatever they were).
+__device__ __forceinline__ void keep8(const Dropout& d, const DropoutKey& k, uint64_t block, float (&v)[8]) {
     const u32x4 w = philox(k, block);
+    // compared in the upper halves, where a least of 2^16 would be lost: no
+    // element is kept then
+    const uint32_t least = d.least << 16, none = d.least >> 16;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu;
-        v[e] = bits >= d.least ? v[e] * d.factor : 0.f;
+        const uint32_t bits = e & 1 ? w[e >> 1] : w[e >> 1] << 16;
+        v[e] = bits >= least ? v[e] : 0.f;
     }
+    if (none)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+}
+
+// The same, what is kept scaled.
+__device__ __forceinline__ void drop8(const Dropout& d, const DropoutKey& k, uint64_t block, float (&v)[8]) {
+    keep8(d, k, block, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= d.factor;
 }
 
 }  // namespace pcpp

@@ -32,7 +32,9 @@ namespace {
 
 constexpr int kMaxThreads = 512;
 constexpr int kMaxGroups = 256;
-constexpr int kMaxChunks = 64;
+constexpr int kRunRows = 8;      // rows that a thread of the statistics takes at a time
+constexpr int kBlocks = 512;     // workgroups of a launch that sums: two to a compute unit
+constexpr int kFewChunks = 32;   // chunks whose records every consumer merges; more are merged in a launch of their own
 
 // How a launch cuts [B, N, C]: slabs of S channels (whole groups), chunks of
 // tokens; a thread holds one vector of V in a row, RP rows side by side.
@@ -52,6 +54,7 @@ struct NormActParams {
     void* y;             // forward's y, backward's dx
     float* stats;        // [B][G][2] mean, rstd: forward writes it (or null), backward reads it
     float* records;      // forward [B][chunks][G][3] count, mean, M2; backward [B][chunks][G][2] sums of w, w n
+    float* merged;       // the records of all chunks as one, or null: `records` are few
     float* columns;      // backward: [2][B * chunks][C] sums of g n and g, or null
     bf16* dgamma;
     bf16* dbeta;
@@ -61,13 +64,60 @@ struct NormActParams {
     float eps;
 };
 
+// Eight channels as they lie in memory, so that rows on their way take few
+// registers.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<bf16> {
+    bf16x8 a;
+    __device__ __forceinline__ void load(const bf16* p) { a = *(const bf16x8*)p; }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32(a[e]);
+    }
+};
+template <>
+struct Raw<float> {
+    f32x4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = *(const f32x4*)p;
+        b = *(const f32x4*)(p + 4);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+    }
+};
+
+// A thread's rows t, t + RP, .. of a tensor, ROWS at a time, the next ROWS on
+// their way while these are worked on.
+template <typename T, int ROWS>
+struct Rows {
+    Raw<T> cur[ROWS], next[ROWS];
+    __device__ __forceinline__ static void fetch(Raw<T> (&to)[ROWS], const T* base, int t, int hi, const Cut& a) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (t + i * a.RP < hi) to[i].load(base + (int64_t)(t + i * a.RP) * a.C);
+    }
+    __device__ __forceinline__ void begin(const T* base, int t, int hi, const Cut& a) { fetch(cur, base, t, hi, a); }
+    __device__ __forceinline__ void ahead(const T* base, int t, int hi, const Cut& a) { fetch(next, base, t + ROWS * a.RP, hi, a); }
+    __device__ __forceinline__ void step() {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) cur[i] = next[i];
+    }
+};
+
+// c / cg without a division, by the inverse: exact for c below 2^13.
+__device__ __forceinline__ int group_of(int c, float inv_cg) { return (int)(((float)c + 0.5f) * inv_cg); }
+
 // Row lane, vector and channel of a thread; false for the threads left over.
 struct Place {
     int r, v, c0;
     bool in;
 };
 __device__ __forceinline__ Place place_of(const Cut& a, int slab) {
-    const int r = threadIdx.x / a.V, v = threadIdx.x - r * a.V;
+    const int r = group_of(threadIdx.x, 1.f / (float)a.V), v = threadIdx.x - r * a.V;
     return Place{r, v, slab * a.S + 8 * v, r < a.RP};
 }
 
@@ -102,17 +152,20 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
     for (int e = 0; e < 8; ++e) mean[e] = m2[e] = 0.f;
     float n = 0.f;
     if (at.in) {
-        for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
+        Rows<T, ROWS> xs;
+        int t = lo + at.r;
+        xs.begin(x, t, hi, a);
+        for (; t < hi; t += a.RP * ROWS, xs.step()) {
+            xs.ahead(x, t, hi, a);
             float v[ROWS][8];
             int rows = 0;
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
+                const bool here = t + i * a.RP < hi;
+                xs.cur[i].get(v[i]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-                if (t + i * a.RP < hi) {
-                    load8(x + (int64_t)(t + i * a.RP) * a.C, v[i]);
-                    rows = i + 1;
-                }
+                for (int e = 0; e < 8; ++e) v[i][e] = here ? v[i][e] : 0.f;
+                rows += here;
             }
             const float cnt = (float)rows, total = n + cnt;
             const float share = cnt / total, both = n * share;
@@ -142,17 +195,18 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
     const int g = threadIdx.x / T_, l = threadIdx.x % T_;
     const bool mine = g < a.gs;
     const int entries = mine ? a.RP * a.cg : 0;
+    const float inv_cg = 1.f / (float)a.cg;
     auto rows_of = [&](int r) { return (float)max(0, (hi - lo - r + a.RP - 1) / a.RP); };
     float sum = 0.f;
     for (int i = l; i < entries; i += T_) {
-        const int r = i / a.cg, c = g * a.cg + i - r * a.cg;
+        const int r = group_of(i, inv_cg), c = g * a.cg + i - r * a.cg;
         sum = __builtin_fmaf(rows_of(r), lds_mean[r * a.S + c], sum);
     }
     const float count = (float)(hi - lo) * (float)a.cg;
     const float gm = lanes_sum(sum, T_) / count;
     float q = 0.f;
     for (int i = l; i < entries; i += T_) {
-        const int r = i / a.cg, c = g * a.cg + i - r * a.cg;
+        const int r = group_of(i, inv_cg), c = g * a.cg + i - r * a.cg;
         const float d = lds_mean[r * a.S + c] - gm;
         q += __builtin_fmaf(d * d, rows_of(r), lds_m2[r * a.S + c]);
     }
@@ -162,6 +216,72 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
         o[0] = count;
         o[1] = gm;
         o[2] = q;
+    }
+}
+
+// The records of more than kFewChunks chunks as one: a workgroup to a group, and
+// a thread to two records, so that all are on their way at once (4.9 us with a
+// wavefront that walks them).
+constexpr int kMergeThreads = 256;
+static_assert(kBlocks <= 2 * kMergeThreads, "two records a thread");
+
+// The sum of v over the workgroup.
+__device__ __forceinline__ float block_sum(float v, float* lds) {
+    v = lanes_sum(v, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kMergeThreads / 64; ++w) t += lds[w];
+    return t;
+}
+__global__ __launch_bounds__(kMergeThreads) void norm_act_merge_stats(NormActParams p) {
+    __shared__ float lds[kMergeThreads / 64];
+    const Cut a = p.cut;
+    const int g = blockIdx.x, b = blockIdx.y;
+    const float* rec = p.records + ((int64_t)b * a.chunks * a.G + g) * 3;
+    const float count = (float)a.N * (float)a.cg;
+    float r[2][3];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int i = threadIdx.x + u * kMergeThreads;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) r[u][k] = i < a.chunks ? rec[(int64_t)i * a.G * 3 + k] : 0.f;
+    }
+    const float m = block_sum(__builtin_fmaf(r[0][0], r[0][1], r[1][0] * r[1][1]), lds) / count;
+    float q = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const float d = r[u][1] - m;
+        q += __builtin_fmaf(d * d, r[u][0], r[u][2]);
+    }
+    q = block_sum(q, lds);
+    if (threadIdx.x == 0) {
+        float* o = p.merged + ((int64_t)b * a.G + g) * 3;
+        o[0] = count;
+        o[1] = m;
+        o[2] = q;
+    }
+}
+__global__ __launch_bounds__(kMergeThreads) void norm_act_merge_sums(NormActParams p) {
+    __shared__ float lds[kMergeThreads / 64];
+    const Cut a = p.cut;
+    const int g = blockIdx.x, b = blockIdx.y;
+    const float* rec = p.records + ((int64_t)b * a.chunks * a.G + g) * 2;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int i = threadIdx.x + u * kMergeThreads;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k] += i < a.chunks ? rec[(int64_t)i * a.G * 2 + k] : 0.f;
+    }
+    s[0] = block_sum(s[0], lds);
+    s[1] = block_sum(s[1], lds);
+    if (threadIdx.x == 0) {
+        float* o = p.merged + ((int64_t)b * a.G + g) * 2;
+        o[0] = s[0];
+        o[1] = s[1];
     }
 }
 
@@ -182,16 +302,24 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_apply(NormActParams p) {
     __shared__ float g_mean[kMaxGroups], g_rstd[kMaxGroups];
     const Cut a = p.cut;
     const int slab = blockIdx.y, b = blockIdx.z;
+    const Place at = place_of(a, slab);
+    const int lo = (int)((int64_t)a.N * blockIdx.x / p.apply_blocks), hi = (int)((int64_t)a.N * (blockIdx.x + 1) / p.apply_blocks);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    const T* x = (const T*)p.x + base;
+    Rows<T, ROWS> xs;
+    int t = lo + at.r;
+    if (at.in) xs.begin(x, t, hi, a);  // (on their way while the records are merged)
     {
         const int T_ = group_lanes(a.threads, a.gs);
         const int g = threadIdx.x / T_, l = threadIdx.x % T_;
         const bool mine = g < a.gs;
-        const float* rec = p.records + ((int64_t)b * a.chunks * a.G + slab * a.gs + (mine ? g : 0)) * 3;
+        const int chunks = p.merged ? 1 : a.chunks;
+        const float* rec = (p.merged ? p.merged : p.records) + ((int64_t)b * chunks * a.G + slab * a.gs + (mine ? g : 0)) * 3;
         float sum = 0.f, q = 0.f;
         const float count = (float)a.N * (float)a.cg;
-        for (int i = l; i < a.chunks; i += T_) sum = __builtin_fmaf(rec[(int64_t)i * a.G * 3], rec[(int64_t)i * a.G * 3 + 1], sum);
+        for (int i = l; i < chunks; i += T_) sum = __builtin_fmaf(rec[(int64_t)i * a.G * 3], rec[(int64_t)i * a.G * 3 + 1], sum);
         const float m = lanes_sum(sum, T_) / count;
-        for (int i = l; i < a.chunks; i += T_) {
+        for (int i = l; i < chunks; i += T_) {
             const float* o = rec + (int64_t)i * a.G * 3;
             const float d = o[1] - m;
             q += __builtin_fmaf(d * d, o[0], o[2]);
@@ -209,66 +337,67 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_apply(NormActParams p) {
         }
     }
     __syncthreads();
-    const Place at = place_of(a, slab);
     if (!at.in) return;
-    float mean[8], rstd[8], gamma[8], beta[8];
+    float mean[8], rstd[8];
+    const float inv_cg = 1.f / (float)a.cg;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int g = (8 * at.v + e) / a.cg;
+        const int g = group_of(8 * at.v + e, inv_cg);
         mean[e] = g_mean[g];
         rstd[e] = g_rstd[g];
     }
-    load8(p.gamma + at.c0, gamma);
-    load8(p.beta + at.c0, beta);
+    const bf16x8 gamma = *(const bf16x8*)(p.gamma + at.c0), beta = *(const bf16x8*)(p.beta + at.c0);
     const DropoutKey key = dropout_key(p.drop);
-    const int lo = (int)((int64_t)a.N * blockIdx.x / p.apply_blocks), hi = (int)((int64_t)a.N * (blockIdx.x + 1) / p.apply_blocks);
-    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
-    for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
-        float v[ROWS][8];
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            if (t + i * a.RP < hi) load8((const T*)p.x + base + (int64_t)(t + i * a.RP) * a.C, v[i]);
+    for (; t < hi; t += a.RP * ROWS, xs.step()) {
+        xs.ahead(x, t, hi, a);
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             if (t + i * a.RP >= hi) break;
             const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
+            float v[8];
+            xs.cur[i].get(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                v[i][e] = act_of<ACT>(__builtin_fmaf((v[i][e] - mean[e]) * rstd[e], gamma[e], beta[e]), nullptr);
-            if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, v[i]);
-            store8((T*)p.y + o, v[i]);
+                v[e] = act_of<ACT>(__builtin_fmaf((v[e] - mean[e]) * rstd[e], bf16_to_f32(gamma[e]), bf16_to_f32(beta[e])), nullptr);
+            if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, v);
+            store8((T*)p.y + o, v);
         }
     }
 }
 
 // ---- backward ----
 
-// g and n of eight channels of a row: v holds x, d holds dy.
+// A thread's channels.
+struct Channels {
+    float mean[8], rstd[8];
+    bf16x8 gamma, beta;
+    __device__ __forceinline__ Channels(const NormActParams& p, const Place& at, int slab, int b) {
+        const Cut& a = p.cut;
+        const float inv_cg = 1.f / (float)a.cg;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float* s = p.stats + ((int64_t)b * a.G + slab * a.gs + group_of(8 * at.v + e, inv_cg)) * 2;
+            mean[e] = s[0];
+            rstd[e] = s[1];
+        }
+        gamma = *(const bf16x8*)(p.gamma + at.c0);
+        beta = *(const bf16x8*)(p.beta + at.c0);
+    }
+};
+
+// Eight channels of the row at o: v, x, becomes n; d, dy, becomes g but for
+// dropout's factor, which all have in common.
 template <int ACT>
-__device__ __forceinline__ void grad8(const NormActParams& p, const DropoutKey& key, int64_t o, const float (&mean)[8],
-                                      const float (&rstd)[8], const float (&gamma)[8], const float (&beta)[8],
+__device__ __forceinline__ void grad8(const NormActParams& p, const DropoutKey& key, int64_t o, const Channels& c,
                                       float (&v)[8], float (&d)[8]) {
-    if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, d);
+    if (p.drop.least > 0) keep8(p.drop, key, (uint64_t)o / 8, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        v[e] = (v[e] - mean[e]) * rstd[e];
+        v[e] = (v[e] - c.mean[e]) * c.rstd[e];
         float da;
-        act_of<ACT>(__builtin_fmaf(v[e], gamma[e], beta[e]), &da);
+        act_of<ACT>(__builtin_fmaf(v[e], bf16_to_f32(c.gamma[e]), bf16_to_f32(c.beta[e])), &da);
         d[e] *= da;
     }
-}
-
-__device__ __forceinline__ void load_params(const NormActParams& p, const Place& at, int slab, int b, float (&mean)[8],
-                                            float (&rstd)[8], float (&gamma)[8], float (&beta)[8]) {
-    const Cut& a = p.cut;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float* s = p.stats + ((int64_t)b * a.G + slab * a.gs + (8 * at.v + e) / a.cg) * 2;
-        mean[e] = s[0];
-        rstd[e] = s[1];
-    }
-    load8(p.gamma + at.c0, gamma);
-    load8(p.beta + at.c0, beta);
 }
 
 template <typename T, int ACT, int ROWS>
@@ -279,30 +408,31 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_sums(NormActParams 
     const int lo = (int)((int64_t)a.N * chunk / a.chunks), hi = (int)((int64_t)a.N * (chunk + 1) / a.chunks);
     const Place at = place_of(a, slab);
     if (at.in) {
-        float mean[8], rstd[8], gamma[8], beta[8], sn[8], sg[8];
-        load_params(p, at, slab, b, mean, rstd, gamma, beta);
+        const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+        const T *x = (const T*)p.x + base, *dy = (const T*)p.dy + base;
+        Rows<T, ROWS> xs, ds;
+        int t = lo + at.r;
+        xs.begin(x, t, hi, a);
+        ds.begin(dy, t, hi, a);
+        const Channels ch(p, at, slab, b);
+        float sn[8], sg[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) sn[e] = sg[e] = 0.f;
         const DropoutKey key = dropout_key(p.drop);
-        const int64_t base = (int64_t)b * a.N * a.C + at.c0;
-        for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
-            float v[ROWS][8], d[ROWS][8];
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                if (t + i * a.RP < hi) {
-                    const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
-                    load8((const T*)p.x + o, v[i]);
-                    load8((const T*)p.dy + o, d[i]);
-                }
-            }
+        for (; t < hi; t += a.RP * ROWS, xs.step(), ds.step()) {
+            xs.ahead(x, t, hi, a);
+            ds.ahead(dy, t, hi, a);
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
                 if (t + i * a.RP >= hi) break;
-                grad8<ACT>(p, key, base + (int64_t)(t + i * a.RP) * a.C, mean, rstd, gamma, beta, v[i], d[i]);
+                float v[8], d[8];
+                xs.cur[i].get(v);
+                ds.cur[i].get(d);
+                grad8<ACT>(p, key, base + (int64_t)(t + i * a.RP) * a.C, ch, v, d);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    sn[e] = __builtin_fmaf(d[i][e], v[i][e], sn[e]);
-                    sg[e] += d[i][e];
+                    sn[e] = __builtin_fmaf(d[e], v[e], sn[e]);
+                    sg[e] += d[e];
                 }
             }
         }
@@ -315,6 +445,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_sums(NormActParams 
         for (int r = 0; r < a.RP; ++r) {
             tn += lds_n[r * a.S + c];
             tg += lds_g[r * a.S + c];
+        }
+        if (p.drop.least > 0) {
+            tn *= p.drop.factor;
+            tg *= p.drop.factor;
         }
         if (p.columns != nullptr) {
             float* o = p.columns + ((int64_t)b * a.chunks + chunk) * a.C + slab * a.S + c;
@@ -352,8 +486,17 @@ __device__ __forceinline__ void column_totals(const NormActParams& p, int block,
     const int c = 16 * (block - which * per) + l, rows = a.B * a.chunks;
     const float* in = p.columns + (int64_t)which * rows * a.C;
     float t = 0.f;
-    if (c < a.C)
-        for (int i = r; i < rows; i += lanes) t += in[(int64_t)i * a.C + c];
+    if (c < a.C) {
+        int i = r;
+        for (; i + 7 * lanes < rows; i += 8 * lanes) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = in[(int64_t)(i + u * lanes) * a.C + c];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t += v[u];
+        }
+        for (; i < rows; i += lanes) t += in[(int64_t)i * a.C + c];
+    }
     lds[17 * r + l] = t;
     __syncthreads();
     bf16* out = which ? p.dbeta : p.dgamma;
@@ -379,13 +522,24 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_apply(NormActParams
     }
     const int part = (int)(blockIdx.x % p.apply_blocks), sb = (int)(blockIdx.x / p.apply_blocks);
     const int slab = sb % slabs, b = sb / slabs;
+    const Place at = place_of(a, slab);
+    const int lo = (int)((int64_t)a.N * part / p.apply_blocks), hi = (int)((int64_t)a.N * (part + 1) / p.apply_blocks);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    const T *x = (const T*)p.x + base, *dy = (const T*)p.dy + base;
+    Rows<T, ROWS> xs, ds;
+    int t = lo + at.r;
+    if (at.in) {  // (on their way while the records are merged)
+        xs.begin(x, t, hi, a);
+        ds.begin(dy, t, hi, a);
+    }
     {
         const int T_ = group_lanes(a.threads, a.gs);
         const int g = threadIdx.x / T_, l = threadIdx.x % T_;
         const bool mine = g < a.gs;
-        const float* rec = p.records + ((int64_t)b * a.chunks * a.G + slab * a.gs + (mine ? g : 0)) * 2;
+        const int chunks = p.merged ? 1 : a.chunks;
+        const float* rec = (p.merged ? p.merged : p.records) + ((int64_t)b * chunks * a.G + slab * a.gs + (mine ? g : 0)) * 2;
         float s0 = 0.f, s1 = 0.f;
-        for (int i = l; i < a.chunks; i += T_) {
+        for (int i = l; i < chunks; i += T_) {
             s0 += rec[(int64_t)i * a.G * 2];
             s1 += rec[(int64_t)i * a.G * 2 + 1];
         }
@@ -398,44 +552,42 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_apply(NormActParams
         }
     }
     __syncthreads();
-    const Place at = place_of(a, slab);
     if (!at.in) return;
-    float mean[8], rstd[8], gamma[8], beta[8], m0[8], m1[8];
-    load_params(p, at, slab, b, mean, rstd, gamma, beta);
+    const Channels ch(p, at, slab, b);
+    float m0[8], m1[8], gamma[8];
+    const float inv_cg = 1.f / (float)a.cg;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int g = (8 * at.v + e) / a.cg;
+        const int g = group_of(8 * at.v + e, inv_cg);
         m0[e] = g_m0[g];
         m1[e] = g_m1[g];
+        gamma[e] = bf16_to_f32(ch.gamma[e]) * (p.drop.least > 0 ? p.drop.factor : 1.f);
     }
     const DropoutKey key = dropout_key(p.drop);
-    const int lo = (int)((int64_t)a.N * part / p.apply_blocks), hi = (int)((int64_t)a.N * (part + 1) / p.apply_blocks);
-    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
-    for (int t = lo + at.r; t < hi; t += a.RP * ROWS) {
-        float v[ROWS][8], d[ROWS][8];
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            if (t + i * a.RP < hi) {
-                const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
-                load8((const T*)p.x + o, v[i]);
-                load8((const T*)p.dy + o, d[i]);
-            }
-        }
+    for (; t < hi; t += a.RP * ROWS, xs.step(), ds.step()) {
+        xs.ahead(x, t, hi, a);
+        ds.ahead(dy, t, hi, a);
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             if (t + i * a.RP >= hi) break;
             const int64_t o = base + (int64_t)(t + i * a.RP) * a.C;
-            grad8<ACT>(p, key, o, mean, rstd, gamma, beta, v[i], d[i]);
+            float v[8], d[8];
+            xs.cur[i].get(v);
+            ds.cur[i].get(d);
+            grad8<ACT>(p, key, o, ch, v, d);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d[i][e] = rstd[e] * (__builtin_fmaf(d[i][e], gamma[e], -m0[e]) - v[i][e] * m1[e]);
-            store8((T*)p.y + o, d[i]);
+            for (int e = 0; e < 8; ++e) d[e] = ch.rstd[e] * (__builtin_fmaf(d[e], gamma[e], -m0[e]) - v[e] * m1[e]);
+            store8((T*)p.y + o, d);
         }
     }
 }
 
 int gcd_of(int a, int b) { return b == 0 ? a : gcd_of(b, a % b); }
 
-// Slabs as wide as still give the chip its workgroups.
+// Whole rows where the tokens alone make enough workgroups: every row is one run
+// of memory.  Else slabs, as wide as still give the chip its workgroups.  256
+// threads, though some of them may be idle (2 x 57600 x 640 bf16 with 240 of 256
+// at work 288 us forward and backward, with 320 of 320 at work 348).
 Cut cut_of(int B, int N, int C, int G) {
     Cut best = {};
     const int cg = C / G, least = 8 / gcd_of(8, cg);  // groups whose channels are whole vectors; divides G as 8 divides C
@@ -444,11 +596,16 @@ Cut cut_of(int B, int N, int C, int G) {
         Cut a = {B, N, C, G, cg, gs * cg, gs * cg / 8, 0, gs, 0, 256};
         if (a.V > 256) a.threads = kMaxThreads;
         a.RP = a.threads / a.V;
-        const int64_t fit = (N + 8 * a.RP - 1) / (8 * a.RP);
-        a.chunks = (int)(fit < kMaxChunks ? fit : kMaxChunks);
+        const int64_t fit = (N + kRunRows * a.RP - 1) / (kRunRows * a.RP);
+        if (gs == G && B * fit >= kBlocks) {
+            const int64_t most = (kBlocks + B - 1) / B;
+            a.chunks = (int)(fit < most ? fit : most);
+            return a;
+        }
+        a.chunks = (int)(fit < kFewChunks ? fit : kFewChunks);
         if (best.B != 0 && (a.V < 8 || 5 * a.V * a.RP < 4 * best.V * best.RP)) continue;
         best = a;
-        if ((int64_t)B * (G / gs) * a.chunks >= 512) break;
+        if ((int64_t)B * (G / gs) * a.chunks >= kBlocks) break;
     }
     return best;
 }
@@ -461,8 +618,11 @@ int apply_blocks_of(const Cut& a) {
     return (int)(n > 0 ? n : 1);
 }
 
-int64_t stats_floats(const Cut& a) { return (int64_t)a.B * a.chunks * a.G * 3; }
-int64_t grad_floats(const Cut& a) { return (int64_t)a.B * a.chunks * (2 * (int64_t)a.C + 2 * a.G); }
+// [merged][records], and backward [columns].
+int64_t merged_floats(const Cut& a) { return ((int64_t)a.B * a.G * 3 + 3) / 4 * 4; }
+int64_t stats_floats(const Cut& a) { return merged_floats(a) + (int64_t)a.B * a.chunks * a.G * 3; }
+int64_t grad_records(const Cut& a) { return (int64_t)a.B * a.chunks * 2 * a.G; }
+int64_t grad_floats(const Cut& a) { return merged_floats(a) + grad_records(a) + (int64_t)a.B * a.chunks * 2 * a.C; }
 
 template <typename F>
 void with_act(int act, F f) {
@@ -520,7 +680,8 @@ PCPP_EXPORT int pcpp_group_norm_act(const pcpp_norm_act_geom_t* g, const void* x
     p.beta = (const bf16*)beta;
     p.y = y;
     p.stats = stats;
-    p.records = (float*)workspace;
+    p.records = (float*)workspace + merged_floats(a);
+    p.merged = a.chunks > kFewChunks ? (float*)workspace : nullptr;
     p.drop = make_dropout(g->drop, rng, draw);
     p.cut = a;
     p.apply_blocks = apply_blocks_of(a);
@@ -528,13 +689,14 @@ PCPP_EXPORT int pcpp_group_norm_act(const pcpp_norm_act_geom_t* g, const void* x
     const hipStream_t s = (hipStream_t)stream;
     const dim3 sums(a.chunks, a.C / a.S, a.B), apply(p.apply_blocks, a.C / a.S, a.B);
     if (g->dtype == PCPP_DTYPE_F32)
-        norm_act_stats<float, 8><<<sums, a.threads, 0, s>>>(p);
+        norm_act_stats<float, kRunRows / 2><<<sums, a.threads, 0, s>>>(p);
     else
-        norm_act_stats<bf16, 8><<<sums, a.threads, 0, s>>>(p);
+        norm_act_stats<bf16, kRunRows><<<sums, a.threads, 0, s>>>(p);
+    if (p.merged) norm_act_merge_stats<<<dim3(a.G, a.B), kMergeThreads, 0, s>>>(p);
     if (hipGetLastError() != hipSuccess) return PCPP_EHIP;
     with_act(g->act, [&](auto act) {
         if (g->dtype == PCPP_DTYPE_F32)
-            norm_act_apply<float, act(), 4><<<apply, a.threads, 0, s>>>(p);
+            norm_act_apply<float, act(), 2><<<apply, a.threads, 0, s>>>(p);
         else
             norm_act_apply<bf16, act(), 4><<<apply, a.threads, 0, s>>>(p);
     });
@@ -569,8 +731,9 @@ PCPP_EXPORT int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, cons
     p.beta = (const bf16*)beta;
     p.y = dx;
     p.stats = (float*)stats;
-    p.records = (float*)workspace;
-    p.columns = dgamma || dbeta ? (float*)workspace + (int64_t)a.B * a.chunks * 2 * a.G : nullptr;
+    p.records = (float*)workspace + merged_floats(a);
+    p.merged = a.chunks > kFewChunks ? (float*)workspace : nullptr;
+    p.columns = dgamma || dbeta ? p.records + grad_records(a) : nullptr;
     p.dgamma = (bf16*)dgamma;
     p.dbeta = (bf16*)dbeta;
     p.drop = make_dropout(g->drop, rng, draw);
@@ -581,16 +744,17 @@ PCPP_EXPORT int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, cons
     const int64_t blocks = (int64_t)p.apply_blocks * (a.C / a.S) * a.B + column_blocks(p);
     with_act(g->act, [&](auto act) {
         if (g->dtype == PCPP_DTYPE_F32)
-            norm_act_grad_sums<float, act(), 4><<<sums, a.threads, 0, s>>>(p);
+            norm_act_grad_sums<float, act(), 1><<<sums, a.threads, 0, s>>>(p);
         else
-            norm_act_grad_sums<bf16, act(), 4><<<sums, a.threads, 0, s>>>(p);
+            norm_act_grad_sums<bf16, act(), 2><<<sums, a.threads, 0, s>>>(p);
     });
+    if (p.merged) norm_act_merge_sums<<<dim3(a.G, a.B), kMergeThreads, 0, s>>>(p);
     if (hipGetLastError() != hipSuccess) return PCPP_EHIP;
     with_act(g->act, [&](auto act) {
         if (g->dtype == PCPP_DTYPE_F32)
-            norm_act_grad_apply<float, act(), 4><<<(unsigned)blocks, a.threads, 0, s>>>(p);
+            norm_act_grad_apply<float, act(), 1><<<(unsigned)blocks, a.threads, 0, s>>>(p);
         else
-            norm_act_grad_apply<bf16, act(), 4><<<(unsigned)blocks, a.threads, 0, s>>>(p);
+            norm_act_grad_apply<bf16, act(), 2><<<(unsigned)blocks, a.threads, 0, s>>>(p);
     });
     return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }

@@ -466,15 +466,33 @@ __global__ __launch_bounds__(NT) void masked_join(Params p) {
     const int b = bk / p.KH, kh = bk - b * p.KH;
     const float* po = p.part_o + ((int64_t)rest * p.pieces * (16 * DB) + reg) * 64 + lane;
     const float* pml = p.part_ml + ((int64_t)rest * p.pieces * 32 + col) * 2;
-    float m = -INFINITY;
-    for (int k = 0; k < p.pieces; ++k) m = fmaxf(m, pml[(int64_t)k * 64]);
-    float v = 0.f, total = 0.f;
-    for (int k = 0; k < p.pieces; ++k) {
-        const float mk = pml[(int64_t)k * 64];
-        if (mk == -INFINITY) continue;
-        const float f = mk == m ? 1.f : fast_exp2(mk - m);
-        total = __builtin_fmaf(pml[(int64_t)k * 64 + 1], f, total);
-        v = __builtin_fmaf(po[(int64_t)k * (16 * DB * 64)], f, v);
+    // Eight pieces at a time, all of their loads on their way together.
+    float m = -INFINITY, v = 0.f, total = 0.f;
+    for (int k0 = 0; k0 < p.pieces; k0 += 8) {
+        float mk[8], lk[8], ok[8], top = m;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int k = min(k0 + u, p.pieces - 1);
+            mk[u] = pml[(int64_t)k * 64];
+            lk[u] = pml[(int64_t)k * 64 + 1];
+            ok[u] = po[(int64_t)k * (16 * DB * 64)];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (k0 + u >= p.pieces) mk[u] = -INFINITY;
+            top = fmaxf(top, mk[u]);
+        }
+        const float f = m == top ? 1.f : fast_exp2(m - top);  // (both may be -infinity)
+        v *= f;
+        total *= f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (mk[u] == -INFINITY) continue;  // (nothing seen: its sums are 0)
+            const float w = mk[u] == top ? 1.f : fast_exp2(mk[u] - top);
+            total = __builtin_fmaf(lk[u], w, total);
+            v = __builtin_fmaf(ok[u], w, v);
+        }
+        m = top;
     }
     const int rows = p.G * p.nq, rho = rb * MASKED_FEW_ROWS + col;
     if (rho >= rows) return;
