@@ -220,8 +220,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
 }
 
 // The records of more than kFewChunks chunks as one: a workgroup to a group, and
-// a thread to two records, so that all are on their way at once (4.9 us with a
-// wavefront that walks them).
+// a thread to two records, so that all are on their way at once.
 constexpr int kMergeThreads = 256;
 static_assert(kBlocks <= 2 * kMergeThreads, "two records a thread");
 

@@ -131,13 +131,16 @@ struct Tile {
 // 16 bytes per lane from a wave-uniform base and a lane's offset straight into
 // LDS, lane l's at lds + 16 l.  In assembly, since the compiler's own tracking
 // of such writes would wait for all of them before any LDS read; the kernels
-// order them by landed() and barriers.
+// order them by landed() and barriers.  The base may come out of a vector
+// instruction (a lane read) right before: a load may read such a scalar five
+// instructions later at the earliest, and within assembly the compiler does not
+// see to that.
 __device__ __forceinline__ void load_lds(uint64_t base, uint32_t off, uint32_t lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 // The same of 4 bytes, lane l's at lds + 4 l.
 __device__ __forceinline__ void load_lds4(uint64_t base, uint32_t off, uint32_t lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+    asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
