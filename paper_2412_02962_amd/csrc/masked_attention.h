@@ -372,6 +372,17 @@ __device__ __forceinline__ Place place_in(int64_t items, int blocks, bool fallin
 }
 inline unsigned blocks_for(int64_t n) { return (unsigned)((n + PARTS - 1) / PARTS * PARTS); }
 
+// Rows of a tensor as the second operand of a product over channels: row
+// (lane % 32), zeros where there is none.
+template <int DB>
+__device__ __forceinline__ void load_rows(const bf16* row, bool in, int D, bf16x8 (&o)[2 * DB], int lane) {
+#pragma unroll
+    for (int kk = 0; kk < 2 * DB; ++kk) {
+        const int c = 16 * kk + 8 * (lane >> 5);
+        o[kk] = in && c < D ? *(const bf16x8*)(row + c) : bf16x8{};
+    }
+}
+
 // Sixteen registers as two operands.
 __device__ __forceinline__ void pack(const float (&w)[16], bf16x8 (&o)[2]) {
 #pragma unroll

@@ -50,17 +50,6 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[DB]) {
         for (int r = 0; r < 16; ++r) acc[mb][r] = 0.f;
 }
 
-// Rows of a tensor as the second operand of a product over channels: row
-// (lane % 32), zeros where there is none.
-template <int DB>
-__device__ __forceinline__ void load_rows(const bf16* row, bool in, int D, bf16x8 (&o)[2 * DB], int lane) {
-#pragma unroll
-    for (int kk = 0; kk < 2 * DB; ++kk) {
-        const int c = 16 * kk + 8 * (lane >> 5);
-        o[kk] = in && c < D ? *(const bf16x8*)(row + c) : bf16x8{};
-    }
-}
-
 template <int DB>
 __device__ __forceinline__ void store_rows(bf16* row, const f32x16 (&acc)[DB], float f, int D, int lane) {
 #pragma unroll

@@ -58,9 +58,10 @@ struct Context {
 // 32 keys from key j0, rows row0 of the tiles in LDS.  partial: some query does
 // not see some key.  TWO: the probabilities as two bf16 (for few queries, where
 // the products cost nothing and a token's error counts).
-template <int DB, bool CAP, bool BIAS, bool TWO>
+// after_scores: what may run once the keys have been used.
+template <int DB, bool CAP, bool BIAS, bool TWO, typename After>
 __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs,
-                                     int row0, int j0, bool partial, bool first) {
+                                     int row0, int j0, bool partial, bool first, After after_scores) {
     const Params& p = c.p;
     const Row& row = c.row;
     const Reader<DB> rd = c.rd.fresh();
@@ -101,7 +102,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
                 for (int g = 0; g < 4; ++g) {
                     const i32x4 d = *(const i32x4*)(docs + at + 8 * g);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[4 * g + e] = d[e] == row.doc ? w[4 * g + e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) w[4 * g + e] = (TWO ? max(d[e], -1) : d[e]) == row.doc ? w[4 * g + e] : -INFINITY;
                 }
             }
         }
@@ -140,6 +141,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
         over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
         search = true;
     }
+    after_scores();
     st.l += sum;
     add_rows<DB>(st.o, pr, rd, vt, row0);
     if constexpr (TWO) {
@@ -154,17 +156,8 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
 __device__ __forceinline__ uint32_t keys_seen(const Params& p, const Row& row, const int* docs, int j0) {
     uint32_t seen = 0;
     for (int j = 0; j < 32; ++j)
-        seen |= (uint32_t)((j0 + j < row.limit) & (!p.kv_doc || docs[j] == row.doc)) << j;
+        seen |= (uint32_t)((j0 + j < row.limit) & (!p.kv_doc || max(docs[j], -1) == row.doc)) << j;
     return seen;
-}
-
-template <int DB>
-__device__ __forceinline__ void load_query(const Params& p, const bf16* row, bool in, bf16x8 (&q)[2 * DB], int lane) {
-#pragma unroll
-    for (int kk = 0; kk < 2 * DB; ++kk) {
-        const int c = 16 * kk + 8 * (lane >> 5);
-        q[kk] = in && c < p.D ? *(const bf16x8*)(row + c) : bf16x8{};
-    }
 }
 
 __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int head, int i, bool in) {
@@ -197,7 +190,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     const bool in = i < p.nq;
     const Row row = row_of(p, sq, b, head, i, in);
     bf16x8 q[2 * DB];
-    load_query<DB>(p, p.q + b * p.q_batch + (int64_t)min(i, p.nq - 1) * p.q_row + head * p.D, in, q, lane);
+    load_rows<DB>(p.q + b * p.q_batch + (int64_t)min(i, p.nq - 1) * p.q_row + head * p.D, in, p.D, q, lane);
 
     const int end = tiles_of(limit_of(p, sq, last));
     const int lim_lo = limit_of(p, sq, w0), lim_hi = w0 <= wlast ? limit_of(p, sq, wlast) : 0;
@@ -272,7 +265,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
         for (int h = 0; h < 2; ++h) {
             const int j0 = t * TILE + 32 * h;
             if (j0 >= lim_hi || apart) continue;
-            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same, first);
+            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same, first, []() {});
             first = false;
         }
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
@@ -325,7 +318,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     const int g = min(rho, rows - 1) / p.nq, i = min(rho, rows - 1) - g * p.nq, head = kh * p.G + g;
     const Row row = row_of(p, sq, b, head, i, true);
     bf16x8 q[2 * DB];
-    load_query<DB>(p, p.q + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, true, q, lane);
+    load_rows<DB>(p.q + b * p.q_batch + (int64_t)i * p.q_row + head * p.D, true, p.D, q, lane);
     DocRange mine = {};
     if (p.kv_doc) mine = range_of_lanes(row.doc, true);
     const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
@@ -334,7 +327,8 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     const int t0 = (int)((int64_t)tiles * piece / p.pieces), t1 = (int)((int64_t)tiles * (piece + 1) / p.pieces);
     char* lds = lds_all + wave * 2 * SLOT;
     const uint32_t lds0 = lds_address(lds);
-    const Loader<DB, 1, FEW_KEYS> kload(p.k_row, p.D, 0, lane), vload(p.v_row, p.D, 0, lane);
+    using Load = Loader<DB, 1, FEW_KEYS>;
+    const Load kload(p.k_row, p.D, 0, lane), vload(p.v_row, p.D, 0, lane);
     const Reader<DB> rd(lane);
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
@@ -362,10 +356,15 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     };
     auto same = [&](int t) { return !p.kv_doc || (t >= t0 && (whole >> ((base - t) / NW) & 1)); };
     int dr = -1;
-    auto issue = [&](int t, int slot) {
-        kload.issue(kb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT);
+    // Keys and values of two tiles are on their way at a time, each into the
+    // place of those just used.
+    const uint32_t docs0 = lds_address(docs[wave]);
+    auto issue_k = [&](int t, int slot) { kload.issue(kb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT); };
+    auto issue_v = [&](int t, int slot) {
         vload.issue(vb, t * FEW_KEYS, sq.len, lds0 + slot * SLOT + HALF);
-        if (p.kv_doc) dr = lane < FEW_KEYS && t * FEW_KEYS + lane < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * FEW_KEYS + lane], -1) : -1;
+        if (p.kv_doc && lane < FEW_KEYS)
+            load_lds4(uniform64((uint64_t)(uintptr_t)(p.kv_doc + (int64_t)b * p.nkv + t * FEW_KEYS)), 4 * min(lane, sq.len - 1 - t * FEW_KEYS),
+                      docs0 + slot * FEW_KEYS * 4);
     };
     if (p.D < 32 * DB) {
         clear_tiles(lds_all, NW * 2 * SLOT, NT);
@@ -378,17 +377,26 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     bool first = true;
     const Context<DB> c = {p, q, row, rd, lane};
     int slot = 0, t = next(t1 - 1 - wave);
-    bool whole_t = same(t);
-    if (t >= t0) issue(t, slot);
+    bool whole_t = same(t), whole_u = false;
+    int u = t - NW;  // the tile after t
+    if (t >= t0) {
+        issue_k(t, 0);
+        issue_v(t, 0);
+        u = next(u);
+        whole_u = same(u);
+        if (u >= t0) {
+            issue_k(u, 1);
+            issue_v(u, 1);
+        }
+    }
     while (t >= t0) {
-        landed();
-        if (p.kv_doc && lane < FEW_KEYS) docs[wave][slot][lane] = dr;
-        const int tn = next(t - NW);
-        const bool whole_n = same(tn);
-        // (the other slot has been read: the products of the tile before have
-        // waited for that, or this does)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (tn >= t0) issue(tn, slot ^ 1);
+        // t's loads, not u's, which were issued after them
+        if (u >= t0 && p.kv_doc)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * Load::PIECES + 1) : "memory");
+        else if (u >= t0)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * Load::PIECES) : "memory");
+        else
+            landed();
         const int j0 = t * FEW_KEYS;
         char *kt = lds + slot * SLOT, *vt = kt + HALF;
         const bool partial = j0 + FEW_KEYS > lim_lo || !whole_t;
@@ -400,9 +408,18 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
                 for (int o = 0; o < HALF; o += 1024) make_finite16(vt + o + 16 * lane);
             }
         }
-        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first);
+        const int un = u >= t0 ? next(u - NW) : u;
+        const bool whole_n = same(un);
+        const bool more = u >= t0 && un >= t0;
+        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first, [&]() {
+            if (more) issue_k(un, slot);
+        });
         first = false;
-        t = tn, whole_t = whole_n;
+        // (the values have been read)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) issue_v(un, slot);
+        t = u, whole_t = whole_u;
+        u = un, whole_u = whole_n;
         slot ^= 1;
     }
 
