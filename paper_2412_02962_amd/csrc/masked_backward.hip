@@ -88,6 +88,8 @@ __device__ __forceinline__ void store_sums(bf16* row, float* part, const f32x16 
         }
 }
 
+constexpr float NEAR = 8.f;  // (in log2 units: a bias of a factor of 256)
+
 template <int DB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     using T = Tile<DB>;
@@ -190,9 +192,23 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             off += w[r];
-            o[r >> 3][r & 7] = f32_to_bf16(CAP ? w[r] * dp[r] : w[r]);
+            if constexpr (CAP) w[r] *= dp[r];
+            o[r >> 3][r & 7] = f32_to_bf16(w[r]);
         }
         add_rows<DB>(acc, o, rd, kt, row0);
+        if constexpr (BIAS) {
+            // A bias rests a query on the few keys near it, and there y's own
+            // rounding (in delta) is seen in dq.  The weights' is taken out for
+            // them, so that the two do not add up.
+            const int apart = max(j0 - pos, pos - j0 - 31);
+            const bool near = slope2 > 0.f && slope2 * (float)apart < NEAR;
+            if (__any(near)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w[r] = near ? w[r] - bf16_to_f32(o[r >> 3][r & 7]) : 0.f;
+                pack(w, o);
+                add_rows<DB>(acc, o, rd, kt, row0);
+            }
+        }
     };
 
     clear<DB>(acc);
