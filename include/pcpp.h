@@ -997,8 +997,10 @@ int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, const void* x,
  */
 typedef struct {
     int32_t batch;         /* sequences B, 1 .. 65535                        */
-    int32_t n_q, n_kv;     /* tokens, 1 .. 2^24                              */
-    int32_t heads;         /* of the queries, 1 .. 1024                      */
+    int32_t n_q, n_kv;     /* tokens, 1 .. 2^24; n = the larger              */
+    int32_t heads;         /* of the queries, 1 .. 1024; B heads n <= 2^29,
+                            * B heads ceil(n / 128) <= 2^22, and for gradients
+                            * B heads n_q <= 2^27                            */
     int32_t kv_heads;      /* of the keys and values, dividing heads         */
     int32_t head_dim;      /* D, a multiple of 8, 8 .. 128                   */
     int32_t causal;        /* 0 or 1                                         */
@@ -1016,7 +1018,7 @@ typedef struct {
 /* Device arrays, 4-byte aligned, read by the kernels; each may be NULL. */
 typedef struct {
     const int32_t* kv_len; /* [B], taken into 0 .. n_kv; NULL: n_kv          */
-    const int32_t* q_pos;  /* [B], any values; NULL: n_kv - n_q              */
+    const int32_t* q_pos;  /* [B], taken into -2^30 .. 2^30; NULL: n_kv - n_q */
     const int32_t* prefix; /* [B]; needs causal; NULL: 0                     */
     const int32_t* q_doc;  /* [B, n_q] document of each query, < 0: none     */
     const int32_t* kv_doc; /* [B, n_kv]; both or neither                     */

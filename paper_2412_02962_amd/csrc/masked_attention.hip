@@ -22,6 +22,8 @@ namespace {
 constexpr int kMaxTokens = 1 << 24;
 constexpr int64_t kMaxBatch = (int64_t)1 << 40;  // elements
 constexpr int64_t kMaxRow = 1 << 24;             // 64 rows are less than 2^32 bytes
+constexpr int64_t kMaxHeadTokens = 1 << 29, kMaxHeadBlocks = 1 << 22;
+constexpr int64_t kMaxGradTokens = 1 << 27;      // masked_delta: 16 threads to a query of a head
 
 // A tensor's rows in elements: [batch, tokens, width] at `row` and `batch`.
 struct Layout {
@@ -54,8 +56,9 @@ int check_geom(const pcpp_masked_geom_t* g, Shape* s) {
     if (!isfinite(g->scale) || !isfinite(g->cap) || g->cap < 0.f) return PCPP_EINVAL;
     if (g->cap > 0.f && !isfinite(g->scale / g->cap * 2.f * LOG2E)) return PCPP_EINVAL;
     if (g->head_dim < 8 || g->head_dim % 8 != 0 || g->head_dim > 128) return PCPP_ENOTSUP;
-    // a launch has fewer than 2^31 workgroups and 2^32 threads
-    if ((int64_t)g->batch * g->heads * (g->n_q > g->n_kv ? g->n_q : g->n_kv) > ((int64_t)1 << 30)) return PCPP_EINVAL;
+    // A launch has fewer than 2^32 threads: 256 for 128 tokens of a sequence's head.
+    const int64_t heads = (int64_t)g->batch * g->heads, most = g->n_q > g->n_kv ? g->n_q : g->n_kv;
+    if (heads * most > kMaxHeadTokens || heads * ((most + 127) / 128) > kMaxHeadBlocks) return PCPP_EINVAL;
     const int qw = g->heads * g->head_dim, kw = g->kv_heads * g->head_dim;
     if (!layout_of(g->q_row, g->q_batch, g->batch, g->n_q, qw, &s->q) ||
         !layout_of(g->k_row, g->k_batch, g->batch, g->n_kv, kw, &s->k) ||
@@ -193,9 +196,14 @@ PCPP_EXPORT int pcpp_masked_attention(const pcpp_masked_geom_t* g, const pcpp_ma
     return launch_masked_few(p, s) == hipSuccess ? PCPP_OK : PCPP_EHIP;
 }
 
+static int check_backward(const pcpp_masked_geom_t* g, Shape* s) {
+    const int st = check_geom(g, s);
+    return st == PCPP_OK && (int64_t)g->batch * g->heads * g->n_q > kMaxGradTokens ? PCPP_EINVAL : st;
+}
+
 PCPP_EXPORT size_t pcpp_masked_attention_backward_workspace_size(const pcpp_masked_geom_t* g) {
     Shape s;
-    return check_geom(g, &s) == PCPP_OK ? (size_t)backward_bytes(g) : 0;
+    return check_backward(g, &s) == PCPP_OK ? (size_t)backward_bytes(g) : 0;
 }
 
 PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, const pcpp_mask_t* m, const void* q,
@@ -203,7 +211,7 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
                                                const void* dy, void* dq, void* dk, void* dv, void* workspace,
                                                size_t ws_bytes, void* stream) {
     Shape sh;
-    int st = check_geom(g, &sh);
+    int st = check_backward(g, &sh);
     if (st == PCPP_OK) st = check_mask(g, m);
     if (st != PCPP_OK) return st;
     const void* needed[] = {q, k, v, y, lse, dy};
@@ -226,7 +234,7 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
     const Range out[] = {{dq, qb}, {dk, kb}, {dv, vb}};
     for (const Range& o : out)
         if (outputs_overlap(&o, 1, in, n_in)) return PCPP_EINVAL;
-    if (outputs_overlap(&in[6], 1, in, 6)) return PCPP_EINVAL;
+    if (outputs_overlap(&in[6], 1, in, 6) || outputs_overlap(&in[6], 1, in + 7, n_in - 7)) return PCPP_EINVAL;
     Params p = params_of(g, m, sh, workspace);
     p.q = (const bf16*)q, p.k = (const bf16*)k, p.v = (const bf16*)v, p.y = (bf16*)y, p.dy = (const bf16*)dy;
     p.lse = (float*)lse;

@@ -1,0 +1,94 @@
+"""GroupNorm with its activation over many tokens, and as a program calls it."""
+
+import pytest
+import torch
+
+from tests import norm_act_reference as ref
+from tests.test_gpu_norm_act import BF16, DEV, DRAW, F32, F64, FIRST, SEED, _call, _inputs, _near
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+@pytest.mark.parametrize("shape", [(2, 70001, 64, 16), (1, 140000, 32, 32), (600, 5, 48, 3)], ids=str)
+def test_many_records(shape, dtype):
+    """Chunks of whole rows, their records merged in a launch of their own; and
+    more images than workgroups."""
+    B, N, C, G = shape
+    x, gamma, beta, dy = _inputs(B, N, C, dtype, seed=31)
+    y, stats, dx, dgamma, dbeta = _call(x, gamma, beta, G, 1e-5, "silu", 0.1, dy)
+    d = [t.to(F64) for t in (x, gamma, beta, dy)]
+    r = ref.forward(*d[:3], G, 1e-5, "silu", 0.1, SEED, FIRST + DRAW, dtype)
+    _near(stats[..., 0], r["mean"], r["mean_bound"] + 1e-30, "mean")
+    _near(stats[..., 1], r["rstd"], r["rstd_bound"], "rstd")
+    _near(y, r["y"], r["bound"], "y")
+    want, bounds = ref.backward(r, d[1], d[3], "silu", 0.1, SEED, FIRST + DRAW, dtype)
+    for got, w, b, tag in zip((dx, dgamma, dbeta), want, bounds, ("dx", "dgamma", "dbeta")):
+        _near(got, w, b, tag)
+
+
+def test_beyond_2_to_32_bytes():
+    """The second of two images lies 4.3 GB behind the first: as by itself."""
+    from paper_2412_02962_amd import pcpp
+    B, N, C, G = 2, 1 << 21, 1032, 8
+    gen = torch.Generator(DEV).manual_seed(32)
+    x = torch.empty(B, N, C, dtype=BF16, device=DEV).normal_(generator=gen)
+    dy = torch.empty(B, N, C, dtype=BF16, device=DEV).normal_(generator=gen)
+    gamma, beta = (torch.empty(C, dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
+
+    def run(x, dy):
+        b = x.shape[0]
+        g = pcpp.make_norm_act_geom(b, N, C, G)
+        n = pcpp.pcpp_group_norm_act_workspace_size(g)
+        ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+        y, dx, stats = torch.empty_like(x), torch.empty_like(x), torch.empty(b, G, 2, device=DEV)
+        pcpp.pcpp_group_norm_act(g, x, gamma, beta, None, 0, y, stats, ws, n)
+        pcpp.pcpp_group_norm_act_backward(g, x, gamma, beta, stats, None, 0, dy, dx, None, None, ws, n)
+        return y, dx, stats
+    both, alone = run(x, dy), run(x[1:], dy[1:])
+    # The statistics are merged in other runs: float32 sums of 2^31 / 8 terms, in
+    # 14 merges and runs of 8 at most; y and dx may round to the next bf16.
+    torch.testing.assert_close(both[2][1:], alone[2], rtol=2.0 ** -18, atol=2.0 ** -18)
+    for a, b in zip(both[:2], alone[:2]):
+        a, b = a[1, -4096:].float(), b[0, -4096:].float()
+        assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -14).all()
+
+
+def test_captured_and_replayed():
+    """A training step's calls: the state moves on inside the graph."""
+    from paper_2412_02962_amd import pcpp
+    B, N, C, G = 2, 9000, 64, 16
+    gen = torch.Generator(DEV).manual_seed(33)
+    x, dy = (torch.empty(B, N, C, dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
+    gamma, beta = (torch.empty(C, dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
+    state = torch.tensor([SEED, 0], dtype=torch.int64, device=DEV)
+    g = pcpp.make_norm_act_geom(B, N, C, G, drop=0.2)
+    n = pcpp.pcpp_group_norm_act_workspace_size(g)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    make = lambda: [torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta),
+                    torch.empty(B, G, 2, device=DEV)]
+
+    def run(o):
+        y, dx, dgamma, dbeta, stats = o
+        pcpp.pcpp_group_norm_act(g, x, gamma, beta, state, 0, y, stats, ws, n)
+        pcpp.pcpp_group_norm_act_backward(g, x, gamma, beta, stats, state, 0, dy, dx, dgamma, dbeta, ws, n)
+        state[1:].add_(1)
+    out = make()
+    run(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(out)
+    seen = []
+    for step in range(4):
+        x.normal_(generator=gen)
+        eager = make()
+        run(eager)
+        state[1:].sub_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(state[1]) == step + 2
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b), step
+        seen.append(out[0] == 0)
+    assert not torch.equal(seen[0], seen[1])
