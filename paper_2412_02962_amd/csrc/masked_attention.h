@@ -251,13 +251,13 @@ __device__ __forceinline__ void clear_tiles(char* lds, int bytes, int threads) {
 // direction; `mine` is the wavefront's part of `all`.
 struct DocWindow {
     const DocRange* ranges;
+    DocRange* kept;  // the wavefront's 64 of them, in LDS
     int end, base;
-    DocRange all, mine, r;
+    DocRange all, mine;
     uint64_t meets;
     bool on;
-    __device__ __forceinline__ void init(const DocRange* ranges_, int end_, const DocRange& all_, const DocRange& mine_, bool on_) {
-        ranges = ranges_, end = end_, base = -(1 << 30), all = all_, mine = mine_, on = on_;
-        r = DocRange{0x7fffffff, -1};
+    __device__ __forceinline__ void init(const DocRange* ranges_, DocRange* kept_, int end_, const DocRange& all_, const DocRange& mine_, bool on_) {
+        ranges = ranges_, kept = kept_, end = end_, base = -(1 << 30), all = all_, mine = mine_, on = on_;
         meets = 0;
     }
     // The first tile from t on (end: none).
@@ -285,13 +285,15 @@ struct DocWindow {
     __device__ __forceinline__ void load(int from) {
         base = from;
         const int u = from + (int)(threadIdx.x & 63);
-        r = u >= 0 && u < end ? ranges[u] : DocRange{0x7fffffff, -1};
+        const DocRange r = u >= 0 && u < end ? ranges[u] : DocRange{0x7fffffff, -1};
+        kept[threadIdx.x & 63] = r;
         meets = __ballot(ranges_meet(r, all));
     }
     // Of a tile that next() has just returned: all of it and of the workgroup,
     // or of the wavefront, one document; none of the wavefront's in it.
     __device__ __forceinline__ DocRange range(int t) const {
-        return DocRange{__builtin_amdgcn_readlane(r.lo, t - base), __builtin_amdgcn_readlane(r.hi, t - base)};
+        const DocRange r = kept[t - base];
+        return DocRange{__builtin_amdgcn_readfirstlane(r.lo), __builtin_amdgcn_readfirstlane(r.hi)};
     }
     __device__ __forceinline__ bool same_all(int t) const { return !on || same_document(range(t), all); }
     __device__ __forceinline__ bool same(int t) const { return !on || same_document(range(t), mine); }

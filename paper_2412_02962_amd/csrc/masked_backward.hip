@@ -96,6 +96,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     constexpr int SLOT = 2 * T::BYTES;  // K, V
     __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
     __shared__ __attribute__((aligned(16))) int docs[2][TILE];
+    __shared__ DocRange kept[NW][64];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + BLOCK - 1) / BLOCK;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
             all = r[0];
             if (last / TILE > i0 / TILE) all = joined(all, r[1]);
         }
-        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
+        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), kept[wave], end, all, mine, p.kv_doc != nullptr);
     }
     const Loader<DB, NW, TILE> kload(p.k_row, p.D, wave, lane), vload(p.v_row, p.D, wave, lane);
     const Reader<DB> reader(lane);
@@ -279,6 +280,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ __attribute__((aligned(16))) QueryTile<ROWS> brought[2];
     __shared__ Spoilt spoilt[NT];
+    __shared__ DocRange kept[NW][64];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nkb = (p.nkv + BLOCK - 1) / BLOCK;
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
             all = r[0];
             if (klast / TILE > k0 / TILE) all = joined(all, r[1]);
         }
-        window.init(p.q_range + (int64_t)b * tiles_of(p.nq), tiles_of(p.nq), all, mine, p.kv_doc != nullptr);
+        window.init(p.q_range + (int64_t)b * tiles_of(p.nq), kept[wave], tiles_of(p.nq), all, mine, p.kv_doc != nullptr);
     }
     // The first tile from t on that may have the block's documents.
     auto next = [&](int t) {

@@ -59,7 +59,7 @@ struct Context {
 // not see some key.  TWO: the probabilities as two bf16 (for few queries, where
 // the products cost nothing and a token's error counts).
 // after_scores: what may run once the keys have been used.
-template <int DB, bool CAP, bool BIAS, bool TWO, typename After>
+template <int DB, int HB, bool CAP, bool BIAS, bool TWO, typename After>
 __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs,
                                      int row0, int j0, bool partial, bool first, After after_scores) {
     const Params& p = c.p;
@@ -73,43 +73,56 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
     // scores are computed again: registers for them would be held all along).
     // The first step of all begins with the maximum.
     bool search = first, tried = false;
-    float w[16];
-    bf16x8 pr[2];
+    float w[HB][16];
+    bf16x8 pr[HB][2];
     float sum;
     uint32_t over = search ? ~0u : 0u;  // the lanes that need another maximum
 #pragma unroll 1
     for (;;) {
-        f32x16 s;
+        f32x16 s[HB];
 #pragma unroll
-        for (int kk = 0; kk < 2 * DB; ++kk) s = mfma32x32x16(rd.rows(kt, row0, kk), c.q[kk], kk == 0 ? f32x16{} : s);
+        for (int h = 0; h < HB; ++h) {
+#pragma unroll
+            for (int kk = 0; kk < 2 * DB; ++kk) s[h] = mfma32x32x16(rd.rows(kt, row0 + 32 * h, kk), c.q[kk], kk == 0 ? f32x16{} : s[h]);
+            if constexpr (HB > 1) __builtin_amdgcn_sched_barrier(0);
+        }
         // Scores less the maximum, in log2 units; -infinity where not seen (also
         // while the maximum is still -infinity and all others are infinite).
         const float add = search ? 0.f : -st.m;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            w[r] = score<CAP>(p, s[r], add);
-            if constexpr (BIAS) w[r] = __builtin_fmaf(-row.slope2, fabsf(far - (float)(8 * (r >> 2) + (r & 3))), w[r]);
-        }
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                w[h][r] = score<CAP>(p, s[h][r], add);
+                if constexpr (BIAS) w[h][r] = __builtin_fmaf(-row.slope2, fabsf(far - (float)(32 * h + 8 * (r >> 2) + (r & 3))), w[h][r]);
+            }
         if (partial) {
             int limit = row.limit - base;
             asm volatile("" : "+v"(limit));  // (a branch, not selections in every step)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = 8 * (r >> 2) + (r & 3) < limit ? w[r] : -INFINITY;
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w[h][r] = 32 * h + 8 * (r >> 2) + (r & 3) < limit ? w[h][r] : -INFINITY;
             if (p.kv_doc) {
                 int at = row0 + 4 * half;
                 asm volatile("" : "+v"(at));
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
+                for (int g = 0; g < 4 * HB; ++g) {
                     const i32x4 d = *(const i32x4*)(docs + at + 8 * g);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[4 * g + e] = (TWO ? max(d[e], -1) : d[e]) == row.doc ? w[4 * g + e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        float& x = w[g >> 2][4 * (g & 3) + e];
+                        x = max(d[e], -1) == row.doc ? x : -INFINITY;
+                    }
                 }
             }
         }
         if (search) {
-            float mx = w[0];
+            float mx = w[0][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, w[r]);
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, w[h][r]);
             // (each query by its own sums: what others see is nothing to it)
             const float m_new = over ? fmaxf(st.m, max_halves(mx)) : st.m;
             const float alpha = m_new == st.m ? 1.f : fast_exp2(st.m - m_new);
@@ -126,29 +139,36 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
         }
         sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            w[r] = fast_exp2(w[r]);
-            w[r + 1] = fast_exp2(w[r + 1]);
-            const bf16x2 pk = {f32_to_bf16(w[r]), f32_to_bf16(w[r + 1])};
-            pr[r >> 3][r & 7] = pk[0];
-            pr[r >> 3][(r & 7) + 1] = pk[1];
-            if constexpr (TWO)
-                sum += w[r] + w[r + 1];
-            else
-                sum = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, sum, false);
-        }
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                float &a = w[h][r], &b = w[h][r + 1];
+                a = fast_exp2(a);
+                b = fast_exp2(b);
+                const bf16x2 pk = {f32_to_bf16(a), f32_to_bf16(b)};
+                pr[h][r >> 3][r & 7] = pk[0];
+                pr[h][r >> 3][(r & 7) + 1] = pk[1];
+                if constexpr (TWO)
+                    sum += a + b;
+                else
+                    sum = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, sum, false);
+            }
         if (tried || !__any(!(sum < P_LIMIT))) break;
         over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
         search = true;
     }
     after_scores();
     st.l += sum;
-    add_rows<DB>(st.o, pr, rd, vt, row0);
-    if constexpr (TWO) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] -= bf16_to_f32(pr[r >> 3][r & 7]);
-        pack(w, pr);
-        add_rows<DB>(st.o, pr, rd, vt, row0);
+    for (int h = 0; h < HB; ++h) {
+        add_rows<DB>(st.o, pr[h], rd, vt, row0 + 32 * h);
+    }
+    if constexpr (TWO) {
+        static_assert(HB == 1, "few queries");
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[0][r] -= bf16_to_f32(pr[0][r >> 3][r & 7]);
+        pack(w[0], pr[0]);
+        add_rows<DB>(st.o, pr[0], rd, vt, row0);
     }
 }
 
@@ -171,11 +191,13 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
 
 template <int DB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) {
+    constexpr int HB = DB <= 2 ? 2 : 1;
     using T = Tile<DB>;
     constexpr int SLOT = 2 * T::BYTES;  // K, V
     __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
     __shared__ __attribute__((aligned(16))) int docs[2][TILE];
     __shared__ Spoilt spoilt[NT];
+    __shared__ DocRange kept[NW][64];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + QB - 1) / QB;
@@ -204,7 +226,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
             all = r[0];
             if (last / TILE > i0 / TILE) all = joined(all, r[1]);
         }
-        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), end, all, mine, p.kv_doc != nullptr);
+        window.init(p.kv_range + (int64_t)b * tiles_of(p.nkv), kept[wave], end, all, mine, p.kv_doc != nullptr);
     }
 
     const Loader<DB, NW, TILE> kload(p.k_row, p.D, wave, lane), vload(p.v_row, p.D, wave, lane);
@@ -212,11 +234,12 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     const bf16* kb = p.k + b * p.k_batch + kh * p.D;
     const bf16* vb = p.v + b * p.v_batch + kh * p.D;
     const uint32_t lds0 = lds_address(lds);
-    int dr = -1;
+    const uint32_t docs0 = lds_address(docs);
     auto issue = [&](int t, int slot) {
         kload.issue(kb, t * TILE, sq.len, lds0 + slot * SLOT);
         vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
-        if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid], -1) : -1;
+        if (p.kv_doc && tid < TILE)
+            load_lds4(uniform64((uint64_t)(uintptr_t)(p.kv_doc + (int64_t)b * p.nkv + t * TILE)), 4 * min(tid, sq.len - 1 - t * TILE), docs0 + slot * TILE * 4);
     };
     if (p.D < 32 * DB) {
         clear_tiles(lds, 2 * SLOT, NT);
@@ -239,7 +262,6 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     }
     while (more) {
         landed();
-        if (p.kv_doc && tid < TILE) docs[slot][tid] = dr;
         __syncthreads();  // the tile is there, and nobody reads the one before any more
         int tn = t;
         bool same_n = true, apart_n = false, same_all_n = true;
@@ -262,10 +284,10 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
             }
         }
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2; h += HB) {
             const int j0 = t * TILE + 32 * h;
             if (j0 >= lim_hi || apart) continue;
-            step<DB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same, first, []() {});
+            step<DB, HB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 * HB > lim_lo || !same, first, []() {});
             first = false;
         }
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
@@ -411,7 +433,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
         const int un = u >= t0 ? next(u - NW) : u;
         const bool whole_n = same(un);
         const bool more = u >= t0 && un >= t0;
-        step<DB, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first, [&]() {
+        step<DB, 1, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first, [&]() {
             if (more) issue_k(un, slot);
         });
         first = false;
