@@ -55,13 +55,13 @@ struct Context {
     int lane;
 };
 
-// 32 keys from key j0, rows row0 of the tiles in LDS.  partial: some query does
+// 32 HB keys from key j0, the tiles' first rows.  partial: some query does
 // not see some key.  TWO: the probabilities as two bf16 (for few queries, where
 // the products cost nothing and a token's error counts).
 // after_scores: what may run once the keys have been used.
 template <int DB, int HB, bool CAP, bool BIAS, bool TWO, typename After>
-__device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs,
-                                     int row0, int j0, bool partial, bool first, After after_scores) {
+__device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs, int j0,
+                                     bool partial, bool first, After after_scores) {
     const Params& p = c.p;
     const Row& row = c.row;
     const Reader<DB> rd = c.rd.fresh();
@@ -83,7 +83,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
 #pragma unroll
         for (int h = 0; h < HB; ++h) {
 #pragma unroll
-            for (int kk = 0; kk < 2 * DB; ++kk) s[h] = mfma32x32x16(rd.rows(kt, row0 + 32 * h, kk), c.q[kk], kk == 0 ? f32x16{} : s[h]);
+            for (int kk = 0; kk < 2 * DB; ++kk) s[h] = mfma32x32x16(rd.rows(kt, 32 * h, kk), c.q[kk], kk == 0 ? f32x16{} : s[h]);
             if constexpr (HB > 1) __builtin_amdgcn_sched_barrier(0);
         }
         // Scores less the maximum, in log2 units; -infinity where not seen (also
@@ -104,7 +104,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) w[h][r] = 32 * h + 8 * (r >> 2) + (r & 3) < limit ? w[h][r] : -INFINITY;
             if (p.kv_doc) {
-                int at = row0 + 4 * half;
+                int at = 4 * half;
                 asm volatile("" : "+v"(at));
 #pragma unroll
                 for (int g = 0; g < 4 * HB; ++g) {
@@ -161,14 +161,14 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
     st.l += sum;
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
-        add_rows<DB>(st.o, pr[h], rd, vt, row0 + 32 * h);
+        add_rows<DB>(st.o, pr[h], rd, vt, 32 * h);
     }
     if constexpr (TWO) {
         static_assert(HB == 1, "few queries");
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[0][r] -= bf16_to_f32(pr[0][r >> 3][r & 7]);
         pack(w[0], pr[0]);
-        add_rows<DB>(st.o, pr[0], rd, vt, row0);
+        add_rows<DB>(st.o, pr[0], rd, vt, 0);
     }
 }
 
@@ -191,7 +191,6 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
 
 template <int DB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) {
-    constexpr int HB = DB <= 2 ? 2 : 1;
     using T = Tile<DB>;
     constexpr int SLOT = 2 * T::BYTES;  // K, V
     __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
@@ -283,11 +282,9 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
                 __syncthreads();
             }
         }
-#pragma unroll 1
-        for (int h = 0; h < 2; h += HB) {
-            const int j0 = t * TILE + 32 * h;
-            if (j0 >= lim_hi || apart) continue;
-            step<DB, HB, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], 32 * h, j0, j0 + 32 * HB > lim_lo || !same, first, []() {});
+        const int j0 = t * TILE;
+        if (j0 < lim_hi && !apart) {
+            step<DB, 2, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], j0, j0 + TILE > lim_lo || !same, first, []() {});
             first = false;
         }
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
@@ -433,7 +430,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
         const int un = u >= t0 ? next(u - NW) : u;
         const bool whole_n = same(un);
         const bool more = u >= t0 && un >= t0;
-        step<DB, 1, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], 0, j0, partial, first, [&]() {
+        step<DB, 1, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], j0, partial, first, [&]() {
             if (more) issue_k(un, slot);
         });
         first = false;
