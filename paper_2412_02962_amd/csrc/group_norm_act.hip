@@ -34,6 +34,11 @@ constexpr int kMaxThreads = 512;
 constexpr int kMaxGroups = 256;
 constexpr int kRunRows = 8;      // rows that a thread of the statistics takes at a time
 constexpr int kBlocks = 512;     // workgroups of a launch that sums: two to a compute unit
+// A slab of an image in a workgroup's registers: the rows that a thread holds,
+// and, where the slab has several groups, half as many (see whole_of).
+constexpr int kWholeRows = 8, kGradRows = 6;
+constexpr int kWholeBlocks = 256;
+constexpr int kWholeVectors = 4; // of such a slab's rows, at least
 constexpr int kFewChunks = 32;   // chunks whose records every consumer merges; more are merged in a launch of their own
 
 // How a launch cuts [B, N, C]: slabs of S channels (whole groups), chunks of
@@ -581,6 +586,250 @@ __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_apply(NormActParams
     }
 }
 
+// ---- few tokens: a slab of an image in one workgroup's registers, one launch ----
+
+// The sum of v over the wavefronts of the thread's group: as many to each
+// of the slab's gs groups (1, 2, 4 or 8 of them).
+__device__ __forceinline__ float group_total(const Cut& a, float v, float* lds) {
+    const int waves = a.threads / 64 / a.gs, wave = threadIdx.x >> 6;
+    v = lanes_sum(v, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
+    __syncthreads();
+    float t = 0.f;
+    for (int w = 0; w < waves; ++w) t += lds[wave / waves * waves + w];
+    return t;
+}
+// Per-channel values of all threads, in part [RP][S], summed over the rows and
+// channels of the thread's group of wavefronts.
+__device__ __forceinline__ float group_share(const Cut& a, const float (&v)[8], const Place& at, float* part) {
+    if (a.gs == 1) {
+        float t = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t += v[e];
+        return t;  // (0 of the threads left over)
+    }
+    __syncthreads();
+    if (at.in) store8(part + at.r * a.S + 8 * at.v, v);
+    __syncthreads();
+    const int lanes = a.threads / a.gs, g = threadIdx.x / lanes;
+    const float inv_cg = 1.f / (float)a.cg;
+    float t = 0.f;
+    for (int i = threadIdx.x % lanes; i < a.RP * a.cg; i += lanes) {
+        const int r = group_of(i, inv_cg);
+        t += part[r * a.S + g * a.cg + i - r * a.cg];
+    }
+    return t;
+}
+
+// Mean by the sum, then the deviations from it: their squares, and their sum for
+// what the mean is off by.
+template <typename T, int ACT>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_whole(NormActParams p) {
+    __shared__ __attribute__((aligned(16))) float part[kMaxThreads * 8];
+    __shared__ float lds[kMaxThreads / 64], g_mean[8], g_rstd[8];
+    const Cut a = p.cut;
+    const int slab = blockIdx.x, b = blockIdx.y;
+    const Place at = place_of(a, slab);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    Raw<T> x[kWholeRows];
+    float s[8], q[8], mean[8], rstd[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = q[e] = 0.f;
+    if (at.in) {
+#pragma unroll
+        for (int i = 0; i < kWholeRows; ++i)
+            if (at.r + i * a.RP < a.N) x[i].load((const T*)p.x + base + (int64_t)(at.r + i * a.RP) * a.C);
+#pragma unroll
+        for (int i = 0; i < kWholeRows; ++i)
+            if (at.r + i * a.RP < a.N) {
+                float v[8];
+                x[i].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += v[e];
+            }
+    }
+    const float count = (float)a.N * (float)a.cg, inv_cg = 1.f / (float)a.cg;
+    const int lanes = kMaxThreads / a.gs, g = threadIdx.x / lanes;
+    const bool first = threadIdx.x % lanes == 0;
+    const float m = group_total(a, group_share(a, s, at, part), lds) / count;
+    if (first) g_mean[g] = m;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        mean[e] = at.in ? g_mean[group_of(8 * at.v + e, inv_cg)] : 0.f;
+        s[e] = 0.f;
+    }
+    if (at.in) {
+#pragma unroll
+        for (int i = 0; i < kWholeRows; ++i)
+            if (at.r + i * a.RP < a.N) {
+                float v[8];
+                x[i].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float d = v[e] - mean[e];
+                    s[e] += d;
+                    q[e] = __builtin_fmaf(d, d, q[e]);
+                }
+            }
+    }
+    const float off = group_total(a, group_share(a, s, at, part), lds) / count;
+    const float var = group_total(a, group_share(a, q, at, part), lds) / count - off * off;
+    if (first) {
+        g_mean[g] = m + off;
+        g_rstd[g] = 1.f / sqrtf(fmaxf(var, 0.f) + p.eps);
+        if (p.stats != nullptr) {
+            float* o = p.stats + ((int64_t)b * a.G + slab * a.gs + g) * 2;
+            o[0] = g_mean[g];
+            o[1] = g_rstd[g];
+        }
+    }
+    __syncthreads();
+    if (!at.in) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        mean[e] = g_mean[group_of(8 * at.v + e, inv_cg)];
+        rstd[e] = g_rstd[group_of(8 * at.v + e, inv_cg)];
+    }
+    const bf16x8 gamma = *(const bf16x8*)(p.gamma + at.c0), beta = *(const bf16x8*)(p.beta + at.c0);
+    const DropoutKey key = dropout_key(p.drop);
+#pragma unroll
+    for (int i = 0; i < kWholeRows; ++i) {
+        if (at.r + i * a.RP >= a.N) break;
+        const int64_t o = base + (int64_t)(at.r + i * a.RP) * a.C;
+        float v[8];
+        x[i].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = act_of<ACT>(__builtin_fmaf((v[e] - mean[e]) * rstd[e], bf16_to_f32(gamma[e]), bf16_to_f32(beta[e])), nullptr);
+        if (p.drop.least > 0) drop8(p.drop, key, (uint64_t)o / 8, v);
+        store8((T*)p.y + o, v);
+    }
+}
+
+// The sums of w and w n, and the images' sums of the columns (of the only image:
+// dgamma and dbeta themselves).
+template <typename T, int ACT>
+__global__ __launch_bounds__(kMaxThreads) void norm_act_grad_whole(NormActParams p) {
+    __shared__ __attribute__((aligned(16))) float part[2][kMaxThreads * 8];
+    __shared__ float lds[kMaxThreads / 64], g_m0[8], g_m1[8];
+    const Cut a = p.cut;
+    const int slab = blockIdx.x, b = blockIdx.y;
+    const Place at = place_of(a, slab);
+    const int64_t base = (int64_t)b * a.N * a.C + at.c0;
+    Raw<T> x[kGradRows];
+    float gr[kGradRows][8];  // dy, then g but for dropout's factor
+    const DropoutKey key = dropout_key(p.drop);
+    const float factor = p.drop.least > 0 ? p.drop.factor : 1.f;
+    const float inv_cg = 1.f / (float)a.cg;
+    if (at.in) {
+#pragma unroll
+        for (int i = 0; i < kGradRows; ++i)
+            if (at.r + i * a.RP < a.N) {
+                x[i].load((const T*)p.x + base + (int64_t)(at.r + i * a.RP) * a.C);
+                load8((const T*)p.dy + base + (int64_t)(at.r + i * a.RP) * a.C, gr[i]);
+            }
+    }
+    const Place safe = at.in ? at : Place{0, 0, slab * a.S, false};
+    const Channels ch(p, safe, slab, b);
+    float sn[8], sg[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sn[e] = sg[e] = 0.f;
+    if (at.in) {
+#pragma unroll
+        for (int i = 0; i < kGradRows; ++i)
+            if (at.r + i * a.RP < a.N) {
+                float v[8];
+                x[i].get(v);
+                grad8<ACT>(p, key, base + (int64_t)(at.r + i * a.RP) * a.C, ch, v, gr[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sn[e] = __builtin_fmaf(gr[i][e], v[e], sn[e]);
+                    sg[e] += gr[i][e];
+                }
+            }
+    }
+    if (p.dgamma != nullptr || p.dbeta != nullptr) {
+        if (at.in) {
+            store8(part[0] + at.r * a.S + 8 * at.v, sn);
+            store8(part[1] + at.r * a.S + 8 * at.v, sg);
+        }
+        __syncthreads();
+        // every channel by several threads, then their sums
+        const int k = group_of(threadIdx.x, 1.f / (float)a.S), c = threadIdx.x - k * a.S, rows = kMaxThreads / a.S;
+        float tn = 0.f, tg = 0.f;
+        if (k < rows)
+            for (int r = k; r < a.RP; r += rows) {
+                tn += part[0][r * a.S + c];
+                tg += part[1][r * a.S + c];
+            }
+        __syncthreads();
+        if (k < rows) {
+            part[0][threadIdx.x] = tn;
+            part[1][threadIdx.x] = tg;
+        }
+        __syncthreads();
+        if (threadIdx.x < a.S) {
+            for (int r = 1; r < rows; ++r) {
+                tn += part[0][r * a.S + c];
+                tg += part[1][r * a.S + c];
+            }
+            tn *= factor;
+            tg *= factor;
+            const int channel = slab * a.S + c;
+            if (p.columns != nullptr) {
+                p.columns[(int64_t)b * a.C + channel] = tn;
+                p.columns[((int64_t)a.B + b) * a.C + channel] = tg;
+            } else {
+                if (p.dgamma != nullptr) p.dgamma[channel] = f32_to_bf16(tn);
+                if (p.dbeta != nullptr) p.dbeta[channel] = f32_to_bf16(tg);
+            }
+        }
+    }
+    float gamma[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        gamma[e] = bf16_to_f32(ch.gamma[e]) * factor;
+        sn[e] *= gamma[e];
+        sg[e] *= gamma[e];
+    }
+    const float count = (float)a.N * (float)a.cg;
+    const float t0 = group_total(a, group_share(a, sg, at, part[0]), lds) / count;
+    const float t1 = group_total(a, group_share(a, sn, at, part[0]), lds) / count;
+    const int lanes = kMaxThreads / a.gs;
+    if (threadIdx.x % lanes == 0) {
+        g_m0[threadIdx.x / lanes] = t0;
+        g_m1[threadIdx.x / lanes] = t1;
+    }
+    __syncthreads();
+    if (!at.in) return;
+    float m0[8], m1[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        m0[e] = g_m0[group_of(8 * at.v + e, inv_cg)];
+        m1[e] = g_m1[group_of(8 * at.v + e, inv_cg)];
+    }
+#pragma unroll
+    for (int i = 0; i < kGradRows; ++i) {
+        if (at.r + i * a.RP >= a.N) break;
+        const int64_t o = base + (int64_t)(at.r + i * a.RP) * a.C;
+        float v[8];
+        x[i].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float n = (v[e] - ch.mean[e]) * ch.rstd[e];
+            v[e] = ch.rstd[e] * (__builtin_fmaf(gr[i][e], gamma[e], -m0[e]) - n * m1[e]);
+        }
+        store8((T*)p.y + o, v);
+    }
+}
+
+__global__ __launch_bounds__(kMaxThreads) void norm_act_columns(NormActParams p) {
+    __shared__ float lds[17 * (kMaxThreads / 16)];
+    column_totals(p, (int)blockIdx.x, lds);
+}
+
 int gcd_of(int a, int b) { return b == 0 ? a : gcd_of(b, a % b); }
 
 // Whole rows where the tokens alone make enough workgroups: every row is one run
@@ -607,6 +856,22 @@ Cut cut_of(int B, int N, int C, int G) {
         if ((int64_t)B * (G / gs) * a.chunks >= kBlocks) break;
     }
     return best;
+}
+
+// The least slab, if a workgroup's registers hold it of all tokens and there are
+// not more workgroups than compute units; else V = 0.  A workgroup of such a
+// slab then does on its own, in one launch, what else the whole chip does in
+// two: faster as long as that is little.  2 x 64 x 1280 bf16 5.7 us forward and
+// 8.4 backward (else 12.9 and 12.0), 2 x 512 x 1280 9.6 and 13.4 (13.9 and
+// 14.9), 8 x 512 x 1280 14.0 and 21.6 (19.5 and 31.0); with the groups of 10
+// channels of 1 x 800 x 320, eight rows of four groups, 13.3 and 15.1 (11.3 and
+// 14.4); with 2048 workgroups, 64 x 256 x 1280, 40 and 87 (40 and 62).
+Cut whole_of(int B, int N, int C, int G, int rows) {
+    const int cg = C / G, gs = 8 / gcd_of(8, cg);
+    Cut a = {B, N, C, G, cg, gs * cg, gs * cg / 8, 0, gs, 1, kMaxThreads};
+    a.RP = a.threads / a.V;
+    if (a.V < kWholeVectors || a.S > kMaxThreads || N > (gs == 1 ? rows : rows / 2) * a.RP || (int64_t)B * (C / a.S) > kWholeBlocks) a.V = 0;
+    return a;
 }
 
 // Rows of a thread of the apply launches: enough workgroups first.
@@ -686,6 +951,18 @@ PCPP_EXPORT int pcpp_group_norm_act(const pcpp_norm_act_geom_t* g, const void* x
     p.apply_blocks = apply_blocks_of(a);
     p.eps = g->eps;
     const hipStream_t s = (hipStream_t)stream;
+    const Cut whole = whole_of(g->batch, g->tokens, g->channels, g->groups, kWholeRows);
+    if (whole.V > 0) {
+        p.cut = whole;
+        with_act(g->act, [&](auto act) {
+            const dim3 grid(whole.C / whole.S, whole.B);
+            if (g->dtype == PCPP_DTYPE_F32)
+                norm_act_whole<float, act()><<<grid, whole.threads, 0, s>>>(p);
+            else
+                norm_act_whole<bf16, act()><<<grid, whole.threads, 0, s>>>(p);
+        });
+        return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+    }
     const dim3 sums(a.chunks, a.C / a.S, a.B), apply(p.apply_blocks, a.C / a.S, a.B);
     if (g->dtype == PCPP_DTYPE_F32)
         norm_act_stats<float, kRunRows / 2><<<sums, a.threads, 0, s>>>(p);
@@ -739,6 +1016,20 @@ PCPP_EXPORT int pcpp_group_norm_act_backward(const pcpp_norm_act_geom_t* g, cons
     p.cut = a;
     p.apply_blocks = apply_blocks_of(a);
     const hipStream_t s = (hipStream_t)stream;
+    const Cut whole = whole_of(g->batch, g->tokens, g->channels, g->groups, kGradRows);
+    if (whole.V > 0) {
+        p.cut = whole;
+        p.columns = (dgamma || dbeta) && whole.B > 1 ? (float*)workspace : nullptr;
+        with_act(g->act, [&](auto act) {
+            const dim3 grid(whole.C / whole.S, whole.B);
+            if (g->dtype == PCPP_DTYPE_F32)
+                norm_act_grad_whole<float, act()><<<grid, whole.threads, 0, s>>>(p);
+            else
+                norm_act_grad_whole<bf16, act()><<<grid, whole.threads, 0, s>>>(p);
+        });
+        if (p.columns) norm_act_columns<<<column_blocks(p), whole.threads, 0, s>>>(p);
+        return hipGetLastError() == hipSuccess ? PCPP_OK : PCPP_EHIP;
+    }
     const dim3 sums(a.chunks, a.C / a.S, a.B);
     const int64_t blocks = (int64_t)p.apply_blocks * (a.C / a.S) * a.B + column_blocks(p);
     with_act(g->act, [&](auto act) {

@@ -27,6 +27,33 @@ def test_many_records(shape, dtype):
         _near(got, w, b, tag)
 
 
+# One, two, four and eight groups of 40 channels to a slab; the most tokens that
+# one workgroup holds, forward (8 or 4 rows of 102) and backward (6 or 3), and
+# one more; the widest slab and a wider one; as many workgroups as compute units
+# and more.
+HELD = [(2, 250, 640, 32), (3, 408, 320, 32), (1, 409, 320, 32), (2, 306, 320, 32), (1, 307, 320, 32), (1, 816, 1280, 32),
+        (1, 817, 1280, 32), (2, 612, 1280, 32), (2, 613, 1280, 32), (1, 7, 1280, 256), (1, 64, 512, 1), (2, 65, 512, 1),
+        (1, 30, 520, 1), (8, 20, 1280, 32), (9, 20, 1280, 32)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+@pytest.mark.parametrize("shape", HELD, ids=str)
+def test_tokens_that_a_workgroup_holds(shape, dtype):
+    B, N, C, G = shape
+    x, gamma, beta, dy = _inputs(B, N, C, dtype, seed=34)
+    y, stats, dx, dgamma, dbeta = _call(x, gamma, beta, G, 1e-5, "gelu", 0.2, dy)
+    d = [t.to(F64) for t in (x, gamma, beta, dy)]
+    r = ref.forward(*d[:3], G, 1e-5, "gelu", 0.2, SEED, FIRST + DRAW, dtype)
+    _near(stats[..., 0], r["mean"], r["mean_bound"] + 1e-30, "mean")
+    _near(stats[..., 1], r["rstd"], r["rstd_bound"], "rstd")
+    _near(y, r["y"], r["bound"], "y")
+    want, bounds = ref.backward(r, d[1], d[3], "gelu", 0.2, SEED, FIRST + DRAW, dtype)
+    for got, w, b, tag in zip((dx, dgamma, dbeta), want, bounds, ("dx", "dgamma", "dbeta")):
+        _near(got, w, b, tag)
+    again = _call(x, gamma, beta, G, 1e-5, "gelu", 0.2, dy, in_place=True, params=False)
+    assert torch.equal(again[2], dx) and torch.equal(again[0], y)
+
+
 def test_beyond_2_to_32_bytes():
     """The second of two images lies 4.3 GB behind the first: as by itself."""
     from paper_2412_02962_amd import pcpp
