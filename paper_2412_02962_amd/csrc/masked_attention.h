@@ -391,14 +391,31 @@ __device__ __forceinline__ void pack(const float (&w)[16], bf16x8 (&o)[2]) {
     for (int r = 0; r < 16; ++r) o[r >> 3][r & 7] = f32_to_bf16(w[r]);
 }
 
-// acc += sum over the 32 rows from row0 of (their weights) x (their channels).
-template <int DB>
-__device__ __forceinline__ void add_rows(f32x16 (&acc)[DB], const bf16x8 (&w)[2], const Reader<DB>& rd, const char* tile,
-                                         int row0) {
+// use(i, read(i)) for i = 0 .. N - 1, the reads AHEAD of their uses: where the
+// registers are few, the compiler's own order is each read, its wait, its use
+// (8192 causal, heads of 128, us: forward 315 and 304 with two ahead, dq 432 and
+// 425, dk and dv 645 and 609; one, three and four ahead are within 1 % of that).
+template <int N, int AHEAD, typename Read, typename Use>
+__device__ __forceinline__ void staged(Read read, Use use) {
+    decltype(read(0)) ring[AHEAD + 1];
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+    for (int i = 0; i < AHEAD && i < N; ++i) ring[i] = read(i);
 #pragma unroll
-        for (int mb = 0; mb < DB; ++mb) acc[mb] = mfma32x32x16(rd.columns(tile, row0 + 16 * st, mb), w[st], acc[mb]);
+    for (int i = 0; i < N; ++i) {
+        if (i + AHEAD < N) ring[(i + AHEAD) % (AHEAD + 1)] = read(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        use(i, ring[i % (AHEAD + 1)]);
+    }
+}
+
+// acc += sum over 32 HB rows from row0 of (their weights) x (their channels).
+template <int DB, int HB>
+__device__ __forceinline__ void add_rows(f32x16 (&acc)[DB], const bf16x8 (&w)[HB][2], const Reader<DB>& rd, const char* tile, int row0) {
+    staged<2 * DB * HB, 2>([&](int i) __attribute__((always_inline)) { return rd.columns(tile, row0 + 16 * (i / DB), i % DB); },
+                               [&](int i, const bf16x8& x) __attribute__((always_inline)) {
+                                   const int st = i / DB, mb = i % DB;
+                                   acc[mb] = mfma32x32x16(x, w[st >> 1][st & 1], acc[mb]);
+                               });
 }
 
 // ---- infinities and NaN in rows that the mask hides from some lanes ----

@@ -8,6 +8,14 @@
 // delta_i = dy_i . y_i takes y as it was rounded; the sum over the keys of P (dP -
 // delta) is what it is off by, since that sum is 0.  masked_dq adds it up and
 // leaves the better delta to masked_dkv, which runs after it.
+//
+// Five products of the forward's two, and the exponentials twice: bound by the
+// vector unit and by waits for LDS, with 16 DB sums of 32 x 32 a lane (twice that
+// for masked_dkv) leaving room for two wavefronts a SIMD and few operands ahead.
+// 8192 causal, 16 heads of 128 on 4 of the keys: masked_dq 425 us (970 TFLOP/s),
+// masked_dkv 609 (900); capped and biased 576 and 724, the matrix unit busy for
+// 29 % of the cycles in both, the vector unit for 52 and 41.  2 x 4096, 10 heads
+// of 64: 180 (715) and 278 (620).
 
 #include <type_traits>
 
@@ -153,11 +161,14 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
         const char* vt = kt + T::BYTES;
         const Reader<DB> rd = reader.fresh();
         f32x16 s, dp;
-#pragma unroll
-        for (int kk = 0; kk < 2 * DB; ++kk) {
-            s = mfma32x32x16(rd.rows(kt, row0, kk), q[kk], kk == 0 ? f32x16{} : s);
-            dp = mfma32x32x16(rd.rows(vt, row0, kk), dy[kk], kk == 0 ? f32x16{} : dp);
-        }
+        staged<4 * DB, 2>([&](int i) __attribute__((always_inline)) { return rd.rows(i & 1 ? vt : kt, row0, i >> 1); },
+                           [&](int i, const bf16x8& x) __attribute__((always_inline)) {
+                               const int kk = i >> 1;
+                               if (i & 1)
+                                   dp = mfma32x32x16(x, dy[kk], kk == 0 ? f32x16{} : dp);
+                               else
+                                   s = mfma32x32x16(x, q[kk], kk == 0 ? f32x16{} : s);
+                           });
         const int base = j0 + 4 * half;
         const float far = (float)(pos - base);
         float w[16];
@@ -189,14 +200,14 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
                 }
             }
         }
-        bf16x8 o[2];
+        bf16x8 o[1][2];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             off += w[r];
             if constexpr (CAP) w[r] *= dp[r];
-            o[r >> 3][r & 7] = f32_to_bf16(w[r]);
+            o[0][r >> 3][r & 7] = f32_to_bf16(w[r]);
         }
-        add_rows<DB>(acc, o, rd, kt, row0);
+        add_rows<DB, 1>(acc, o, rd, kt, row0);
         if constexpr (BIAS) {
             // A bias rests a query on the few keys near it, and there y's own
             // rounding (in delta) is seen in dq.  The weights' is taken out for
@@ -205,9 +216,9 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
             const bool near = slope2 > 0.f && slope2 * (float)apart < NEAR;
             if (__any(near)) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) w[r] = near ? w[r] - bf16_to_f32(o[r >> 3][r & 7]) : 0.f;
-                pack(w, o);
-                add_rows<DB>(acc, o, rd, kt, row0);
+                for (int r = 0; r < 16; ++r) w[r] = near ? w[r] - bf16_to_f32(o[0][r >> 3][r & 7]) : 0.f;
+                pack(w, o[0]);
+                add_rows<DB, 1>(acc, o, rd, kt, row0);
             }
         }
     };
@@ -367,16 +378,27 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) dp[4 * g + e] = d[e];
         }
-#pragma unroll
-        for (int kk = 0; kk < 2 * DB; ++kk) {
-            s = mfma32x32x16(rd.rows(qt, row0, kk), k[kk], kk == 0 ? f32x16{} : s);
-            if constexpr (V_LDS)
-                dp = mfma32x32x16(rd.rows(gt, row0, kk), rd.rows(vt, 32 * wave, kk), dp);
-            else
-                dp = mfma32x32x16(rd.rows(gt, row0, kk), v[kk], dp);
-            if constexpr (DB > 3)
-                if (kk & 1) __builtin_amdgcn_sched_barrier(0);  // no more operands ahead than registers for them
-        }
+        // q for s, and dy with v for dp, in turn
+        struct Operands {
+            bf16x8 a, b;
+        };
+        staged<4 * DB, (DB > 3 ? 1 : 2)>(
+            [&](int i) __attribute__((always_inline)) {
+                Operands o;
+                o.a = rd.rows(i & 1 ? gt : qt, row0, i >> 1);
+                if constexpr (V_LDS)
+                    if (i & 1) o.b = rd.rows(vt, 32 * wave, i >> 1);
+                return o;
+            },
+            [&](int i, const Operands& o) __attribute__((always_inline)) {
+                const int kk = i >> 1;
+                if ((i & 1) == 0)
+                    s = mfma32x32x16(o.a, k[kk], kk == 0 ? f32x16{} : s);
+                else if constexpr (V_LDS)
+                    dp = mfma32x32x16(o.a, o.b, dp);
+                else
+                    dp = mfma32x32x16(o.a, v[kk], dp);
+            });
         const int base = i0 + 4 * half;
         const float far = (float)(sq.pos0 + base - j);
         float w[16], z[16];
@@ -414,13 +436,13 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
                 }
             }
         }
-        bf16x8 o[2];
+        bf16x8 o[1][2];
         if constexpr (DB > 3) __builtin_amdgcn_sched_barrier(0);
-        pack(w, o);
-        add_rows<DB>(dv, o, rd, gt, row0);
+        pack(w, o[0]);
+        add_rows<DB, 1>(dv, o, rd, gt, row0);
         if constexpr (DB > 3) __builtin_amdgcn_sched_barrier(0);
-        pack(z, o);
-        add_rows<DB>(dk, o, rd, qt, row0);
+        pack(z, o[0]);
+        add_rows<DB, 1>(dk, o, rd, qt, row0);
     };
 
     spoilt[tid] = Spoilt{0, 0};

@@ -4,8 +4,18 @@
 //
 // Scores are computed transposed, S^T = K Q^T, a query to a lane: its maximum,
 // its sum and its mask are a lane's own, and P^T is the operand of y^T = V^T P^T
-// as it stands.  The maximum is taken only when a lane's probabilities of 32
-// keys sum to 2^20 or more (or to no number): until then the one before serves.
+// as it stands.  The maximum is taken only when a lane's probabilities of a
+// step's keys sum to 2^20 or more (or to no number): until then the one before
+// serves, which saves its exchange between the halves of the wavefront and the
+// results' factor in nearly every step.  A step is 64 keys, so that the products
+// of some run under the exponentials of others (8192 queries and keys, bf16: 16
+// heads of 64 337 us, 32 keys a step 402; of 128 562, else 654).
+//
+// Bound by the vector unit and the wavefronts' own waits, two or three of them to
+// a SIMD: 8192 causal, 16 heads of 128 on 4 of the keys, capped and biased
+// (three transcendental operations a score), 404 us and 680 TFLOP/s, the matrix
+// unit busy for 27 % of the cycles and the vector unit for 52; without cap and
+// bias 305 us, 900 TFLOP/s; not causal, 16 heads of keys too, 565 us, 970.
 
 #include <type_traits>
 
@@ -80,12 +90,11 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
 #pragma unroll 1
     for (;;) {
         f32x16 s[HB];
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-#pragma unroll
-            for (int kk = 0; kk < 2 * DB; ++kk) s[h] = mfma32x32x16(rd.rows(kt, 32 * h, kk), c.q[kk], kk == 0 ? f32x16{} : s[h]);
-            if constexpr (HB > 1) __builtin_amdgcn_sched_barrier(0);
-        }
+        staged<2 * DB * HB, 2>([&](int i) __attribute__((always_inline)) { return rd.rows(kt, 32 * (i / (2 * DB)), i % (2 * DB)); },
+                               [&](int i, const bf16x8& k) __attribute__((always_inline)) {
+                                   const int h = i / (2 * DB), kk = i % (2 * DB);
+                                   s[h] = mfma32x32x16(k, c.q[kk], kk == 0 ? f32x16{} : s[h]);
+                               });
         // Scores less the maximum, in log2 units; -infinity where not seen (also
         // while the maximum is still -infinity and all others are infinite).
         const float add = search ? 0.f : -st.m;
@@ -159,22 +168,20 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
     }
     after_scores();
     st.l += sum;
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-        add_rows<DB>(st.o, pr[h], rd, vt, 32 * h);
-    }
+    add_rows<DB, HB>(st.o, pr, rd, vt, 0);
     if constexpr (TWO) {
         static_assert(HB == 1, "few queries");
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[0][r] -= bf16_to_f32(pr[0][r >> 3][r & 7]);
         pack(w[0], pr[0]);
-        add_rows<DB>(st.o, pr[0], rd, vt, 0);
+        add_rows<DB, HB>(st.o, pr, rd, vt, 0);
     }
 }
 
 // Which of the 32 keys from j0 the lane's query sees.
 __device__ __forceinline__ uint32_t keys_seen(const Params& p, const Row& row, const int* docs, int j0) {
     uint32_t seen = 0;
+#pragma unroll 1
     for (int j = 0; j < 32; ++j)
         seen |= (uint32_t)((j0 + j < row.limit) & (!p.kv_doc || max(docs[j], -1) == row.doc)) << j;
     return seen;
