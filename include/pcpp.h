@@ -1005,7 +1005,8 @@ typedef struct {
     int32_t head_dim;      /* D, a multiple of 8, 8 .. 128                   */
     int32_t causal;        /* 0 or 1                                         */
     float scale;           /* finite                                         */
-    float cap;             /* finite, > 0; 0: none                           */
+    float cap;             /* up to 4096; 0: none.  A capped score is right
+                            * to 2^-22 of the cap                            */
     int32_t reserved;      /* must be 0                                      */
     /* Elements from a token to the next and from a sequence to the next, both
      * multiples of 8; 0: contiguous (heads * D, and tokens * the row).  A row
@@ -1056,6 +1057,8 @@ int pcpp_masked_attention(const pcpp_masked_geom_t* g, const pcpp_mask_t* m,
  *   y, lse  the forward pass's;  dy  in y's layout
  *   dq, dk, dv  in the layouts of q, k, v; dq, or dk and dv, may be NULL.
  *         Every token's row is written, those behind kv_len too (with 0).
+ *         They may lie side by side in the rows of one tensor; no two may
+ *         share elements (the same pointer: PCPP_EINVAL).
  * No atomics: a result is the same at every call.  Otherwise as above.
  */
 size_t pcpp_masked_attention_backward_workspace_size(const pcpp_masked_geom_t* g);

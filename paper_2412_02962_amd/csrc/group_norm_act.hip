@@ -12,7 +12,14 @@
 // records merged by every workgroup that needs them.  A thread keeps its eight
 // channels for all of its rows, so that their parameters stay in registers.
 // Nothing of the forward pass but mean and rstd is kept: z, the activation's
-// derivative and dropout's mask are computed again.
+// derivative and dropout's mask are computed again.  Few tokens take one launch,
+// a slab of an image in a workgroup's registers (whole_of).
+//
+// 2 x 57600 x 640 bf16, SiLU, dropout: statistics 40 us (3.7 TB/s), apply 66
+// (4.5), sums 77 (3.8; the vector unit's: the mask and the activation), dx 86
+// (5.1), and 5 for each merging of records; 2 x 65536 x 320 without dropout 23,
+// 5 and 28.  The rows of a thread are on their way ROWS at a time while as many
+// are worked on (without that forward and backward 316 us, with it 280).
 
 #include <stdint.h>
 

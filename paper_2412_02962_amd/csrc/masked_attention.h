@@ -5,8 +5,8 @@
 // the lanes: of the scores' tile a lane holds one column (lane % 32) and the
 // rows 8 (r / 4) + 4 (lane / 32) + r % 4 in register r.  Those registers, eight
 // at a time and rounded to bf16, are the second operand of the next product as
-// they stand, if its first operand takes the contracted rows in the same order:
-// row_operand and column_operand do.
+// they stand, if its first operand takes the contracted rows in the same order,
+// as Reader::columns does.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -115,7 +115,8 @@ __device__ __forceinline__ float score(const Params& p, float dot, float add, fl
 // bytes c of row r lie at c ^ swizzle(r).  LDS serves 256 bytes at a time: 16
 // rows at one channel (row reads), or four rows of 64 bytes (transposing reads
 // by 32 lanes); either lies in different banks.  The swizzle repeats every 16
-// rows, and eight rows on it differs in bit 1. ----
+// rows, and eight rows on it differs in bit 1.  (8192 queries and keys: 34 million
+// conflicting cycles with a swizzle by the row's last bits alone, now none.) ----
 
 template <int DB>
 struct Tile {
@@ -335,9 +336,9 @@ struct TileOrder {
 // their own (workgroup w on part w % 8).  `falling`: an item's blocks grow
 // shorter; a part then takes its list by the length, and every other 32
 // workgroups backwards, so that its 32 compute units get long and short ones.
-// 8192 causal queries, 16 heads of 128: 381 us where they came item by item with
-// the longest first, 492 with every other item's shortest first; 4096, 20 heads
-// of 64: 149 and 128.
+// (Forward, before 64 keys a step: 8192 causal queries, 16 heads of 128, 381 us
+// item by item with the longest first, 492 with every other item's shortest
+// first; 2 x 4096, 10 heads of 64, 149 and 128; this order 350 and 99.)
 constexpr int PARTS = 8, PART_UNITS = 32;
 // A division's result as the scalar it is.
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }

@@ -20,6 +20,7 @@ using namespace masked;
 namespace {
 
 constexpr int kMaxTokens = 1 << 24;
+constexpr float kMaxCap = 4096.f;  // (a capped score is off by up to 2^-23 of the cap)
 constexpr int64_t kMaxBatch = (int64_t)1 << 40;  // elements
 constexpr int64_t kMaxRow = 1 << 24;             // 64 rows are less than 2^32 bytes
 constexpr int64_t kMaxHeadTokens = 1 << 29, kMaxHeadBlocks = 1 << 22;
@@ -53,7 +54,7 @@ int check_geom(const pcpp_masked_geom_t* g, Shape* s) {
         return PCPP_EINVAL;
     if (g->heads < 1 || g->heads > 1024 || g->kv_heads < 1 || g->heads % g->kv_heads != 0) return PCPP_EINVAL;
     if (g->causal != 0 && g->causal != 1) return PCPP_EINVAL;
-    if (!isfinite(g->scale) || !isfinite(g->cap) || g->cap < 0.f) return PCPP_EINVAL;
+    if (!isfinite(g->scale) || !(g->cap >= 0.f && g->cap <= kMaxCap)) return PCPP_EINVAL;
     if (g->cap > 0.f && !isfinite(g->scale / g->cap * 2.f * LOG2E)) return PCPP_EINVAL;
     if (g->head_dim < 8 || g->head_dim % 8 != 0 || g->head_dim > 128) return PCPP_ENOTSUP;
     // A launch has fewer than 2^32 threads: 256 for 128 tokens of a sequence's head.
@@ -85,7 +86,8 @@ int64_t range_bytes(const pcpp_masked_geom_t* g) {
 
 // Rows that share their keys few enough for the pieces of masked_few; how many
 // pieces: as many as give every compute unit two workgroups, of eight tiles of
-// 32 keys or more.
+// 32 keys or more (one token on up to 16384 keys, 64 groups: 80 us; with half as
+// many pieces 98, with twice as many 95).
 struct FewPlan {
     bool use;
     int pieces, row_blocks;
@@ -234,6 +236,7 @@ PCPP_EXPORT int pcpp_masked_attention_backward(const pcpp_masked_geom_t* g, cons
     const Range out[] = {{dq, qb}, {dk, kb}, {dv, vb}};
     for (const Range& o : out)
         if (outputs_overlap(&o, 1, in, n_in)) return PCPP_EINVAL;
+    if (dk && (dq == dk || dq == dv || dk == dv)) return PCPP_EINVAL;
     if (outputs_overlap(&in[6], 1, in, 6) || outputs_overlap(&in[6], 1, in + 7, n_in - 7)) return PCPP_EINVAL;
     Params p = params_of(g, m, sh, workspace);
     p.q = (const bf16*)q, p.k = (const bf16*)k, p.v = (const bf16*)v, p.y = (bf16*)y, p.dy = (const bf16*)dy;

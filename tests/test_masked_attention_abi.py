@@ -39,6 +39,7 @@ BAD_GEOM = [
     ("EINVAL", dict(kv_heads=8)), ("EINVAL", dict(causal=2)), ("EINVAL", dict(reserved=1)),
     ("EINVAL", dict(scale=float("nan"))), ("EINVAL", dict(scale=float("inf"))), ("EINVAL", dict(cap=-1.0)),
     ("EINVAL", dict(cap=float("nan"))), ("EINVAL", dict(cap=float("inf"))), ("EINVAL", dict(cap=1e-30, scale=1e30)),
+    ("EINVAL", dict(cap=4097.0)),
     ("ENOTSUP", dict(head_dim=4)), ("ENOTSUP", dict(head_dim=12)), ("ENOTSUP", dict(head_dim=136)),
     # launches of 2^32 threads
     ("EINVAL", dict(batch=65535, n_q=1, n_kv=1, heads=1024, kv_heads=1)), ("EINVAL", dict(batch=33, n_kv=1 << 24, heads=1, kv_heads=1)),
@@ -107,7 +108,8 @@ BACKWARD = [("EINVAL", {n: None}) for n in ("q", "k", "v", "y", "lse", "dy", "dk
     ("EINVAL", {n: _p(n, 8)}) for n in ("q", "k", "v", "y", "dy", "dq", "dk", "dv", "ws")] + [
     ("EINVAL", dict(lse=_p("lse", 2))), ("EINVAL", dict(dq=None, dk=None, dv=None)), ("EWORKSPACE", dict(ws=None)),
     ("EWORKSPACE", dict(wsb=8)), ("EINVAL", dict(dq=_p("q"))), ("EINVAL", dict(dk=_p("k"))), ("EINVAL", dict(dv=_p("dy", 16))),
-    ("EINVAL", dict(dq=_p("dy"))), ("EINVAL", dict(dk=_p("lse", 0))), ("EINVAL", dict(ws=_p("dq"))), ("EINVAL", dict(ws=_p("y"))),
+    ("EINVAL", dict(dq=_p("dy"))), ("EINVAL", dict(dk=_p("lse", 0))),
+    ("EINVAL", dict(dk=_p("dv"))), ("EINVAL", dict(dq=_p("dk"))), ("EINVAL", dict(dv=_p("dq"))), ("EINVAL", dict(ws=_p("dq"))), ("EINVAL", dict(ws=_p("y"))),
 ]
 
 
