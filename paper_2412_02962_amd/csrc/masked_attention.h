@@ -345,20 +345,21 @@ __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirst
 struct Place {
     int item, block;  // item < 0: none
 };
-__device__ __forceinline__ Place place_in(int64_t items, int blocks, bool falling) {
-    const int64_t n = items * blocks, per = (n + PARTS - 1) / PARTS;
-    const int64_t from = (int64_t)(blockIdx.x % PARTS) * per, to = min(from + per, n);
-    const int64_t k0 = blockIdx.x / PARTS;
-    if (from + k0 >= to || k0 >= per) return Place{-1, 0};
-    const int64_t at = from + k0;
-    if (!falling) return Place{scalar((int)(at / blocks)), scalar((int)(at % blocks))};
-    const int count = (int)(to - from);
-    int k = (int)k0;
+__device__ __forceinline__ Place place_in(int items, int blocks, bool falling) {
+    const int n = items * blocks, per = (n + PARTS - 1) / PARTS;  // (below 2^24)
+    const int from = (int)(blockIdx.x % PARTS) * per, to = min(from + per, n);
+    const int count = to - from;
+    int k = (int)(blockIdx.x / PARTS);
+    if (k >= count) return Place{-1, 0};
+    if (!falling) {
+        const int item = scalar((from + k) / blocks);
+        return Place{item, from + k - item * blocks};
+    }
     const int round = k / PART_UNITS;
     if ((round & 1) && (round + 1) * PART_UNITS <= count) k = round * PART_UNITS + (PART_UNITS - 1 - k % PART_UNITS);
     // The part's list: item h0 from block o on, whole items, item h1 up to block e.
-    const int h0 = scalar((int)(from / blocks)), o = scalar((int)(from % blocks));
-    const int h1 = scalar((int)(to / blocks)), e = scalar((int)(to % blocks));
+    const int h0 = scalar(from / blocks), o = from - h0 * blocks;
+    const int h1 = scalar(to / blocks), e = to - h1 * blocks;
     if (h0 == h1) return Place{h0, o + k};
     const int head = o > 0, whole = h1 - h0 - head;
     auto before = [&](int block) { return whole * block + (head ? max(block - o, 0) : 0) + min(block, e); };  // blocks of smaller number
