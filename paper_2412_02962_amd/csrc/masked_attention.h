@@ -339,24 +339,28 @@ struct TileOrder {
 // (Forward, before 64 keys a step: 8192 causal queries, 16 heads of 128, 381 us
 // item by item with the longest first, 492 with every other item's shortest
 // first; 2 x 4096, 10 heads of 64, 149 and 128; this order 350 and 99.)
+// `uneven`: documents, the same for all heads, so that blocks of like length come
+// at like places: every other 32 workgroups backwards too (2 x 4096, 10 heads,
+// 9 documents: forward 74 and 69 us, dq 87 and 82; dk and dv, in two rounds, 110
+// and 112: not there).
 constexpr int PARTS = 8, PART_UNITS = 32;
 // A division's result as the scalar it is.
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 struct Place {
     int item, block;  // item < 0: none
 };
-__device__ __forceinline__ Place place_in(int items, int blocks, bool falling) {
+__device__ __forceinline__ Place place_in(int items, int blocks, bool falling, bool uneven) {
     const int n = items * blocks, per = (n + PARTS - 1) / PARTS;  // (below 2^24)
     const int from = (int)(blockIdx.x % PARTS) * per, to = min(from + per, n);
     const int count = to - from;
     int k = (int)(blockIdx.x / PARTS);
     if (k >= count) return Place{-1, 0};
+    const int round = k / PART_UNITS;
+    if ((falling || uneven) && (round & 1) && (round + 1) * PART_UNITS <= count) k = round * PART_UNITS + (PART_UNITS - 1 - k % PART_UNITS);
     if (!falling) {
         const int item = scalar((from + k) / blocks);
         return Place{item, from + k - item * blocks};
     }
-    const int round = k / PART_UNITS;
-    if ((round & 1) && (round + 1) * PART_UNITS <= count) k = round * PART_UNITS + (PART_UNITS - 1 - k % PART_UNITS);
     // The part's list: item h0 from block o on, whole items, item h1 up to block e.
     const int h0 = scalar(from / blocks), o = from - h0 * blocks;
     const int h1 = scalar(to / blocks), e = to - h1 * blocks;

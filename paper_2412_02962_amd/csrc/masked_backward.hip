@@ -108,7 +108,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + BLOCK - 1) / BLOCK;
-    const Place place = place_in(p.B * p.H, nqb, p.causal);
+    const Place place = place_in(p.B * p.H, nqb, p.causal, p.kv_doc != nullptr);
     if (place.item < 0) return;
     const int bh = place.item, qb = nqb - 1 - place.block;
     const int b = scalar(bh / p.H), head = bh - b * p.H, kh = scalar(head / p.G);
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nkb = (p.nkv + BLOCK - 1) / BLOCK;
-    const Place place = place_in(p.B * p.KH * p.pieces, nkb, p.causal);
+    const Place place = place_in(p.B * p.KH * p.pieces, nkb, p.causal, false);
     if (place.item < 0) return;
     const int item = place.item, kb = place.block;  // (the first keys are seen by the most)
     const int bk = scalar(item / p.pieces), piece = item - bk * p.pieces;

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nqb = (p.nq + QB - 1) / QB;
-    const Place place = place_in(p.B * p.H, nqb, p.causal);
+    const Place place = place_in(p.B * p.H, nqb, p.causal, p.kv_doc != nullptr);
     if (place.item < 0) return;
     const int bh = place.item, qb = nqb - 1 - place.block;
     const int b = scalar(bh / p.H), head = bh - b * p.H, kh = scalar(head / p.G);
