@@ -384,7 +384,6 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
         return t;
     };
     auto same = [&](int t) { return !p.kv_doc || (t >= t0 && (whole >> ((base - t) / NW) & 1)); };
-    int dr = -1;
     // Keys and values of two tiles are on their way at a time, each into the
     // place of those just used.
     const uint32_t docs0 = lds_address(docs[wave]);

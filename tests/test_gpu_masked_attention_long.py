@@ -24,7 +24,7 @@ def _check(q, k, v, dy, m, causal=False, cap=0.0, scale=0.125, few=False, tag=""
 
 
 # The keys' gradients in pieces of the queries (heads / kv_heads * n_q / 64 tiles
-# of them, eight or more to a piece), the last ones ragged, some empty.
+# of them, two or more to a piece), the last ones ragged, some empty.
 PIECES = [(1, 577, 513, 4, 1, 64), (1, 1100, 300, 2, 1, 128), (2, 700, 130, 6, 2, 96), (1, 1537, 1, 1, 1, 40)]
 
 
@@ -41,6 +41,17 @@ def test_pieces_of_the_queries(shape, kind):
         draw = lambda n: torch.randint(-1, 4, (B, n), generator=gen).sort(-1).values.to(torch.int32)
         m = ref.Masks(q_doc=draw(nq), kv_doc=draw(nkv))
     _check(q, k, v, dy, m, causal=kind == "causal", cap=8.0 if kind == "causal" else 0.0, tag=f"{shape} {kind}")
+
+
+@pytest.mark.parametrize("docs", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+def test_several_rounds_of_workgroups(causal, docs):
+    """560 blocks of queries and 896 of keys: more than twice 32 to each part of
+    the chip, which take them in an order of their own."""
+    shape = (4, 777, 777, 20, 4, 40)
+    (q, k, v, dy), gen = _inputs(*shape, seed=26)
+    doc = torch.randint(-1, 5, (4, 777), generator=gen).sort(-1).values.to(torch.int32) if docs else None
+    _check(q, k, v, dy, ref.Masks(q_doc=doc, kv_doc=doc), causal=causal, scale=0.16, tag=f"{causal} {docs}")
 
 
 @pytest.mark.parametrize("causal", [False, True])

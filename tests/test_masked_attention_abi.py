@@ -136,5 +136,5 @@ def test_workspaces():
     assert f(pcpp.make_masked_geom(1, 1, 1 << 20, 32, 8, 128)) == 8 * (1 + (1 << 14)) + 8 + 512 * 32 * 130 * 4
     # two float32 of every query and head
     assert b(pcpp.make_masked_geom(1, 64, 64, 1, 1, 64)) == 16 + 2 * 64 * 4
-    # causal keys' gradients in four pieces of the queries: 36 tiles
-    assert b(pcpp.make_masked_geom(1, 576, 513, 4, 1, 64, causal=True)) == 8 * (9 + 9) + 2 * 4 * 576 * 4 + 4 * 513 * 2 * 64 * 4
+    # keys' gradients in 18 pieces of the queries, two of 36 tiles each
+    assert b(pcpp.make_masked_geom(1, 576, 513, 4, 1, 64, causal=True)) == 8 * (9 + 9) + 2 * 4 * 576 * 4 + 18 * 513 * 2 * 64 * 4
