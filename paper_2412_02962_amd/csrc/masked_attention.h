@@ -242,7 +242,8 @@ struct Reader {
 };
 
 // 0 to the whole of a workgroup's tiles, where a head has fewer channels than
-// they do: what no load writes stays 0.
+// their rows: what no load writes stays 0, also for the look at infinities and
+// NaN, which takes whole rows.
 __device__ __forceinline__ void clear_tiles(char* lds, int bytes, int threads) {
     for (int i = 16 * threadIdx.x; i < bytes; i += 16 * threads) *(u32x4*)(lds + i) = u32x4{};
 }

@@ -84,8 +84,12 @@ int64_t range_bytes(const pcpp_masked_geom_t* g) {
     return round16((int64_t)g->batch * (tiles_of(g->n_q) + tiles_of(g->n_kv)) * sizeof(DocRange));
 }
 
-// Rows that share their keys few enough for the pieces of masked_few; how many
-// pieces: as many as give every compute unit two workgroups, of eight tiles of
+// Rows that share their keys few enough for masked_few: 64, or of all sequences
+// as many as leave half the compute units without a workgroup of 32 rows, whose
+// four wavefronts then share the keys (forward, us: 1000 queries and keys, 4
+// heads of 64, 22 and 14; 4000, one of 128, 99 and 54; 500, 8 of 128, at the
+// limit, 17.9 and 17.1; with twice the workgroups slower: 2000, 8 of 64, 39 and
+// 45).  How many pieces of the keys: as many as give every compute unit two workgroups, of eight tiles of
 // 32 keys or more (one token on up to 16384 keys, 64 groups: 80 us; with half as
 // many pieces 98, with twice as many 95).
 struct FewPlan {
@@ -94,7 +98,8 @@ struct FewPlan {
 };
 FewPlan few_plan(const pcpp_masked_geom_t* g) {
     const int64_t rows = (int64_t)g->heads / g->kv_heads * g->n_q;
-    FewPlan f = {rows <= 2 * MASKED_FEW_ROWS, 1, (int)((rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS)};
+    const int64_t most = (int64_t)g->batch * g->kv_heads * ((rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS);
+    FewPlan f = {rows <= 2 * MASKED_FEW_ROWS || (most <= 128 && g->n_kv >= 128), 1, (int)((rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS)};
     if (!f.use) return f;
     const int64_t groups = (int64_t)g->batch * g->kv_heads * f.row_blocks, tiles = (g->n_kv + 31) / 32;
     int64_t pieces = (512 + groups - 1) / groups;

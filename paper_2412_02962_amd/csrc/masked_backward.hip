@@ -150,7 +150,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
         vload.issue(vb, t * TILE, sq.len, lds0 + slot * SLOT + T::BYTES);
         if (p.kv_doc && tid < TILE) dr = t * TILE + tid < sq.len ? max(p.kv_doc[(int64_t)b * p.nkv + t * TILE + tid], -1) : -1;
     };
-    if (p.D < 32 * DB) {
+    if (2 * p.D < T::RB) {
         clear_tiles(lds, 2 * SLOT, NT);
         __syncthreads();
     }
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     const int doc = live && p.kv_doc ? own_document(p.kv_doc[(int64_t)b * p.nkv + j]) : NO_DOC;
     // The queries that see key j by length, past and prefix: from .. nq - 1.
     const int from = !live || (p.kv_doc && doc == NO_DOC) ? p.nq : !p.causal || j < sq.prefix ? 0 : min(max(j - sq.pos0, 0), p.nq);
-    if (V_LDS || p.D < 32 * DB) {
+    if (V_LDS || 2 * p.D < T::RB) {
         clear_tiles(lds, LDS, NT);
         __syncthreads();
     }

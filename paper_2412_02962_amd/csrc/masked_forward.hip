@@ -247,7 +247,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
         if (p.kv_doc && tid < TILE)
             load_lds4(uniform64((uint64_t)(uintptr_t)(p.kv_doc + (int64_t)b * p.nkv + t * TILE)), 4 * min(tid, sq.len - 1 - t * TILE), docs0 + slot * TILE * 4);
     };
-    if (p.D < 32 * DB) {
+    if (2 * p.D < T::RB) {
         clear_tiles(lds, 2 * SLOT, NT);
         __syncthreads();
     }
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     if (p.lse && lane < 32) p.lse[(int64_t)bh * p.nq + i] = l == 0.f ? -INFINITY : (st.m + log2f(l)) * LN2;
 }
 
-// ---- few queries ----
+// ---- few queries, or few workgroups of many ----
 //
 // Up to 32 rows (the queries of all heads that share a key head) to a
 // workgroup, which takes a piece of the keys; its wavefronts take tiles of 32
@@ -351,7 +351,9 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
     DocRange mine = {};
     if (p.kv_doc) mine = range_of_lanes(row.doc, true);
     const DocRange* ranges = p.kv_range + (int64_t)b * tiles_of(p.nkv);
-    const int lim_lo = limit_of(p, sq, 0), lim_hi = limit_of(p, sq, p.nq - 1);
+    // the block's queries, of one head, or all
+    const int r0 = rb * MASKED_FEW_ROWS, r1 = min(r0 + MASKED_FEW_ROWS, rows) - 1, h0 = r0 / p.nq, h1 = r1 / p.nq;
+    const int lim_lo = limit_of(p, sq, h0 == h1 ? r0 - h0 * p.nq : 0), lim_hi = limit_of(p, sq, h0 == h1 ? r1 - h0 * p.nq : p.nq - 1);
     const int tiles = (lim_hi + FEW_KEYS - 1) / FEW_KEYS;
     const int t0 = (int)((int64_t)tiles * piece / p.pieces), t1 = (int)((int64_t)tiles * (piece + 1) / p.pieces);
     char* lds = lds_all + wave * 2 * SLOT;
@@ -394,7 +396,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
             load_lds4(uniform64((uint64_t)(uintptr_t)(p.kv_doc + (int64_t)b * p.nkv + t * FEW_KEYS)), 4 * min(lane, sq.len - 1 - t * FEW_KEYS),
                       docs0 + slot * FEW_KEYS * 4);
     };
-    if (p.D < 32 * DB) {
+    if (2 * p.D < T::RB) {
         clear_tiles(lds_all, NW * 2 * SLOT, NT);
         __syncthreads();
     }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests import masked_reference as ref
+from tests import test_gpu_masked_attention as short
 from tests.test_gpu_masked_attention import BF16, DEV, F32, F64, _call, _compare, _dev, _inputs, _ints
 
 pytestmark = pytest.mark.gpu
@@ -41,6 +42,44 @@ def test_pieces_of_the_queries(shape, kind):
         draw = lambda n: torch.randint(-1, 4, (B, n), generator=gen).sort(-1).values.to(torch.int32)
         m = ref.Masks(q_doc=draw(nq), kv_doc=draw(nkv))
     _check(q, k, v, dy, m, causal=kind == "causal", cap=8.0 if kind == "causal" else 0.0, tag=f"{shape} {kind}")
+
+
+# B, nq, nkv, H, KH, D: sequences enough for blocks of 128 queries to a workgroup
+MANY = [(17, 129, 129, 4, 2, 80), (9, 257, 190, 6, 2, 128), (20, 96, 333, 6, 2, 96), (40, 70, 127, 2, 2, 64), (5, 513, 513, 2, 2, 64),
+        (12, 127, 256, 4, 4, 120)]
+
+
+@pytest.mark.parametrize("shape", MANY, ids=str)
+def test_blocks_of_queries(shape):
+    short.test_plain(shape)
+    short.test_causal_prefix_bias_cap(shape)
+    for sorted_ in (True, False):
+        short.test_documents(shape, sorted_)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 700, 513, 20, 20, 64), (1, 700, 300, 20, 20, 128), (1, 400, 140, 40, 20, 96)], ids=str)
+def test_blocks_of_queries_lengths_and_positions(shape, causal):
+    short.test_lengths_and_positions(shape, causal)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")], ids=str)
+@pytest.mark.parametrize("shape", [(12, 200, 200, 2, 1, 64), (14, 150, 150, 2, 2, 128), (20, 200, 260, 2, 1, 40), (20, 200, 260, 2, 1, 96)], ids=str)
+def test_blocks_of_queries_what_is_not_seen(shape, bad):
+    short.test_what_is_not_seen_does_not_count(shape, bad)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_blocks_of_queries_growing_scores(D):
+    """Scores that grow by hundreds along the keys, fall, and one that dwarfs the
+    rest: 40 sequences of 100 queries."""
+    (q, k, v, dy), _ = _inputs(40, 100, 400, 1, 1, D, seed=27)
+    for order in (1, -1):
+        ramp = torch.arange(400.0)[:, None] * order
+        k2 = (torch.ones(400, D) * ramp / 100).to(BF16).reshape(1, 400, 1, D).repeat(40, 1, 1, 1)
+        _check(torch.full_like(q, 4.0), k2, v, dy, ref.Masks(), tag=f"ramp {order}")
+    k[:, 250] = 30.0
+    _check(q, k, v, dy, ref.Masks(), tag="spike")
 
 
 @pytest.mark.parametrize("docs", [False, True])
