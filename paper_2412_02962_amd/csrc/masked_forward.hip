@@ -39,16 +39,17 @@ struct Row {
     float slope2;         // of the bias, log2 units
 };
 
-// Running maximum (log2 units), sum and result of the lanes' queries.
+// Running maximum (log2 units), sum and result of the lanes' queries; `exact`:
+// the sum of the probabilities as they were before their rounding to bf16.
 template <int DB>
 struct State {
-    float m, l;
+    float m, l, exact;
     f32x16 o[DB];
 };
 template <int DB>
 __device__ __forceinline__ void clear(State<DB>& st) {
     st.m = -INFINITY;
-    st.l = 0.f;
+    st.l = st.exact = 0.f;
 #pragma unroll
     for (int mb = 0; mb < DB; ++mb)
 #pragma unroll
@@ -68,8 +69,14 @@ struct Context {
 // 32 HB keys from key j0, the tiles' first rows.  partial: some query does
 // not see some key.  TWO: the probabilities as two bf16 (for few queries, where
 // the products cost nothing and a token's error counts).
+// EXACT: the sum for lse too.  y is divided by the sum of the rounded
+// probabilities: where one key dominates, the rounding of its weight is above
+// and below the line and cancels.  In lse nothing would cancel it: off by up to
+// 2^-8 there, and with it all of the row's probabilities in the backward pass.
+// (Without lse and with it, us: 8192 causal, 16 heads of 128 on 4, 289 and 303;
+// 8192, 16 heads of 64, 345 and 366; packed documents 67.0 and 67.1.)
 // after_scores: what may run once the keys have been used.
-template <int DB, int HB, bool CAP, bool BIAS, bool TWO, typename After>
+template <int DB, int HB, bool CAP, bool BIAS, bool TWO, bool EXACT, typename After>
 __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs, int j0,
                                      bool partial, bool first, After after_scores) {
     const Params& p = c.p;
@@ -85,7 +92,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
     bool search = first, tried = false;
     float w[HB][16];
     bf16x8 pr[HB][2];
-    float sum;
+    float sum, exact;
     uint32_t over = search ? ~0u : 0u;  // the lanes that need another maximum
 #pragma unroll 1
     for (;;) {
@@ -137,6 +144,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
             const float alpha = m_new == st.m ? 1.f : fast_exp2(st.m - m_new);
             st.m = m_new;
             st.l *= alpha;
+            if constexpr (EXACT) st.exact *= alpha;
 #pragma unroll
             for (int mb = 0; mb < DB; ++mb)
 #pragma unroll
@@ -146,7 +154,7 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
             tried = true;
             continue;
         }
-        sum = 0.f;
+        sum = exact = 0.f;
 #pragma unroll
         for (int h = 0; h < HB; ++h)
 #pragma unroll
@@ -161,13 +169,16 @@ __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const 
                     sum += a + b;
                 else
                     sum = __builtin_amdgcn_fdot2_f32_bf16(pk, bf16x2{(bf16)1.f, (bf16)1.f}, sum, false);
+                if constexpr (EXACT) exact += a + b;
             }
+        if constexpr (EXACT) asm volatile("" : "+v"(exact));  // (here, not behind the loop with all of w for it)
         if (tried || !__any(!(sum < P_LIMIT))) break;
         over = max_halves(sum < P_LIMIT ? 0.f : 1.f) > 0.f;
         search = true;
     }
     after_scores();
     st.l += sum;
+    if constexpr (EXACT) st.exact += exact;
     add_rows<DB, HB>(st.o, pr, rd, vt, 0);
     if constexpr (TWO) {
         static_assert(HB == 1, "few queries");
@@ -196,7 +207,7 @@ __device__ __forceinline__ Row row_of(const Params& p, const Seq& sq, int b, int
     return r;
 }
 
-template <int DB, bool CAP, bool BIAS>
+template <int DB, bool CAP, bool BIAS, bool LSE>
 __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) {
     using T = Tile<DB>;
     constexpr int SLOT = 2 * T::BYTES;  // K, V
@@ -291,7 +302,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
         }
         const int j0 = t * TILE;
         if (j0 < lim_hi && !apart) {
-            step<DB, 2, CAP, BIAS, false>(c, st, kt, kt + T::BYTES, docs[slot], j0, j0 + TILE > lim_lo || !same, first, []() {});
+            step<DB, 2, CAP, BIAS, false, LSE>(c, st, kt, kt + T::BYTES, docs[slot], j0, j0 + TILE > lim_lo || !same, first, []() {});
             first = false;
         }
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
     }
     put_spoilt<DB>(spoilt + tid, st.o);
 
-    const float l = sum_halves(st.l);
+    const float l = sum_halves(st.l), exact = LSE ? sum_halves(st.exact) : 0.f;
     if (!in) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     bf16* out = p.y + b * p.y_batch + (int64_t)i * p.y_row + head * p.D + 4 * (lane >> 5);
@@ -313,7 +324,7 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
             for (int e = 0; e < 4; ++e) v[e] = f32_to_bf16(st.o[mb][4 * g + e] * inv);
             *(bf16x4*)(out + 32 * mb + 8 * g) = v;
         }
-    if (p.lse && lane < 32) p.lse[(int64_t)bh * p.nq + i] = l == 0.f ? -INFINITY : (st.m + log2f(l)) * LN2;
+    if (LSE && lane < 32) p.lse[(int64_t)bh * p.nq + i] = exact == 0.f ? -INFINITY : (st.m + log2f(exact)) * LN2;
 }
 
 // ---- few queries, or few workgroups of many ----
@@ -441,7 +452,7 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
         const int un = u >= t0 ? next(u - NW) : u;
         const bool whole_n = same(un);
         const bool more = u >= t0 && un >= t0;
-        step<DB, 1, CAP, BIAS, true>(c, st, kt, vt, docs[wave][slot], j0, partial, first, [&]() {
+        step<DB, 1, CAP, BIAS, true, false>(c, st, kt, vt, docs[wave][slot], j0, partial, first, [&]() {
             if (more) issue_k(un, slot);
         });
         first = false;
@@ -577,7 +588,10 @@ hipError_t launch_masked_ranges(const Params& p, hipStream_t s) {
 hipError_t launch_masked_forward(const Params& p, hipStream_t s) {
     const int64_t blocks = (int64_t)p.B * p.H * ((p.nq + QB - 1) / QB);
     return with_shape(p, [&](auto db, auto cap, auto bias) {
-        masked_forward<db(), cap(), bias()><<<blocks_for(blocks), NT, 0, s>>>(p);
+        if (p.lse)
+            masked_forward<db(), cap(), bias(), true><<<blocks_for(blocks), NT, 0, s>>>(p);
+        else
+            masked_forward<db(), cap(), bias(), false><<<blocks_for(blocks), NT, 0, s>>>(p);
         return hipGetLastError();
     });
 }
