@@ -930,7 +930,7 @@ int pcpp_dropout(int64_t n, int32_t x_dtype, int32_t y_dtype, float p,
 
 typedef struct {
     int32_t batch;         /* images, 1 .. 65535                             */
-    int32_t tokens;        /* of an image, >= 1                              */
+    int32_t tokens;        /* of an image, 1 .. 2^30                         */
     int32_t channels;      /* a multiple of 8, <= 2560                       */
     int32_t groups;        /* dividing the channels, <= 256                  */
     int32_t act;           /* PCPP_ACT_GELU, PCPP_ACT_SILU or PCPP_ACT_NONE  */

@@ -38,6 +38,7 @@ namespace pcpp {
 namespace {
 
 constexpr int kMaxThreads = 512;
+constexpr int kMaxTokens = 1 << 30;  // row numbers are 32 bits, those of rows on their way behind the last too
 constexpr int kMaxGroups = 256;
 constexpr int kRunRows = 8;      // rows that a thread of the statistics takes at a time
 constexpr int kBlocks = 512;     // workgroups of a launch that sums: two to a compute unit
@@ -905,7 +906,7 @@ void with_act(int act, F f) {
 
 int check_geom(const pcpp_norm_act_geom_t* g) {
     if (!g || g->reserved != 0) return PCPP_EINVAL;
-    if (g->batch < 1 || g->batch > 65535 || g->tokens < 1 || g->channels < 1 || g->groups < 1) return PCPP_EINVAL;
+    if (g->batch < 1 || g->batch > 65535 || g->tokens < 1 || g->tokens > kMaxTokens || g->channels < 1 || g->groups < 1) return PCPP_EINVAL;
     if (!(g->eps > 0.f) || !(g->drop >= 0.f && g->drop <= 1.f)) return PCPP_EINVAL;
     if (g->dtype != PCPP_DTYPE_F32 && g->dtype != PCPP_DTYPE_BF16) return PCPP_ENOTSUP;
     if (g->act != PCPP_ACT_GELU && g->act != PCPP_ACT_SILU && g->act != PCPP_ACT_NONE) return PCPP_ENOTSUP;
