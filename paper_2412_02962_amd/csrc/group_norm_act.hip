@@ -154,7 +154,7 @@ __device__ __forceinline__ int group_lanes(int threads, int gs) {
 // al.'s update: no difference of large sums anywhere.
 template <typename T, int ROWS>
 __global__ __launch_bounds__(kMaxThreads) void norm_act_stats(NormActParams p) {
-    __shared__ float lds_mean[kMaxThreads * 8], lds_m2[kMaxThreads * 8];
+    __shared__ __attribute__((aligned(16))) float lds_mean[kMaxThreads * 8], lds_m2[kMaxThreads * 8];
     const Cut a = p.cut;
     const int chunk = blockIdx.x, slab = blockIdx.y, b = blockIdx.z;
     const int lo = (int)((int64_t)a.N * chunk / a.chunks), hi = (int)((int64_t)a.N * (chunk + 1) / a.chunks);
@@ -414,7 +414,7 @@ __device__ __forceinline__ void grad8(const NormActParams& p, const DropoutKey& 
 
 template <typename T, int ACT, int ROWS>
 __global__ __launch_bounds__(kMaxThreads) void norm_act_grad_sums(NormActParams p) {
-    __shared__ float lds_n[kMaxThreads * 8], lds_g[kMaxThreads * 8];
+    __shared__ __attribute__((aligned(16))) float lds_n[kMaxThreads * 8], lds_g[kMaxThreads * 8];
     const Cut a = p.cut;
     const int chunk = blockIdx.x, slab = blockIdx.y, b = blockIdx.z;
     const int lo = (int)((int64_t)a.N * chunk / a.chunks), hi = (int)((int64_t)a.N * (chunk + 1) / a.chunks);
