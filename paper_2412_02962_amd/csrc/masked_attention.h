@@ -216,10 +216,12 @@ struct Reader {
         col_at = (uint32_t)(t * T::RB + 16 * ((e >> 3) ^ T::swizzle(t)) + 2 * (e & 7));
     }
     // The addresses of the reads that follow are worked out there, not kept in
-    // registers for the whole loop.
+    // registers for the whole loop (TIGHT: where a third wavefront of a SIMD needs
+    // them).
+    template <bool TIGHT = false>
     __device__ __forceinline__ Reader fresh() const {
         Reader r = *this;
-        if constexpr (DB > 2) asm volatile("" : "+v"(r.row_at), "+v"(r.col_at));
+        if constexpr (DB > 2 || TIGHT) asm volatile("" : "+v"(r.row_at), "+v"(r.col_at));
         return r;
     }
     // Rows row0 + (lane % 32), channels 16 kk + 8 (lane / 32) ..: a product
@@ -427,12 +429,14 @@ __device__ __forceinline__ void add_rows(f32x16 (&acc)[DB], const bf16x8 (&w)[HB
 
 // ---- infinities and NaN in rows that the mask hides from some lanes ----
 //
-// A product takes 0 x infinity from a row that a lane's weight of 0 hides.  So
-// a tile that some lane does not see all of is looked over when it has landed;
-// where it holds infinities or NaN (never, in a sound program), every lane
-// notes which of its sums they belong to, and they become 0 in LDS.
+// A product over rows takes 0 x infinity from a row that a lane's weight of 0
+// hides.  So a tile that some lane does not see all of is looked over when it has
+// landed; where it holds infinities or NaN (never, in a sound program), every
+// lane notes which of its sums they belong to, and which of its scores they make
+// infinite or NaN where these are products with the same tile; then they become 0
+// in LDS.
 
-// Sixteen bytes at a: whether there are any; and, `clean`, 0 in their place.
+// Sixteen bytes at a: whether there are any; and 0 in their place.
 __device__ __forceinline__ bool not_finite16(const char* a) {
     const u32x4 w = *(const u32x4*)a;
     bool bad = false;
@@ -481,10 +485,13 @@ __device__ __forceinline__ void note_spoilt(Spoilt* mine, const char* tile, int 
     mine->plus = plus;
     mine->minus = minus;
 }
+// Into the sums: with weights above 0 an infinity stays one; `no_number`: with
+// weights of 0 it is NaN.
 template <int DB>
-__device__ __forceinline__ void put_spoilt(const Spoilt* mine, f32x16 (&acc)[DB]) {
-    const uint64_t plus = mine->plus, minus = mine->minus;
+__device__ __forceinline__ void put_spoilt(const Spoilt* mine, f32x16 (&acc)[DB], bool no_number = false) {
+    uint64_t plus = mine->plus, minus = mine->minus;
     if (!__any((plus | minus) != 0)) return;
+    if (no_number) plus = minus = plus | minus;
 #pragma unroll
     for (int mb = 0; mb < DB; ++mb)
 #pragma unroll
@@ -492,6 +499,35 @@ __device__ __forceinline__ void put_spoilt(const Spoilt* mine, f32x16 (&acc)[DB]
             if (plus >> (16 * mb + r) & 1) acc[mb][r] += INFINITY;
             if (minus >> (16 * mb + r) & 1) acc[mb][r] -= INFINITY;
         }
+}
+
+// What the infinities and NaN of the 32 rows from row0 of a tile make of the
+// lane's scores with them, `own` its own row in memory: bit r for infinity in
+// register r, bit 16 + r for -infinity, both for NaN.  (One by one: a product of
+// matrices in this place would cost the kernels 25 registers more.)
+template <int DB>
+__device__ __forceinline__ uint32_t note_scores(const char* tile, int row0, const bf16* own, int D, int lane) {
+    uint32_t odd = 0;
+#pragma unroll 1
+    for (int r = 0; r < 16; ++r) {
+        const int j = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+        float z = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < D; ++c) {
+            const float x = bf16_to_f32(*(const bf16*)(tile + (row0 + j) * Tile<DB>::RB + 16 * (c >> 3 ^ Tile<DB>::swizzle(j)) + 2 * (c & 7)));
+            if (!(fabsf(x) < INFINITY)) z = __builtin_fmaf(x, bf16_to_f32(own[c]), z);
+        }
+        odd |= (uint32_t)!(z < INFINITY) << r | (uint32_t)!(z > -INFINITY) << (16 + r);
+    }
+    return odd;
+}
+// What the product with the cleaned rows is added to.
+__device__ __forceinline__ void put_scores(uint32_t odd, f32x16& s) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        s[r] += (odd >> r & 1 ? INFINITY : 0.f) - (odd >> (16 + r) & 1 ? INFINITY : 0.f);
+        asm volatile("" : "+v"(odd));
+    }
 }
 
 __device__ __forceinline__ float max_halves(float v) {

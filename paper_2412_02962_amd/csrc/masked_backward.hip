@@ -99,11 +99,13 @@ __device__ __forceinline__ void store_sums(bf16* row, float* part, const f32x16 
 constexpr float NEAR = 8.f;  // (in log2 units: a bias of a factor of 256)
 
 template <int DB, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
+__global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_dq(Params p) {
     using T = Tile<DB>;
     constexpr int SLOT = 2 * T::BYTES;  // K, V
     __shared__ __attribute__((aligned(16))) char lds[2 * SLOT];
     __shared__ __attribute__((aligned(16))) int docs[2][TILE];
+    __shared__ Spoilt spoilt[NT];
+    __shared__ uint32_t odd[2][NT];
     __shared__ DocRange kept[NW][64];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -157,9 +159,9 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
 
     f32x16 acc[DB];
     float off = 0.f;  // sum of P (dP - delta)
-    auto step = [&](const char* kt, const int* dt, int row0, int j0, bool partial) __attribute__((always_inline)) {
+    auto step = [&](const char* kt, const int* dt, int row0, int j0, bool partial, bool cleaned) __attribute__((always_inline)) {
         const char* vt = kt + T::BYTES;
-        const Reader<DB> rd = reader.fresh();
+        const Reader<DB> rd = reader.template fresh<CAP>();
         f32x16 s, dp;
         staged<4 * DB, 2>([&](int i) __attribute__((always_inline)) { return rd.rows(i & 1 ? vt : kt, row0, i >> 1); },
                            [&](int i, const bf16x8& x) __attribute__((always_inline)) {
@@ -169,6 +171,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
                                else
                                    s = mfma32x32x16(x, q[kk], kk == 0 ? f32x16{} : s);
                            });
+        if (cleaned) put_scores(odd[row0 / 32][threadIdx.x], s);
         const int base = j0 + 4 * half;
         const float far = (float)(pos - base);
         float w[16];
@@ -223,6 +226,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
         }
     };
 
+    spoilt[tid] = Spoilt{0, 0};
     clear<DB>(acc);
     int slot = 0, t = window.next(0);
     bool same = true, apart = false, same_all = true;
@@ -242,12 +246,26 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
             issue(tn, slot ^ 1);
         }
         char* kt = lds + slot * SLOT;
+        bool cleaned = false;
         if ((t + 1) * TILE > least || !same_all) {
             bool bad = false;
 #pragma unroll
             for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(kt + o + 16 * tid);
-            if (__syncthreads_or(bad)) {
-                // (a query that sees such a key has no number in its lse, and so none in dz)
+            cleaned = scalar(__syncthreads_or(bad));
+            if (cleaned) {
+                int row = w0 + (lane & 31);
+                asm volatile("" : "+v"(row));  // (worked out here)
+                const bf16* own = p.q + b * p.q_batch + (int64_t)min(row, p.nq - 1) * p.q_row + head * p.D;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t seen = 0;
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j)
+                        seen |= (uint32_t)((t * TILE + 32 * h + j < limit) & (!p.kv_doc || docs[slot][32 * h + j] == doc)) << j;
+                    note_spoilt<DB>(spoilt + tid, kt, 32 * h, seen, lane);
+                    odd[h][tid] = note_scores<DB>(kt, 32 * h, own, p.D, lane);
+                }
+                __syncthreads();
                 for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(kt + o + 16 * tid);
                 __syncthreads();
             }
@@ -256,11 +274,13 @@ __global__ __launch_bounds__(NT, 2) void masked_dq(Params p) {
         for (int h = 0; h < 2; ++h) {
             const int j0 = t * TILE + 32 * h;
             if (j0 >= lim_hi || apart) continue;
-            step(kt, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same);
+            step(kt, docs[slot], 32 * h, j0, j0 + 32 > lim_lo || !same, cleaned);
         }
         t = tn, same = same_n, apart = apart_n, same_all = same_all_n;
         slot ^= 1;
     }
+    // (a key with an infinity: its score is infinite, and dz 0, by the cap or by P, or NaN)
+    put_spoilt<DB>(spoilt + tid, acc, true);
     off = sum_halves(off);
     if (!in) return;
     if (lane < 32) {
@@ -290,7 +310,8 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     constexpr int LDS = 2 * SLOT + (V_LDS ? BLOCK * T::RB : 0);
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ __attribute__((aligned(16))) QueryTile<ROWS> brought[2];
-    __shared__ Spoilt spoilt[NT];
+    __shared__ Spoilt spoilt_v[NT], spoilt_k[NT];
+    __shared__ uint32_t odd[ROWS / 32][NT];
     __shared__ DocRange kept[NW][64];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -368,7 +389,8 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
     };
 
     f32x16 dk[DB], dv[DB];
-    auto step = [&](const char* qt, const QueryTile<ROWS>& rows, int row0, int i0, float slope2, bool partial) __attribute__((always_inline)) {
+    auto step = [&](const char* qt, const QueryTile<ROWS>& rows, int row0, int i0, float slope2, bool partial,
+                    bool cleaned) __attribute__((always_inline)) {
         const char* gt = qt + TB;
         const Reader<DB> rd = reader.fresh();
         f32x16 s, dp;
@@ -399,6 +421,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
                 else
                     dp = mfma32x32x16(o.a, v[kk], dp);
             });
+        if (cleaned) put_scores(odd[row0 / 32][threadIdx.x], s);
         const int base = i0 + 4 * half;
         const float far = (float)(sq.pos0 + base - j);
         float w[16], z[16];
@@ -445,7 +468,7 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
         add_rows<DB, 1>(dk, o, rd, qt, row0);
     };
 
-    spoilt[tid] = Spoilt{0, 0};
+    spoilt_v[tid] = spoilt_k[tid] = Spoilt{0, 0};
     clear<DB>(dk);
     clear<DB>(dv);
     int slot = 0, g = 0, t = 0;
@@ -486,20 +509,28 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
         const float slope2 = BIAS && p.slopes ? p.slopes[kh * p.G + g] * LOG2E : 0.f;
         char* qt = lds + slot * SLOT;
         const int i0 = t * ROWS;
+        bool cleaned = false;
         if (i0 + ROWS > p.nq || k0 + BLOCK > limit_of(p, sq, i0) || !same_all) {
             bool bad = false;
 #pragma unroll 1
             for (int o = 0; o < SLOT; o += 16 * NT) bad |= not_finite16(qt + o + 16 * tid);
-            if (__syncthreads_or(bad)) {
+            cleaned = scalar(__syncthreads_or(bad));
+            if (cleaned) {
+                int row = j;
+                asm volatile("" : "+v"(row));  // (worked out here)
+                const bf16* own = p.k + b * p.k_batch + (int64_t)min(row, sq.len - 1) * p.k_row + kh * p.D;
+#pragma unroll 1
                 for (int h = 0; h < ROWS; h += 32) {
                     uint32_t seen = 0;
                     for (int r = 0; r < 32; ++r) {
                         const int i = i0 + h + r, d = brought[slot].doc[h + r];
                         seen |= (uint32_t)((i >= from) & (i < p.nq) & (!p.kv_doc || d == doc)) << r;
                     }
-                    note_spoilt<DB>(spoilt + tid, qt + TB, h, seen, lane);
+                    note_spoilt<DB>(spoilt_v + tid, qt + TB, h, seen, lane);
+                    note_spoilt<DB>(spoilt_k + tid, qt, h, seen, lane);
+                    odd[h / 32][tid] = note_scores<DB>(qt, h, own, p.D, lane);
                 }
-                // (a query that is no number has none in its lse, and so none in P and dz)
+                // (dP needs no note: a query whose dy is not finite has NaN in its delta)
                 __syncthreads();
                 for (int o = 0; o < SLOT; o += 16 * NT) make_finite16(qt + o + 16 * tid);
                 __syncthreads();
@@ -509,12 +540,15 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
         for (int h = 0; h < ROWS; h += 32) {
             const int ih = i0 + h;
             if (apart || ih >= p.nq || w0 >= limit_of(p, sq, min(ih + 31, p.nq - 1))) continue;
-            step(qt, brought[slot], h, ih, slope2, ih + 32 > p.nq || w0 + 32 > limit_of(p, sq, ih) || !same);
+            step(qt, brought[slot], h, ih, slope2, ih + 32 > p.nq || w0 + 32 > limit_of(p, sq, ih) || !same,
+                 cleaned);
         }
         g = gn, t = tn, same = same_n, apart = apart_n, same_all = same_all_n, more = more_n;
         slot ^= 1;
     }
-    put_spoilt<DB>(spoilt + tid, dv);
+    put_spoilt<DB>(spoilt_v + tid, dv);
+    // (a query with an infinity: its scores are infinite, and dz 0, by the cap, or NaN)
+    put_spoilt<DB>(spoilt_k + tid, dk, true);
     if (!in) return;
     constexpr int CH = 32 * DB;
     float* part = p.pieces > 1 ? p.part_o + (((int64_t)piece * p.B * p.KH + bk) * p.nkv + j) * (2 * CH) : nullptr;
