@@ -131,3 +131,23 @@ def test_scores_of_plus_infinity_are_no_numbers(shape):
         assert torch.equal(got[n][:, others], clean[n][:, others]) and got[n][:, 200].isnan().all(), n
     for n in ("dk", "dv"):
         assert got[n][:, :201].isnan().all() and torch.equal(got[n][:, 201:], clean[n][:, 201:]), n
+
+
+@pytest.mark.parametrize("bad", [float("nan"), INF, -INF], ids=str)
+@pytest.mark.parametrize("shape", [(1, 100, 2, 1, 64), (40, 100, 4, 2, 64), (20, 200, 4, 4, 128), (30, 150, 2, 1, 40)], ids=str)
+def test_queries_and_gradients_of_the_past_do_not_count(shape, bad):
+    """Causal, without documents: no number in an early query and an early
+    gradient; keys behind them do not see it, bit for bit."""
+    B, n, H, KH, D = shape
+    (q, k, v, dy), _ = _inputs(B, n, n, H, KH, D, seed=85)
+    clean = _call(q, k, v, ref.Masks(), True, 0.125, 0.0, dy)
+    q[:, 30], dy[:, 20] = bad, bad
+    got = _call(q, k, v, ref.Masks(), True, 0.125, 0.0, dy)
+    for t in ("dk", "dv"):
+        assert torch.isfinite(clean[t]).all() and torch.equal(got[t][:, 31:], clean[t][:, 31:]), t
+        assert got[t][:, :21].isnan().all() or t == "dv" and not torch.isfinite(got[t][:, :21]).any(), t
+    others = torch.ones(n, dtype=torch.bool)
+    others[30] = False
+    assert torch.equal(got["y"][:, others], clean["y"][:, others])
+    others[20] = False
+    assert torch.equal(got["dq"][:, others], clean["dq"][:, others])
