@@ -459,12 +459,24 @@ __device__ __forceinline__ void make_finite16(char* a) {
 struct Spoilt {
     uint64_t plus, minus;
 };
-// The 32 rows from row0 of a tile; bit j of `seen`: the lane sees row j.
+// Which of the 32 rows from row0 of a tile have any (a bit each), if some lane
+// sees such a row, `seen` its rows; else 0: nobody's sums and scores take any.
 template <int DB>
-__device__ __forceinline__ void note_spoilt(Spoilt* mine, const char* tile, int row0, uint32_t seen, int lane) {
+__device__ __forceinline__ uint32_t spoilt_rows(const char* tile, int row0, uint32_t seen, int lane) {
+    bool bad = false;
+#pragma unroll 1
+    for (int c = lane >> 5; c < Tile<DB>::VECS; c += 2) bad |= not_finite16(tile + (row0 + (lane & 31)) * Tile<DB>::RB + 16 * c);
+    const uint64_t both = __ballot(bad);
+    const uint32_t rows = (uint32_t)both | (uint32_t)(both >> 32);
+    return __any((seen & rows) != 0) ? rows : 0u;
+}
+// Those rows of a tile; bit j of `seen`: the lane sees row j.
+template <int DB>
+__device__ __forceinline__ void note_spoilt(Spoilt* mine, const char* tile, int row0, uint32_t rows, uint32_t seen, int lane) {
     uint64_t plus = mine->plus, minus = mine->minus;
 #pragma unroll 1
-    for (int j = 0; j < 32; ++j) {
+    for (; rows; rows &= rows - 1) {
+        const int j = __builtin_ctz(rows);
         const bool sees = seen >> j & 1;
 #pragma unroll 1
         for (int g = 0; g < 4 * DB; ++g) {
@@ -501,21 +513,27 @@ __device__ __forceinline__ void put_spoilt(const Spoilt* mine, f32x16 (&acc)[DB]
         }
 }
 
-// What the infinities and NaN of the 32 rows from row0 of a tile make of the
-// lane's scores with them, `own` its own row in memory: bit r for infinity in
-// register r, bit 16 + r for -infinity, both for NaN.  (One by one: a product of
-// matrices in this place would cost the kernels 25 registers more.)
+// What those rows make of the lane's scores with them, `own` its own row in
+// memory: bit r for infinity in register r, bit 16 + r for -infinity, both for
+// NaN.  (One by one: a product of matrices in this place would cost the kernels
+// 25 registers more.)
 template <int DB>
-__device__ __forceinline__ uint32_t note_scores(const char* tile, int row0, const bf16* own, int D, int lane) {
+__device__ __forceinline__ uint32_t note_scores(const char* tile, int row0, uint32_t rows, const bf16* own, int D, int lane) {
     uint32_t odd = 0;
 #pragma unroll 1
-    for (int r = 0; r < 16; ++r) {
-        const int j = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+    for (; rows; rows &= rows - 1) {
+        const int j = __builtin_ctz(rows), r = 4 * (j >> 3) + (j & 3);
+        if ((j >> 2 & 1) != lane >> 5) continue;
         float z = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < D; ++c) {
-            const float x = bf16_to_f32(*(const bf16*)(tile + (row0 + j) * Tile<DB>::RB + 16 * (c >> 3 ^ Tile<DB>::swizzle(j)) + 2 * (c & 7)));
-            if (!(fabsf(x) < INFINITY)) z = __builtin_fmaf(x, bf16_to_f32(own[c]), z);
+        for (int g = 0; g < D / 8; ++g) {
+            const char* at = tile + (row0 + j) * Tile<DB>::RB + 16 * (g ^ Tile<DB>::swizzle(j));
+            if (!not_finite16(at)) continue;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                const float x = bf16_to_f32(((const bf16*)at)[e]);
+                if (!(fabsf(x) < INFINITY)) z = __builtin_fmaf(x, bf16_to_f32(own[8 * g + e]), z);
+            }
         }
         odd |= (uint32_t)!(z < INFINITY) << r | (uint32_t)!(z > -INFINITY) << (16 + r);
     }

@@ -262,8 +262,9 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_dq(Params p) {
 #pragma unroll 1
                     for (int j = 0; j < 32; ++j)
                         seen |= (uint32_t)((t * TILE + 32 * h + j < limit) & (!p.kv_doc || docs[slot][32 * h + j] == doc)) << j;
-                    note_spoilt<DB>(spoilt + tid, kt, 32 * h, seen, lane);
-                    odd[h][tid] = note_scores<DB>(kt, 32 * h, own, p.D, lane);
+                    const uint32_t rows = spoilt_rows<DB>(kt, 32 * h, seen, lane);
+                    note_spoilt<DB>(spoilt + tid, kt, 32 * h, rows, seen, lane);
+                    odd[h][tid] = note_scores<DB>(kt, 32 * h, rows, own, p.D, lane);
                 }
                 __syncthreads();
                 for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(kt + o + 16 * tid);
@@ -526,9 +527,10 @@ __global__ __launch_bounds__(NT, 2) void masked_dkv(Params p) {
                         const int i = i0 + h + r, d = brought[slot].doc[h + r];
                         seen |= (uint32_t)((i >= from) & (i < p.nq) & (!p.kv_doc || d == doc)) << r;
                     }
-                    note_spoilt<DB>(spoilt_v + tid, qt + TB, h, seen, lane);
-                    note_spoilt<DB>(spoilt_k + tid, qt, h, seen, lane);
-                    odd[h / 32][tid] = note_scores<DB>(qt, h, own, p.D, lane);
+                    note_spoilt<DB>(spoilt_v + tid, qt + TB, h, spoilt_rows<DB>(qt + TB, h, seen, lane), seen, lane);
+                    const uint32_t rows = spoilt_rows<DB>(qt, h, seen, lane);
+                    note_spoilt<DB>(spoilt_k + tid, qt, h, rows, seen, lane);
+                    odd[h / 32][tid] = note_scores<DB>(qt, h, rows, own, p.D, lane);
                 }
                 // (dP needs no note: a query whose dy is not finite has NaN in its delta)
                 __syncthreads();

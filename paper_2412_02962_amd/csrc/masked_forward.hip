@@ -293,8 +293,10 @@ __global__ __launch_bounds__(NT, DB <= 2 ? 3 : 2) void masked_forward(Params p) 
 #pragma unroll
             for (int o = 0; o < T::BYTES; o += 16 * NT) bad |= not_finite16(vt + o + 16 * tid);
             if (__syncthreads_or(bad)) {
-                for (int h = 0; h < 2; ++h)
-                    note_spoilt<DB>(spoilt + tid, vt, 32 * h, keys_seen(p, row, docs[slot] + 32 * h, t * TILE + 32 * h), lane);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t seen = keys_seen(p, row, docs[slot] + 32 * h, t * TILE + 32 * h);
+                    note_spoilt<DB>(spoilt + tid, vt, 32 * h, spoilt_rows<DB>(vt, 32 * h, seen, lane), seen, lane);
+                }
                 __syncthreads();
                 for (int o = 0; o < T::BYTES; o += 16 * NT) make_finite16(vt + o + 16 * tid);
                 __syncthreads();
@@ -445,7 +447,8 @@ __global__ __launch_bounds__(NT, 1) void masked_few(Params p) {
             bool bad = false;
             for (int o = 0; o < HALF; o += 1024) bad |= not_finite16(vt + o + 16 * lane);
             if (__any(bad)) {
-                note_spoilt<DB>(spoilt + tid, vt, 0, keys_seen(p, row, docs[wave][slot], j0), lane);
+                const uint32_t seen = keys_seen(p, row, docs[wave][slot], j0);
+                note_spoilt<DB>(spoilt + tid, vt, 0, spoilt_rows<DB>(vt, 0, seen, lane), seen, lane);
                 for (int o = 0; o < HALF; o += 1024) make_finite16(vt + o + 16 * lane);
             }
         }
