@@ -89,19 +89,20 @@ int64_t range_bytes(const pcpp_masked_geom_t* g) {
 // four wavefronts then share the keys (forward, us: 1000 queries and keys, 4
 // heads of 64, 22 and 14; 4000, one of 128, 99 and 54; 500, 8 of 128, at the
 // limit, 17.9 and 17.1; with twice the workgroups slower: 2000, 8 of 64, 39 and
-// 45).  How many pieces of the keys: as many as give every compute unit two workgroups, of eight tiles of
-// 32 keys or more (one token on up to 16384 keys, 64 groups: 80 us; with half as
+// 45; so too where walks are short, 4 x 333, 16 of 64, causal, 14.4 and 18.2, or
+// uneven, 2 x 4096, 10 of 64, 9 documents, 66 and 99).  How many pieces of the
+// keys: as many as give every compute unit two workgroups, of eight tiles of 32
+// keys or more (one token on up to 16384 keys, 64 groups: 80 us; with half as
 // many pieces 98, with twice as many 95).
 struct FewPlan {
     bool use;
     int pieces, row_blocks;
 };
 FewPlan few_plan(const pcpp_masked_geom_t* g) {
-    const int64_t rows = (int64_t)g->heads / g->kv_heads * g->n_q;
-    const int64_t most = (int64_t)g->batch * g->kv_heads * ((rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS);
-    FewPlan f = {rows <= 2 * MASKED_FEW_ROWS || (most <= 128 && g->n_kv >= 128), 1, (int)((rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS)};
+    const int64_t rows = (int64_t)g->heads / g->kv_heads * g->n_q, row_blocks = (rows + MASKED_FEW_ROWS - 1) / MASKED_FEW_ROWS;
+    const int64_t groups = (int64_t)g->batch * g->kv_heads * row_blocks, tiles = (g->n_kv + 31) / 32;
+    FewPlan f = {rows <= 2 * MASKED_FEW_ROWS || (groups <= 128 && g->n_kv >= 128), 1, (int)row_blocks};
     if (!f.use) return f;
-    const int64_t groups = (int64_t)g->batch * g->kv_heads * f.row_blocks, tiles = (g->n_kv + 31) / 32;
     int64_t pieces = (512 + groups - 1) / groups;
     if (pieces > tiles / 8) pieces = tiles / 8;
     f.pieces = (int)(pieces > 0 ? pieces : 1);
@@ -120,7 +121,7 @@ int64_t delta_bytes(const pcpp_masked_geom_t* g) { return round16((int64_t)g->ba
 // blocks of keys than two to a compute unit (causal, of uneven length: four), as
 // many as fill them, of two tiles of 64 queries or more (dk and dv with eight or
 // more, and with two: 434 queries and keys, 4 heads of 128, 39 and 21 us; 1000
-// causal, 8 heads on 2, 47 and 38; no size slower).
+// causal, 8 heads on 2, 47 and 38).
 int kv_pieces(const pcpp_masked_geom_t* g) {
     const int64_t blocks = (int64_t)g->batch * g->kv_heads * ((g->n_kv + 127) / 128);
     const int64_t tiles = (int64_t)g->heads / g->kv_heads * ((g->n_q + 63) / 64);

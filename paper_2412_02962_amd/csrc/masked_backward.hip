@@ -12,10 +12,14 @@
 // Five products of the forward's two, and the exponentials twice: bound by the
 // vector unit and by waits for LDS, with 16 DB sums of 32 x 32 a lane (twice that
 // for masked_dkv) leaving room for two wavefronts a SIMD and few operands ahead.
-// 8192 causal, 16 heads of 128 on 4 of the keys: masked_dq 425 us (970 TFLOP/s),
-// masked_dkv 609 (900); capped and biased 576 and 724, the matrix unit busy for
-// 29 % of the cycles in both, the vector unit for 52 and 41.  2 x 4096, 10 heads
-// of 64: 180 (715) and 278 (620).
+// 8192 causal, 16 heads of 128 on 4 of the keys: masked_dq 408 us (1010 TFLOP/s),
+// masked_dkv 586 (940); capped and biased 532 and 693, the matrix unit busy for
+// 31 % of the cycles in both, the vector unit for 56 and 44.  2 x 4096, 10 heads
+// of 64: 162 (795) and 249 (690).
+//
+// P and dz are rounded to bf16, the matrix instructions' operands: half a step
+// each, independent; the gradients are 0.0019 to 0.0024 off so, their own rounding
+// 0.0017.  (Two bf16 each would double the products over keys and queries.)
 
 #include <type_traits>
 

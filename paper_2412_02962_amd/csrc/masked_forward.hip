@@ -11,11 +11,16 @@
 // of some run under the exponentials of others (8192 queries and keys, bf16: 16
 // heads of 64 337 us, 32 keys a step 402; of 128 562, else 654).
 //
+// The probabilities are rounded to bf16, the matrix instructions' operands: up to
+// half a step each, independent.  y is 0.0019 to 0.0024 off so, its own rounding
+// 0.0017.  (Two bf16 each, as masked_few has them, are twice the products.)
+//
 // Bound by the vector unit and the wavefronts' own waits, two or three of them to
 // a SIMD: 8192 causal, 16 heads of 128 on 4 of the keys, capped and biased
-// (three transcendental operations a score), 404 us and 680 TFLOP/s, the matrix
-// unit busy for 27 % of the cycles and the vector unit for 52; without cap and
-// bias 305 us, 900 TFLOP/s; not causal, 16 heads of keys too, 565 us, 970.
+// (three transcendental operations a score), with lse 390 us and 705 TFLOP/s, the
+// matrix unit busy for 28 % of the cycles and the vector unit for 57; without cap
+// and bias 306 us, 900 TFLOP/s, without lse too 292, 940; not causal, 16 heads of
+// keys too, 546 us, 1010 (with lse 570).
 
 #include <type_traits>
 
