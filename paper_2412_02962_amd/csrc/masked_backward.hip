@@ -12,10 +12,10 @@
 // Five products of the forward's two, and the exponentials twice: bound by the
 // vector unit and by waits for LDS, with 16 DB sums of 32 x 32 a lane (twice that
 // for masked_dkv) leaving room for two wavefronts a SIMD and few operands ahead.
-// 8192 causal, 16 heads of 128 on 4 of the keys: masked_dq 408 us (1010 TFLOP/s),
-// masked_dkv 586 (940); capped and biased 532 and 693, the matrix unit busy for
+// 8192 causal, 16 heads of 128 on 4 of the keys: masked_dq 402 us (1025 TFLOP/s),
+// masked_dkv 576 (955); capped and biased 538 and 697, the matrix unit busy for
 // 31 % of the cycles in both, the vector unit for 56 and 44.  2 x 4096, 10 heads
-// of 64: 162 (795) and 249 (690).
+// of 64: 159 (810) and 251 (685).
 //
 // P and dz are rounded to bf16, the matrix instructions' operands: half a step
 // each, independent; the gradients are 0.0019 to 0.0024 off so, their own rounding

@@ -17,10 +17,10 @@
 //
 // Bound by the vector unit and the wavefronts' own waits, two or three of them to
 // a SIMD: 8192 causal, 16 heads of 128 on 4 of the keys, capped and biased
-// (three transcendental operations a score), with lse 390 us and 705 TFLOP/s, the
-// matrix unit busy for 28 % of the cycles and the vector unit for 57; without cap
-// and bias 306 us, 900 TFLOP/s, without lse too 292, 940; not causal, 16 heads of
-// keys too, 546 us, 1010 (with lse 570).
+// (three transcendental operations a score), with lse 389 us and 705 TFLOP/s, the
+// matrix unit busy for 28 % of the cycles and the vector unit for 58; without cap
+// and bias 301 us, 915 TFLOP/s, without lse too 289, 950; not causal, 16 heads of
+// keys too, 550 us, 1000 (with lse 572).
 
 #include <type_traits>
 
@@ -78,8 +78,8 @@ struct Context {
 // probabilities: where one key dominates, the rounding of its weight is above
 // and below the line and cancels.  In lse nothing would cancel it: off by up to
 // 2^-8 there, and with it all of the row's probabilities in the backward pass.
-// (Without lse and with it, us: 8192 causal, 16 heads of 128 on 4, 289 and 303;
-// 8192, 16 heads of 64, 345 and 366; packed documents 67.0 and 67.1.)
+// (Without lse and with it, us: 8192 causal, 16 heads of 128 on 4, 289 and 301;
+// 8192, 16 heads of 64, 343 and 364; packed documents 67.2 and 67.0.)
 // after_scores: what may run once the keys have been used.
 template <int DB, int HB, bool CAP, bool BIAS, bool TWO, bool EXACT, typename After>
 __device__ __forceinline__ void step(const Context<DB>& c, State<DB>& st, const char* kt, const char* vt, const int* docs, int j0,
